@@ -8,6 +8,11 @@
  *
  *   gp_update_summaries  every step: the two EMA query summaries (Sec. 3.2)
  *   gp_decode_attention  every step: paged GQA decode attention (Sec. 3.1)
+ *   gp_append_rope       prompts and new tokens into the cache, rotated on the way
+ *                        (bfloat16, float32, or 8-bit values with scales)
+ *   gp_decode_attention_q8     decode attention over the 8-bit cache
+ *   gp_select_pages, gp_decode_attention_pages   attention over the pages that
+ *                        a bound on their logits selects
  *   gp_boundary_score    at boundaries: calibrated, rotated summaries scored
  *                        against the cached keys, top-p working sets (Sec. 3.2,
  *                        App. E.1) and token importance (Sec. 3.3)
@@ -134,7 +139,7 @@ enum {
 };
 
 /* Which workspace gp_workspace_bytes() sizes. */
-enum { GP_OP_DECODE = 0, GP_OP_SCORE = 1, GP_OP_APPLY = 2 };
+enum { GP_OP_DECODE = 0, GP_OP_SCORE = 1, GP_OP_APPLY = 2, GP_OP_SELECT = 3 };
 
 typedef struct {
     void *k;                 /* [pool_pages][num_kv_heads][page_size][head_dim] */
@@ -495,7 +500,139 @@ gp_status_t gp_append_step(const gp_kv_layer_t *layers, int32_t n_layers, const 
                            float *qstate, int32_t num_slots, float beta_s, float beta_l,
                            hipStream_t stream);
 
-/* Bytes of workspace an operation needs (op = GP_OP_DECODE / SCORE / APPLY). */
+/* A cache of 8-bit values: K and V pools of e4m3 codes (4 exponent and 3
+ * mantissa bits, no infinities, 0x7f and 0xff are NaN) with one float32 scale
+ * per page and KV head, so that element x of a page stands for x * scale.
+ * Half the bytes of a bfloat16 cache per token and 8 more per page and head.
+ * Scales are positive and finite; gp_append_rope_q8 makes powers of two.
+ * Queries, new rows and outputs of a call on such a cache are bfloat16.  Pools
+ * lie at multiples of 16 bytes (GP_ERR_INVALID otherwise). */
+typedef struct {
+    void *k;                 /* [pool_pages][num_kv_heads][page_size][head_dim] */
+    void *v;                 /* same layout as k                                */
+    float *k_scale;          /* [pool_pages][num_kv_heads]                      */
+    float *v_scale;          /* same layout as k_scale                          */
+    int32_t pool_pages;
+    int32_t num_kv_heads;
+    int32_t page_size;       /* must be 16                                      */
+    int32_t head_dim;        /* 64 or 128                                       */
+} gp_kv8_layer_t;
+
+/* New tokens into the paged cache of one layer, keys and queries rotated on
+ * the way (Sec. 3.1 paged cache; half-split rotary pairs, as everywhere in
+ * this library): single tokens of a decode step as well as whole prompts or
+ * chunks of them.
+ *  - Request r brings n_r = tok_start[r + 1] - tok_start[r] tokens, rows
+ *    tok_start[r] .. of k_new, v_new and q (tok_start [num_reqs + 1] int32 on
+ *    the device, not decreasing, from 0 to num_tokens at most); with tok_start
+ *    NULL every request brings one, row r (num_tokens == num_reqs, else
+ *    GP_ERR_INVALID).
+ *  - Row strides are in elements, so that q, k and v may lie side by side in
+ *    one projection's output; within a row [heads][head_dim] is contiguous.
+ *  - Token j of request r has the logical index t = positions[r] + 1 + j:
+ *    positions[r] is that of the request's last token so far, as in
+ *    gp_append_step (-1 before the first).  Pair (x_i, x_{i + d/2}) of its keys
+ *    and queries turns by t * rope_theta^(-2 i / d): the angle in 64 bits, its
+ *    cosine and sine rounded to float32, products and their sum in float32,
+ *    rounded once to the row's type.
+ *  - The rotated keys and the values go to slots m_r + j of the request's
+ *    pages, if all n_r fit (m_r + n_r <= P_r * page_size); a request without
+ *    that room takes none of them.  A held request is left out altogether.
+ *  - q_out [num_tokens][num_q_heads][head_dim] takes the rotated queries of
+ *    all requests that are not held, with or without room (q NULL: no
+ *    queries; num_q_heads is then not looked at).  q_out may be q itself
+ *    where q_stride == num_q_heads * head_dim; any other overlap is refused.
+ *  - advance != 0: seq_lens[r] and positions[r] of the requests that took
+ *    their tokens then grow by n_r (pass 0 for every layer of a model but the
+ *    last, as in gp_decode_step).
+ * Rows and pools may lie at any multiple of their element's size (8-bit
+ * pools: 16 bytes).  Pages that requests share are not copied: the caller
+ * gives a request private pages from m_r on.  The page states are read on the
+ * device, so that nothing but the sums num_tokens and num_reqs is needed on
+ * the host.
+ *
+ * gp_append_rope_q8: rows are bfloat16, the pools 8-bit.  A page's scale of a
+ * KV head is the least power of two s = 2^e, e >= -100, with |x| <= 448 s for
+ * every finite value the call brings to the page, and no less than the scale
+ * that the page had if it held tokens before; where it grows, the codes of the
+ * older tokens are rounded again, to nearest even (exact unless one falls
+ * below the format's normal range).  Codes are x / s rounded to nearest even;
+ * infinities and NaN become NaN.  The keys are rounded from their float32
+ * rotation. */
+gp_status_t gp_append_rope(const gp_kv_layer_t *kv, const gp_page_state_t *ps, int32_t *positions,
+                           const int32_t *tok_start, int32_t num_tokens, const void *q, int64_t q_stride,
+                           void *q_out, const void *k_new, int64_t k_stride, const void *v_new,
+                           int64_t v_stride, int32_t num_q_heads, float rope_theta, int32_t advance,
+                           hipStream_t stream);
+gp_status_t gp_append_rope_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps, int32_t *positions,
+                              const int32_t *tok_start, int32_t num_tokens, const void *q,
+                              int64_t q_stride, void *q_out, const void *k_new, int64_t k_stride,
+                              const void *v_new, int64_t v_stride, int32_t num_q_heads, float rope_theta,
+                              int32_t advance, hipStream_t stream);
+
+/* gp_decode_attention over an 8-bit cache (Sec. 3.1): the same arguments and
+ * rules, q_post and out bfloat16.  The codes are used as the values they stand
+ * for, without further rounding.  Takes the decode workspace of a bfloat16
+ * cache of the shape. */
+gp_status_t gp_decode_attention_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps,
+                                   const void *q_post, int32_t num_q_heads, float scale, void *out,
+                                   void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Bounds of the cached keys, for gp_select_pages: of every page and KV head
+ * the least (bounds[page][head][0]) and the greatest (.. [1]) value that each
+ * head dim takes over the page's resident tokens.  bounds [pool_pages]
+ * [num_kv_heads][2][head_dim] in the KV dtype (8-bit cache: bfloat16, of the
+ * values the codes stand for, rounded to nearest).  A NaN among the keys gives
+ * NaN.  Made for the pages that hold tokens from_tokens[r] .. m_r - 1
+ * (from_tokens [num_reqs] int32 on the device; NULL: from 0), of each request
+ * at most max_update pages, counted from the first (0: no limit; a limit keeps
+ * the launch small where the lengths are known, e.g. 1 after a decode step).
+ * Other pages' bounds stay as they were.  To be called after tokens went in
+ * and, for all of a request's pages, after a compaction moved its rows.  A
+ * held request is left out. */
+gp_status_t gp_page_bounds(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const int32_t *from_tokens,
+                           int32_t max_update, void *bounds, hipStream_t stream);
+gp_status_t gp_page_bounds_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps,
+                              const int32_t *from_tokens, int32_t max_update, void *bounds,
+                              hipStream_t stream);
+
+/* The pages of each request and KV head that decode attention is to read, by a
+ * bound on the logits they can give: score(r, h, p) = sum over the query heads
+ * g of KV head h and over the dims d of max(q_gd * least_pd, q_gd *
+ * greatest_pd), the sum in 64 bits, rounded once to float32 (a q_gd of zero
+ * adds nothing, also where a bound is infinite).  With n =
+ * ceil(m_r / page_size) pages resident, selected[r][h] [budget] gets min(n,
+ * budget) logical page indices in ascending order, then -1: the first
+ * keep_first and the last keep_last pages, and of the others those of the
+ * highest scores (a NaN counts as higher than any; ties go to the lower page).
+ * Where n <= budget these are all pages and no bounds are read.  A held
+ * request's lists are not written.  bounds and q_post are of type `dtype`
+ * (bounds as gp_page_bounds leaves them); 0 <= keep_first, keep_last, their sum
+ * at most the budget, 1 <= budget <= 8192 (GP_ERR_INVALID otherwise); tables
+ * up to 8192 pages wide.  Takes the GP_OP_SELECT workspace. */
+gp_status_t gp_select_pages(const void *bounds, gp_dtype_t dtype, const gp_page_state_t *ps,
+                            const void *q_post, int32_t num_q_heads, int32_t num_kv_heads,
+                            int32_t head_dim, int32_t budget, int32_t keep_first, int32_t keep_last,
+                            int32_t *selected, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* Decode attention over listed pages: gp_decode_attention (or
+ * gp_decode_attention_q8) in which KV head h of request r attends over the
+ * tokens below m_r of the logical pages selected[r][h][0 .. min(n, budget) -
+ * 1], n = ceil(m_r / page_size), and no others.  An entry that is no resident
+ * page (-1, or n and above) adds nothing; a page listed twice counts twice.  A
+ * head whose list has no token gets a zero output.  Lists as gp_select_pages
+ * writes them (from any step: they name table columns, not physical pages).
+ * Takes the decode workspace of a table `budget` pages wide. */
+gp_status_t gp_decode_attention_pages(const gp_kv_layer_t *kv, const gp_page_state_t *ps,
+                                      const int32_t *selected, int32_t budget, const void *q_post,
+                                      int32_t num_q_heads, float scale, void *out, void *ws,
+                                      size_t ws_bytes, hipStream_t stream);
+gp_status_t gp_decode_attention_pages_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps,
+                                         const int32_t *selected, int32_t budget, const void *q_post,
+                                         int32_t num_q_heads, float scale, void *out, void *ws,
+                                         size_t ws_bytes, hipStream_t stream);
+
+/* Bytes of workspace an operation needs (op = GP_OP_DECODE / SCORE / APPLY / SELECT). */
 size_t gp_workspace_bytes(int32_t op, int32_t num_reqs, int32_t num_bnd, int32_t num_q_heads,
                           int32_t num_kv_heads, int32_t head_dim, int32_t max_pages,
                           int32_t page_size, gp_dtype_t dtype, int32_t n_layers);

@@ -18,7 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libgrowpage.so")
 
 GP_F32, GP_BF16 = 0, 1
-GP_OP_DECODE, GP_OP_SCORE, GP_OP_APPLY = 0, 1, 2
+GP_OP_DECODE, GP_OP_SCORE, GP_OP_APPLY, GP_OP_SELECT = 0, 1, 2, 3
 GP_COMPRESS, GP_GROW, GP_FALLBACK, GP_PREEMPT, GP_NOT_BOUNDARY = 0, 1, 2, 3, 4
 GP_SHRINK = 5
 GP_POLICY_GROWPAGE, GP_POLICY_FIXED, GP_POLICY_RANDOM, GP_POLICY_INVERSE, GP_POLICY_SHRINK = 0, 1, 2, 3, 4
@@ -32,7 +32,9 @@ GP_ERR_SCRATCH = 5
 EXPORTS = ("gp_update_summaries", "gp_decode_attention", "gp_decode_attention_noalloc", "gp_decode_attention_shared",
            "gp_decode_attention_stages", "gp_decode_step", "gp_boundary_score", "gp_boundary_score_stages",
            "gp_boundary_apply", "gp_boundary_select", "gp_boundary_decide", "gp_boundary_compact",
-           "gp_release_held", "gp_append_step", "gp_workspace_bytes", "gp_status_string", "gp_stream_read")
+           "gp_release_held", "gp_append_step", "gp_append_rope", "gp_append_rope_q8", "gp_decode_attention_q8",
+           "gp_page_bounds", "gp_page_bounds_q8", "gp_select_pages", "gp_decode_attention_pages",
+           "gp_decode_attention_pages_q8", "gp_workspace_bytes", "gp_status_string", "gp_stream_read")
 
 
 class GrowPageError(RuntimeError):
@@ -45,6 +47,12 @@ class _KVLayer(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pool_pages", ctypes.c_int32),
                 ("num_kv_heads", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int)]
+
+
+class _KV8Layer(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("pool_pages", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
 class _PageState(ctypes.Structure):
@@ -123,6 +131,19 @@ def load() -> ctypes.CDLL:
     lib.gp_append_step.restype = ctypes.c_int
     lib.gp_append_step.argtypes = [ctypes.POINTER(_KVLayer), i32, ctypes.POINTER(_PageState), vp, vp, vp, vp,
                                    i32, vp, vp, vp, i32, f32, f32, vp]
+    i64, ps_p, kv_p, kv8_p = ctypes.c_int64, ctypes.POINTER(_PageState), ctypes.POINTER(_KVLayer), ctypes.POINTER(_KV8Layer)
+    rope_args = [ps_p, vp, vp, i32, vp, i64, vp, vp, i64, vp, i64, i32, f32, i32, vp]
+    pages_args = [ps_p, vp, i32, vp, i32, f32, vp, vp, sz, vp]
+    for name, layer, rest in (("gp_append_rope", kv_p, rope_args), ("gp_append_rope_q8", kv8_p, rope_args),
+                              ("gp_decode_attention_q8", kv8_p, [ps_p, vp, i32, f32, vp, vp, sz, vp]),
+                              ("gp_page_bounds", kv_p, [ps_p, vp, i32, vp, vp]),
+                              ("gp_page_bounds_q8", kv8_p, [ps_p, vp, i32, vp, vp]),
+                              ("gp_decode_attention_pages", kv_p, pages_args),
+                              ("gp_decode_attention_pages_q8", kv8_p, pages_args)):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = [layer] + rest
+    lib.gp_select_pages.restype = ctypes.c_int
+    lib.gp_select_pages.argtypes = [vp, ctypes.c_int, ps_p, vp, i32, i32, i32, i32, i32, i32, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -166,6 +187,26 @@ class KVLayer:
     def c(self) -> _KVLayer:
         pool, hkv, b, d = self.k.shape
         return _KVLayer(_ptr(self.k), _ptr(self.v), pool, hkv, b, d, _dtype_code(self.k))
+
+
+@dataclass
+class KV8Layer:
+    """An 8-bit cache: K and V pools [pool_pages, num_kv_heads, 16, head_dim] of e4m3
+    codes (float8_e4m3fn or uint8) and their scales [pool_pages, num_kv_heads] float32."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    def c(self) -> _KV8Layer:
+        pool, hkv, b, d = self.k.shape
+        for t in (self.k, self.v):
+            if t.dtype not in (torch.float8_e4m3fn, torch.uint8) or t.shape != self.k.shape:
+                raise ValueError("8-bit pools: two tensors of one shape, float8_e4m3fn or uint8")
+        for t in (self.k_scale, self.v_scale):
+            if t.dtype != torch.float32 or tuple(t.shape) != (pool, hkv):
+                raise ValueError("scales of an 8-bit cache: float32 [pool_pages, num_kv_heads]")
+        return _KV8Layer(_ptr(self.k), _ptr(self.v), _ptr(self.k_scale), _ptr(self.v_scale), pool, hkv, b, d)
 
 
 @dataclass
@@ -382,3 +423,129 @@ def gp_append_step(layers: list[KVLayer], ps: PageState, positions: torch.Tensor
                                _ptr(q_pre), q_pre.shape[2], _ptr(slot_ids), _ptr(init), _ptr(qstate),
                                qstate.shape[1], float(beta_s), float(beta_l), _stream(stream))
     _check(st, "gp_append_step")
+
+
+def _rows(t: torch.Tensor, name: str) -> int:
+    """The stride from row to row of [tokens, heads, head_dim], contiguous within a row."""
+    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"{name}: [tokens, heads, head_dim], the heads of a token side by side")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _append_rope(name, kv, dtype, ps, positions, k_new, v_new, rope_theta, q, q_out, tok_start, advance, stream):
+    _, hkv, _, d = kv.k.shape
+    T = k_new.shape[0]
+    for t, heads, what in ((k_new, hkv, "k_new"), (v_new, hkv, "v_new"), (q, None, "q")):
+        if t is not None and (t.dtype != dtype or t.dim() != 3 or t.shape[0] != T or t.shape[2] != d or
+                              (heads is not None and t.shape[1] != heads)):
+            raise ValueError(f"{name}: {what} [tokens, heads, head_dim], {dtype}")
+    if q is not None and (q_out is None or q_out.dtype != dtype or q_out.shape != q.shape):
+        raise ValueError(f"{name}: q_out of q's shape and dtype")
+    if tok_start is not None and (tok_start.dtype != torch.int32 or tok_start.numel() != ps.page_table.shape[0] + 1):
+        raise ValueError(f"{name}: tok_start [num_reqs + 1] int32")
+    c_kv, c_ps = kv.c(), ps.c()
+    st = getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(positions), _ptr(tok_start), T,
+                               None if q is None else q.data_ptr(), 0 if q is None else _rows(q, "q"),
+                               None if q is None else _ptr(q_out), k_new.data_ptr(), _rows(k_new, "k_new"),
+                               v_new.data_ptr(), _rows(v_new, "v_new"), 0 if q is None else q.shape[1],
+                               float(rope_theta), int(bool(advance)), _stream(stream))
+    _check(st, name)
+
+
+def gp_append_rope(kv: KVLayer, ps: PageState, positions: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                   rope_theta: float, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+                   tok_start: torch.Tensor | None = None, advance: bool = True, stream=None) -> None:
+    """New tokens into the cache, keys and queries rotated: k_new, v_new [T, Hkv, d] and
+    q [T, Hq, d] with any stride from token to token; tok_start [R + 1] int32, or None
+    for one token per request; q_out [T, Hq, d] takes the rotated queries."""
+    _append_rope("gp_append_rope", kv, kv.k.dtype, ps, positions, k_new, v_new, rope_theta, q, q_out, tok_start,
+                 advance, stream)
+
+
+def gp_append_rope_q8(kv: KV8Layer, ps: PageState, positions: torch.Tensor, k_new: torch.Tensor,
+                      v_new: torch.Tensor, rope_theta: float, q: torch.Tensor | None = None,
+                      q_out: torch.Tensor | None = None, tok_start: torch.Tensor | None = None,
+                      advance: bool = True, stream=None) -> None:
+    """gp_append_rope into an 8-bit cache (rows bfloat16)."""
+    _append_rope("gp_append_rope_q8", kv, torch.bfloat16, ps, positions, k_new, v_new, rope_theta, q, q_out,
+                 tok_start, advance, stream)
+
+
+def _of(t: torch.Tensor, dtype, name: str) -> int:
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: {dtype}, not {t.dtype}")
+    return _ptr(t)
+
+
+def gp_decode_attention_q8(kv: KV8Layer, ps: PageState, q_post: torch.Tensor, scale: float, out: torch.Tensor,
+                           ws: torch.Tensor, stream=None) -> None:
+    """Decode attention over an 8-bit cache; q_post and out bfloat16."""
+    c_kv, c_ps = kv.c(), ps.c()
+    st = load().gp_decode_attention_q8(ctypes.byref(c_kv), ctypes.byref(c_ps), _of(q_post, torch.bfloat16, "q_post"),
+                                       q_post.shape[1], scale, _of(out, torch.bfloat16, "out"), _ptr(ws), ws.numel(),
+                                       _stream(stream))
+    _check(st, "gp_decode_attention_q8")
+
+
+def _page_bounds(name, kv, dtype, ps, bounds, from_tokens, max_update, stream):
+    pool, hkv, _, d = kv.k.shape
+    if bounds.dtype != dtype or tuple(bounds.shape) != (pool, hkv, 2, d):
+        raise ValueError(f"{name}: bounds [pool_pages, num_kv_heads, 2, head_dim], {dtype}")
+    if from_tokens is not None and (from_tokens.dtype != torch.int32 or from_tokens.numel() != ps.page_table.shape[0]):
+        raise ValueError(f"{name}: from_tokens [num_reqs] int32")
+    c_kv, c_ps = kv.c(), ps.c()
+    _check(getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(from_tokens), int(max_update),
+                                 _ptr(bounds), _stream(stream)), name)
+
+
+def gp_page_bounds(kv: KVLayer, ps: PageState, bounds: torch.Tensor, from_tokens: torch.Tensor | None = None,
+                   max_update: int = 0, stream=None) -> None:
+    """Least and greatest key values of each page, KV head and dim into bounds [pool, Hkv, 2, d]."""
+    _page_bounds("gp_page_bounds", kv, kv.k.dtype, ps, bounds, from_tokens, max_update, stream)
+
+
+def gp_page_bounds_q8(kv: KV8Layer, ps: PageState, bounds: torch.Tensor, from_tokens: torch.Tensor | None = None,
+                      max_update: int = 0, stream=None) -> None:
+    """gp_page_bounds of an 8-bit cache (bounds bfloat16)."""
+    _page_bounds("gp_page_bounds_q8", kv, torch.bfloat16, ps, bounds, from_tokens, max_update, stream)
+
+
+def _lists(selected: torch.Tensor, R: int, Hkv: int) -> int:
+    if selected.dtype != torch.int32 or selected.dim() != 3 or selected.shape[0] != R or selected.shape[1] != Hkv:
+        raise ValueError("selected: int32 [num_reqs, num_kv_heads, budget]")
+    return selected.shape[2]
+
+
+def gp_select_pages(bounds: torch.Tensor, ps: PageState, q_post: torch.Tensor, keep_first: int, keep_last: int,
+                    selected: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """The logical pages each request and KV head is to read, into selected [R, Hkv, budget] int32."""
+    pool, hkv, _, d = bounds.shape
+    R, Hq, _ = q_post.shape
+    budget = _lists(selected, R, hkv)
+    c_ps = ps.c()
+    if pool != c_ps.pool_pages or R != c_ps.num_reqs or q_post.shape[2] != d:
+        raise ValueError("gp_select_pages: bounds [pool_pages, Hkv, 2, d] and q_post [R, Hq, d] of the page state")
+    st = load().gp_select_pages(_ptr(bounds), _dtype_code(bounds), ctypes.byref(c_ps),
+                                _of(q_post, bounds.dtype, "q_post"), Hq, hkv, d, budget, keep_first, keep_last,
+                                _ptr(selected), _ptr(ws), ws.numel(), _stream(stream))
+    _check(st, "gp_select_pages")
+
+
+def _decode_pages(name, kv, dtype, ps, selected, q_post, scale, out, ws, stream):
+    budget = _lists(selected, ps.page_table.shape[0], kv.k.shape[1])
+    c_kv, c_ps = kv.c(), ps.c()
+    _check(getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(selected), budget,
+                                 _of(q_post, dtype, "q_post"), q_post.shape[1], scale, _of(out, dtype, "out"), _ptr(ws),
+                                 ws.numel(), _stream(stream)), name)
+
+
+def gp_decode_attention_pages(kv: KVLayer, ps: PageState, selected: torch.Tensor, q_post: torch.Tensor, scale: float,
+                              out: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """Decode attention over the logical pages selected [R, Hkv, budget]."""
+    _decode_pages("gp_decode_attention_pages", kv, kv.k.dtype, ps, selected, q_post, scale, out, ws, stream)
+
+
+def gp_decode_attention_pages_q8(kv: KV8Layer, ps: PageState, selected: torch.Tensor, q_post: torch.Tensor,
+                                 scale: float, out: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """gp_decode_attention_pages over an 8-bit cache; q_post and out bfloat16."""
+    _decode_pages("gp_decode_attention_pages_q8", kv, torch.bfloat16, ps, selected, q_post, scale, out, ws, stream)

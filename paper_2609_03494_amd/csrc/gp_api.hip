@@ -59,6 +59,20 @@ gp_status_t check_layer(const gp_kv_layer_t *kv) {
     return GP_OK;
 }
 
+bool aligned16(const void *a, const void *b) {
+    return (reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) % 16 == 0;
+}
+
+// An 8-bit layer as the checks and launches take layers (its dtype is that of the
+// queries), after its own checks.
+gp_status_t check_layer8(const gp_kv8_layer_t *kv, gp_kv_layer_t *as) {
+    if (!kv || !kv->k_scale || !kv->v_scale) return GP_ERR_INVALID;
+    *as = {kv->k, kv->v, kv->pool_pages, kv->num_kv_heads, kv->page_size, kv->head_dim, GP_BF16};
+    const gp_status_t st = check_layer(as);
+    if (st != GP_OK) return st;
+    return aligned16(kv->k, kv->v) ? GP_OK : GP_ERR_INVALID;
+}
+
 gp_status_t check_state(const gp_page_state_t *ps, const gp_kv_layer_t *kv) {
     if (!ps || !ps->page_table || !ps->num_pages || !ps->seq_lens) return GP_ERR_INVALID;
     if (ps->num_reqs < 0 || ps->max_pages <= 0) return GP_ERR_INVALID;
@@ -103,6 +117,7 @@ size_t gp_workspace_bytes(int32_t op, int32_t num_reqs, int32_t num_bnd, int32_t
         case GP_OP_DECODE:
             return decode_ws(num_reqs, num_q_heads, num_kv_heads, head_dim, max_pages, decode_waves(elem_bytes(dtype), head_dim)).total;
         case GP_OP_SCORE: return score_ws(num_bnd, num_q_heads, num_kv_heads, max_pages).total;
+        case GP_OP_SELECT: return select_ws(num_reqs, num_kv_heads, max_pages);
         case GP_OP_APPLY:
             return apply_ws(num_bnd, num_kv_heads, head_dim, elem_bytes(dtype), max_pages, n_layers).total;
     }
@@ -153,7 +168,9 @@ struct FoldedSummaries {
 gp_status_t decode_call(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const void *q_post,
                         int32_t num_q_heads, float scale, void *out, void *ws, size_t ws_bytes,
                         const FoldedSummaries *sum, int stages, hipStream_t stream, bool noalloc = false,
-                        const gp_prefix_group_t *groups = nullptr, int32_t num_groups = 0) {
+                        const gp_prefix_group_t *groups = nullptr, int32_t num_groups = 0,
+                        const gp_kv8_layer_t *kv8 = nullptr, bool listed = false, const int32_t *selected = nullptr,
+                        int32_t budget = 0) {
     gp_status_t st = check_layer(kv);
     if (st != GP_OK) return st;
     if ((st = check_state(ps, kv)) != GP_OK) return st;
@@ -164,13 +181,15 @@ gp_status_t decode_call(const gp_kv_layer_t *kv, const gp_page_state_t *ps, cons
         if (!(sum->beta_s >= 0.0f && sum->beta_s <= 1.0f && sum->beta_l >= 0.0f && sum->beta_l <= 1.0f))
             return GP_ERR_INVALID;
     }
+    if (listed && (budget < 1 || budget > kMaxDecodePages)) return GP_ERR_INVALID;
     if (ps->num_reqs == 0) return GP_OK;
-    if (!q_post || !out || (!ws && !noalloc)) return GP_ERR_INVALID;
+    if (!q_post || !out || (!ws && !noalloc) || (listed && !selected)) return GP_ERR_INVALID;
     if (sum && (!sum->q_pre || !sum->slot_ids || !sum->init || !sum->qstate)) return GP_ERR_INVALID;
     if (sum && (!sum->k_new != !sum->v_new)) return GP_ERR_INVALID;
     if (sum && sum->k_new && sum->advance && !sum->positions) return GP_ERR_INVALID;
     if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages) return GP_ERR_UNSUPPORTED;
-    const DecodeWs w = decode_ws(ps->num_reqs, num_q_heads, kv->num_kv_heads, kv->head_dim, ps->max_pages,
+    const DecodeWs w = decode_ws(ps->num_reqs, num_q_heads, kv->num_kv_heads, kv->head_dim,
+                                 listed ? budget : ps->max_pages,
                                  decode_waves(elem_bytes(kv->dtype), kv->head_dim));
     if (noalloc) {
         if (decode_chunked_bytes(ps->num_reqs, num_q_heads, kv->head_dim, ps->max_pages) > kScratchBytes ||
@@ -247,7 +266,18 @@ gp_status_t decode_call(const gp_kv_layer_t *kv, const gp_page_state_t *ps, cons
         if (a.qscale > q) a.qscale = nextafterf(a.qscale, 0.0f);
         a.qscale_lo = std::max((float)(q - a.qscale), FLT_MIN);
     }
-    return from_hip(launch_decode(kv->dtype, kv->head_dim, num_q_heads / kv->num_kv_heads, a, stages, stream));
+    const int G = num_q_heads / kv->num_kv_heads;
+    if (listed) {
+        a.list = selected;
+        a.list_width = budget;
+    }
+    if (kv8) {
+        a.k_scale = kv8->k_scale;
+        a.v_scale = kv8->v_scale;
+        return from_hip(launch_decode_q8(kv->head_dim, G, a, stream));
+    }
+    if (listed) return from_hip(launch_decode_pages(kv->dtype, kv->head_dim, G, a, stream));
+    return from_hip(launch_decode(kv->dtype, kv->head_dim, G, a, stages, stream));
 }
 
 }  // namespace
@@ -294,6 +324,193 @@ gp_status_t gp_decode_step(const gp_kv_layer_t *kv, const gp_page_state_t *ps, c
                               k_new, v_new, positions, advance};
     return decode_call(kv, ps, q_post, num_q_heads, scale, out, ws, ws_bytes, &sum,
                        GP_DECODE_CHUNKS | GP_DECODE_MERGE, stream);
+}
+
+gp_status_t gp_decode_attention_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps, const void *q_post,
+                                   int32_t num_q_heads, float scale, void *out, void *ws, size_t ws_bytes,
+                                   hipStream_t stream) {
+    gp_kv_layer_t as;
+    const gp_status_t st = check_layer8(kv, &as);
+    if (st != GP_OK) return st;
+    return decode_call(&as, ps, q_post, num_q_heads, scale, out, ws, ws_bytes, nullptr,
+                       GP_DECODE_CHUNKS | GP_DECODE_MERGE, stream, false, nullptr, 0, kv);
+}
+
+gp_status_t gp_decode_attention_pages(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const int32_t *selected,
+                                      int32_t budget, const void *q_post, int32_t num_q_heads, float scale,
+                                      void *out, void *ws, size_t ws_bytes, hipStream_t stream) {
+    return decode_call(kv, ps, q_post, num_q_heads, scale, out, ws, ws_bytes, nullptr,
+                       GP_DECODE_CHUNKS | GP_DECODE_MERGE, stream, false, nullptr, 0, nullptr, true, selected, budget);
+}
+
+gp_status_t gp_decode_attention_pages_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps,
+                                         const int32_t *selected, int32_t budget, const void *q_post,
+                                         int32_t num_q_heads, float scale, void *out, void *ws, size_t ws_bytes,
+                                         hipStream_t stream) {
+    gp_kv_layer_t as;
+    const gp_status_t st = check_layer8(kv, &as);
+    if (st != GP_OK) return st;
+    return decode_call(&as, ps, q_post, num_q_heads, scale, out, ws, ws_bytes, nullptr,
+                       GP_DECODE_CHUNKS | GP_DECODE_MERGE, stream, false, nullptr, 0, kv, true, selected, budget);
+}
+
+namespace {
+
+// Elements [p, p + n) and [q, q + m) of `e` bytes share a byte.
+bool overlap(const void *p, int64_t n, const void *q, int64_t m, int e) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a < b + (uintptr_t)m * e && b < a + (uintptr_t)n * e;
+}
+
+gp_status_t rope_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, const gp_page_state_t *ps,
+                      int32_t *positions, const int32_t *tok_start, int32_t num_tokens, const void *q,
+                      int64_t q_stride, void *q_out, const void *k_new, int64_t k_stride, const void *v_new,
+                      int64_t v_stride, int32_t num_q_heads, float rope_theta, int32_t advance,
+                      hipStream_t stream) {
+    gp_status_t st = check_layer(kv);
+    if (st != GP_OK) return st;
+    if ((st = check_state(ps, kv)) != GP_OK) return st;
+    if (!(rope_theta > 0.0f) || !isfinite(rope_theta) || num_tokens < 0) return GP_ERR_INVALID;
+    if (!tok_start && num_tokens != ps->num_reqs) return GP_ERR_INVALID;
+    if (q && !dims_ok(num_q_heads, kv->num_kv_heads, kv->head_dim)) return GP_ERR_UNSUPPORTED;
+    const int64_t row = (int64_t)kv->num_kv_heads * kv->head_dim, qrow = (int64_t)num_q_heads * kv->head_dim;
+    const int e = elem_bytes(kv->dtype);
+    // (no row is 2^30 elements long; products of strides stay within 64 bits)
+    if (k_stride < row || v_stride < row || (q && q_stride < qrow)) return GP_ERR_INVALID;
+    if (std::max({k_stride, v_stride, q ? q_stride : 0}) > int64_t(1) << 30) return GP_ERR_INVALID;
+    if (ps->num_reqs == 0 || num_tokens == 0) return GP_OK;
+    if (!positions || !k_new || !v_new || (q && !q_out)) return GP_ERR_INVALID;
+    if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages || kv->num_kv_heads > 65535) return GP_ERR_UNSUPPORTED;
+    if (q) {
+        const int64_t t = num_tokens - 1;
+        if (overlap(q_out, t * qrow + qrow, q, t * q_stride + qrow, e) && !(q == q_out && q_stride == qrow)) return GP_ERR_INVALID;
+        if (overlap(q_out, t * qrow + qrow, k_new, t * k_stride + row, e) ||
+            overlap(q_out, t * qrow + qrow, v_new, t * v_stride + row, e))
+            return GP_ERR_INVALID;
+    }
+    RopeArgs a = {};
+    a.k = kv->k;
+    a.v = kv->v;
+    a.k_scale = kv8 ? kv8->k_scale : nullptr;
+    a.v_scale = kv8 ? kv8->v_scale : nullptr;
+    a.page_table = ps->page_table;
+    a.num_pages = ps->num_pages;
+    a.seq_lens = ps->seq_lens;
+    a.positions = positions;
+    a.start = tok_start;
+    a.q = q;
+    a.q_out = q ? q_out : nullptr;
+    a.k_new = k_new;
+    a.v_new = v_new;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.R = ps->num_reqs;
+    a.T = num_tokens;
+    a.Hq = q ? num_q_heads : 0;
+    a.Hkv = kv->num_kv_heads;
+    a.max_pages = ps->max_pages;
+    a.pool_pages = kv->pool_pages;
+    // one power, the others by products in extended precision: 64 powers took the
+    // host longer than the launch
+    const long double step = powl((long double)rope_theta, -2.0L / kv->head_dim);
+    long double f = 0.159154943091895335768883763372514362L;              // 1 / (2 pi)
+    for (int i = 0; i < kv->head_dim / 2; ++i, f *= step) a.turns[i] = (double)f;
+    return from_hip(launch_rope(kv8 ? 1 : e, kv->head_dim, a, advance != 0, stream));
+}
+
+gp_status_t bounds_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, const gp_page_state_t *ps,
+                        const int32_t *from_tokens, int32_t max_update, void *bounds, hipStream_t stream) {
+    gp_status_t st = check_layer(kv);
+    if (st != GP_OK) return st;
+    if ((st = check_state(ps, kv)) != GP_OK) return st;
+    if (max_update < 0) return GP_ERR_INVALID;
+    if (ps->num_reqs == 0) return GP_OK;
+    if (!bounds) return GP_ERR_INVALID;
+    if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages || kv->num_kv_heads > 65535) return GP_ERR_UNSUPPORTED;
+    BoundsArgs a = {};
+    a.k = kv->k;
+    a.k_scale = kv8 ? kv8->k_scale : nullptr;
+    a.page_table = ps->page_table;
+    a.num_pages = ps->num_pages;
+    a.seq_lens = ps->seq_lens;
+    a.from = from_tokens;
+    a.bounds = bounds;
+    a.R = ps->num_reqs;
+    a.Hkv = kv->num_kv_heads;
+    a.max_pages = ps->max_pages;
+    a.pool_pages = kv->pool_pages;
+    a.max_update = max_update == 0 || max_update > ps->max_pages ? ps->max_pages : max_update;
+    return from_hip(launch_bounds(kv8 ? 1 : elem_bytes(kv->dtype), kv->head_dim, a, stream));
+}
+
+}  // namespace
+
+gp_status_t gp_append_rope(const gp_kv_layer_t *kv, const gp_page_state_t *ps, int32_t *positions,
+                           const int32_t *tok_start, int32_t num_tokens, const void *q, int64_t q_stride,
+                           void *q_out, const void *k_new, int64_t k_stride, const void *v_new,
+                           int64_t v_stride, int32_t num_q_heads, float rope_theta, int32_t advance,
+                           hipStream_t stream) {
+    return rope_call(kv, nullptr, ps, positions, tok_start, num_tokens, q, q_stride, q_out, k_new, k_stride, v_new,
+                     v_stride, num_q_heads, rope_theta, advance, stream);
+}
+
+gp_status_t gp_append_rope_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps, int32_t *positions,
+                              const int32_t *tok_start, int32_t num_tokens, const void *q, int64_t q_stride,
+                              void *q_out, const void *k_new, int64_t k_stride, const void *v_new,
+                              int64_t v_stride, int32_t num_q_heads, float rope_theta, int32_t advance,
+                              hipStream_t stream) {
+    gp_kv_layer_t as;
+    const gp_status_t st = check_layer8(kv, &as);
+    if (st != GP_OK) return st;
+    return rope_call(&as, kv, ps, positions, tok_start, num_tokens, q, q_stride, q_out, k_new, k_stride, v_new,
+                     v_stride, num_q_heads, rope_theta, advance, stream);
+}
+
+gp_status_t gp_page_bounds(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const int32_t *from_tokens,
+                           int32_t max_update, void *bounds, hipStream_t stream) {
+    return bounds_call(kv, nullptr, ps, from_tokens, max_update, bounds, stream);
+}
+
+gp_status_t gp_page_bounds_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps, const int32_t *from_tokens,
+                              int32_t max_update, void *bounds, hipStream_t stream) {
+    gp_kv_layer_t as;
+    const gp_status_t st = check_layer8(kv, &as);
+    if (st != GP_OK) return st;
+    return bounds_call(&as, kv, ps, from_tokens, max_update, bounds, stream);
+}
+
+gp_status_t gp_select_pages(const void *bounds, gp_dtype_t dtype, const gp_page_state_t *ps, const void *q_post,
+                            int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t budget,
+                            int32_t keep_first, int32_t keep_last, int32_t *selected, void *ws, size_t ws_bytes,
+                            hipStream_t stream) {
+    const gp_status_t st = check_state(ps, nullptr);
+    if (st != GP_OK) return st;
+    if (ps->pool_pages <= 0 || (dtype != GP_F32 && dtype != GP_BF16)) return GP_ERR_INVALID;
+    if (!dims_ok(num_q_heads, num_kv_heads, head_dim)) return GP_ERR_UNSUPPORTED;
+    if (budget < 1 || budget > kMaxDecodePages || keep_first < 0 || keep_last < 0 ||
+        (int64_t)keep_first + keep_last > budget)
+        return GP_ERR_INVALID;
+    if (ps->num_reqs == 0) return GP_OK;
+    if (!bounds || !q_post || !selected || !ws) return GP_ERR_INVALID;
+    if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages || num_kv_heads > 65535) return GP_ERR_UNSUPPORTED;
+    if (ws_bytes < select_ws(ps->num_reqs, num_kv_heads, ps->max_pages)) return GP_ERR_WORKSPACE;
+    SelectArgs a = {};
+    a.bounds = bounds;
+    a.q = q_post;
+    a.page_table = ps->page_table;
+    a.num_pages = ps->num_pages;
+    a.seq_lens = ps->seq_lens;
+    a.scores = static_cast<float *>(ws);
+    a.selected = selected;
+    a.R = ps->num_reqs;
+    a.Hkv = num_kv_heads;
+    a.max_pages = ps->max_pages;
+    a.pool_pages = ps->pool_pages;
+    a.budget = budget;
+    a.keep_first = keep_first;
+    a.keep_last = keep_last;
+    return from_hip(launch_select(dtype, head_dim, num_q_heads / num_kv_heads, a, stream));
 }
 
 gp_status_t gp_boundary_score_stages(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const void *q_pre,

@@ -47,6 +47,14 @@ struct Traits<float> {
     __device__ static inline float load(const float *p) { return *p; }
 };
 
+// One e4m3 value of an 8-bit pool (gp_kv8_layer_t); queries and outputs of such a
+// call are bfloat16.
+struct E4m3 { uint8_t bits; };
+template <typename T>
+struct Elem { using type = T; };
+template <>
+struct Elem<E4m3> { using type = uint16_t; };
+
 constexpr float kNegInf = -__builtin_huge_valf();
 
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
@@ -107,6 +115,14 @@ __device__ inline void lds_read8(uint32_t a0, uint32_t a1, uint32_t a2, uint32_t
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(x0), "=&v"(x1), "=&v"(x2), "=&v"(x3) : "v"(a0), "v"(a1), "v"(a2), "v"(a3) : "memory");
 }
+// four transposed 8-bit reads (ds_read_b64_tr_b8)
+__device__ inline void lds_read_tr8(uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, u32x2_t &x0, u32x2_t &x1,
+                                    u32x2_t &x2, u32x2_t &x3) {
+    __asm__ volatile(
+        "ds_read_b64_tr_b8 %0, %4\n\tds_read_b64_tr_b8 %1, %5\n\tds_read_b64_tr_b8 %2, %6\n\t"
+        "ds_read_b64_tr_b8 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(x0), "=&v"(x1), "=&v"(x2), "=&v"(x3) : "v"(a0), "v"(a1), "v"(a2), "v"(a3) : "memory");
+}
 // four transposed 16-bit reads (ds_read_b64_tr_b16)
 __device__ inline void lds_read_tr(uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, u32x2_t &x0, u32x2_t &x1,
                                    u32x2_t &x2, u32x2_t &x3) {
@@ -148,6 +164,9 @@ __device__ inline float row_ror(float x) {
 __device__ inline int scalar_load(const int32_t *p, int64_t i) {
     return ((const __attribute__((address_space(4))) int32_t *)p)[i];
 }
+__device__ inline float scalar_load(const float *p, int64_t i) {
+    return ((const __attribute__((address_space(4))) float *)p)[i];
+}
 
 // inclusive prefix sum over the wave (DPP row shifts and row broadcasts)
 __device__ inline int wave_scan(int x) {
@@ -172,7 +191,7 @@ struct ReqView {
     bool held, room;
 };
 
-template <bool STEP, bool PREFIX>
+template <bool STEP, bool PREFIX, bool LISTED = false>
 __device__ inline ReqView req_view(const DecodeArgs &a, int r, int m_in, int P_in) {
     ReqView v;
     const int P = min(max(P_in, 0), a.max_pages);
@@ -200,11 +219,12 @@ __device__ inline ReqView req_view(const DecodeArgs &a, int r, int m_in, int P_i
         if (same && pp > 0 && m_in > pp * kPage && P_in > pp && P_in <= a.max_pages && m_in <= P_in * kPage) v.base = pp;
     }
     v.n = cdiv(v.m_attn, kPage) - v.base;
+    if constexpr (LISTED) v.n = min(v.n, a.list_width);
     return v;
 }
-template <bool STEP, bool PREFIX>
+template <bool STEP, bool PREFIX, bool LISTED = false>
 __device__ inline ReqView req_view(const DecodeArgs &a, int r) {
-    return req_view<STEP, PREFIX>(a, r, a.seq_lens[r], a.num_pages[r]);
+    return req_view<STEP, PREFIX, LISTED>(a, r, a.seq_lens[r], a.num_pages[r]);
 }
 
 // The page of K or V that one wave has in flight, by element type: how it is
@@ -274,6 +294,8 @@ struct PageBf16 {
     static constexpr int WAVES = decode_waves(2, D);  // per workgroup: 64 KiB of pages at most
     static constexpr int RPI = 64 / UPR;              // rows per load instruction
     static constexpr int KK = D / 32;                 // product steps over the head dims
+    // the first of the four tokens whose scores a lane of row kg holds
+    __device__ static inline int token0(int kg) { return 4 * kg; }
 
     // byte offset of this lane's unit in load instruction q of keys or values,
     // less 1024 q (the instruction's immediate): row R = q RPI + lane / UPR, unit
@@ -434,6 +456,7 @@ struct Page<float, D, false> {
     static constexpr int RPI = 64 / UPR;
     static constexpr int NJ = D / 16;                 // key units per lane
     static constexpr int DT = D / 16, ACC = DT;
+    __device__ static inline int token0(int kg) { return 4 * kg; }
 
     __device__ static inline uint32_t koff(int lane) {
         return (uint32_t)(lane / UPR * UPR + ((lane % UPR) ^ (lane / UPR))) * 16;
@@ -525,6 +548,7 @@ struct Page<float, D, true> : QuadOut<D> {
     static constexpr int RPI = 64 / UPR;
     static constexpr int NJ = D / 16, NU = D / 64;
     static constexpr int ACC = QuadOut<D>::ACC;
+    __device__ static inline int token0(int kg) { return 4 * kg; }
 
     __device__ static inline uint32_t koff(int lane) {
         const int R = lane / UPR;                     // (% 4, of the first instruction's rows)
@@ -587,6 +611,119 @@ struct Page<float, D, true> : QuadOut<D> {
     }
 };
 
+// e4m3, any number of query heads.  Every e4m3 value is a bfloat16 value, so both
+// products run on v_mfma_f32_16x16x32_bf16 with widened keys and values and lose
+// nothing to the format; the page's two scales meet the sixteen scores and the
+// weights, not the elements.  Row R of the key operand is token 8 (a & 1) + 4 (a >>
+// 1) + R % 4 with a = R / 4, so that lane rows kg and kg ^ 2 hold the scores of eight
+// consecutive tokens, 8 (kg & 1) .. + 7.  P V then takes one product per 16 dims: its
+// contraction of 32 is the sixteen tokens twice, with the bfloat16 high terms of P in
+// rows 0 and 1 and the low ones in rows 2 and 3 (hi + lo carry the float32 weight to
+// about 2^-17), against the same values; two v_permlane32_swap put the terms in place.
+// Half the matrix cycles of the bfloat16 page, whose two terms are two products.
+// A contraction step takes half a 16-byte unit of keys, so a lane's units are whole
+// reads.  Units are swizzled, u ^ R % 8 (d = 64, where two rows share the banks of one:
+// u ^ (R ^ R / 4) % 4), so that the rows of a read fall on distinct banks.
+template <int D>
+struct Page<E4m3, D, false> {
+    static constexpr int UPR = D / 16;                // 16-byte units per row
+    static constexpr int BYTES = kPage * D;
+    static constexpr int LOADS = BYTES / 1024;        // 2 or 1
+    static constexpr int KK = D / 32, NJ = D / 64;
+    static constexpr int DT = D / 16, ACC = DT;
+    __device__ static inline int swizzle(int R) { return D == 128 ? R & 7 : (R ^ R >> 2) & 3; }
+    // rows of load instruction q: q 64 / UPR + lane / UPR (d = 128: the same swizzle in both)
+    __device__ static inline uint32_t koff(int lane) {
+        const int R = lane / UPR;
+        return (uint32_t)(R * UPR + ((lane % UPR) ^ swizzle(R))) * 16;
+    }
+    static constexpr uint32_t kflip(int) { return 0; }
+    __device__ static inline uint32_t voff(int lane) { return koff(lane); }
+    static constexpr uint32_t vflip(int) { return 0; }
+    __device__ static inline int token0(int kg) { return 8 * (kg & 1) + 4 * (kg >> 1); }
+    __device__ static inline uint32_t kread(int n, int kg) {
+        const int R = token0(n / 4) + n % 4;
+        return (R * UPR + (kg ^ swizzle(R))) * 16;
+    }
+    // transposed reads, to be xored with 16 t (tile t): lane j of a group of 16 names
+    // eight bytes (half j % 2) of row 8 (kg & 1) + j / 2; lane n receives dim 16 t + n
+    // of the eight rows
+    __device__ static inline uint32_t vread(int n, int kg) {
+        const int R = 8 * (kg & 1) + n / 2;
+        return (R * UPR + swizzle(R)) * 16 + (n & 1) * 8;
+    }
+    // Q of the lane's head: operand 2 j + s is half s of key unit kg + 4 j
+    static constexpr int QREGS = KK;
+    __device__ static inline int qdim(int j, int n, int kg) { return 16 * (kg + 4 * (j / 2)) + 8 * (j % 2); }
+    __device__ static inline bf16x8_t widen(const u32x2_t &x) {
+        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+        bf16x8_t y;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const bf16x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], 1.0f, false);
+            const bf16x2_t hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], 1.0f, true);
+            y[4 * i] = lo[0];
+            y[4 * i + 1] = lo[1];
+            y[4 * i + 2] = hi[0];
+            y[4 * i + 3] = hi[1];
+        }
+        return y;
+    }
+    __device__ static inline f32x4_t scores(uint32_t ka, const u32x4_t (&q)[QREGS]) {
+        u32x4_t kx[2];
+        lds_read16(ka, ka ^ (NJ - 1) * 64, kx[0], kx[1]);     // (d = 64: one unit, read twice)
+        f32x4_t st = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(u32x2_t{kx[j][2 * s], kx[j][2 * s + 1]}),
+                                                             __builtin_bit_cast(bf16x8_t, q[2 * j + s]), st, 0, 0, 0);
+        return st;
+    }
+    static constexpr int VREGS = DT;
+    typedef u32x2_t v_t;
+    __device__ static inline void read_values(uint32_t va, int, v_t (&vx)[VREGS]) {
+#pragma unroll
+        for (int t = 0; t < DT; t += 4)
+            lds_read_tr8(va ^ 16 * t, va ^ 16 * (t + 1), va ^ 16 * (t + 2), va ^ 16 * (t + 3), vx[t], vx[t + 1], vx[t + 2], vx[t + 3]);
+    }
+    // p: the weights times the values' scale.  A slot past the last token may hold a
+    // NaN: it reads as zero.
+    __device__ static inline void weigh(uint32_t, v_t (&vx)[VREGS], bool, const float (&p)[4], int ntok, f32x4_t (&ot)[DT],
+                                        int kg) {
+        bf16x4s_t phi, plo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const __bf16 hb = (__bf16)p[e];               // round to nearest even
+            phi[e] = __builtin_bit_cast(short, hb);
+            plo[e] = __builtin_bit_cast(short, (__bf16)(p[e] - (float)hb));   // p - hi is exact in float32
+        }
+        const u32x2_t hi = __builtin_bit_cast(u32x2_t, phi), lo = __builtin_bit_cast(u32x2_t, plo);
+        // lower half of the wave: hi of tokens 8 (kg & 1) + 0 .. 3, + 4 .. 7; upper half: lo
+        const auto w0 = __builtin_amdgcn_permlane32_swap(hi[0], lo[0], false, false);
+        const auto w1 = __builtin_amdgcn_permlane32_swap(hi[1], lo[1], false, false);
+        const bf16x8_t b = __builtin_bit_cast(bf16x8_t, u32x4_t{w0[0], w1[0], w0[1], w1[1]});
+        u32x2_t keep = {~0u, ~0u};
+        if (ntok < kPage) {                               // wave-uniform
+            const int k = ntok - 8 * (kg & 1);            // rows of the lane that hold tokens
+            keep[0] = k >= 4 ? ~0u : k <= 0 ? 0u : (1u << 8 * k) - 1;
+            keep[1] = k >= 8 ? ~0u : k <= 4 ? 0u : (1u << 8 * (k - 4)) - 1;
+        }
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+            ot[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(u32x2_t{vx[t][0] & keep[0], vx[t][1] & keep[1]}), b, ot[t],
+                                                            0, 0, 0);
+    }
+    static constexpr int GROUPS = DT;
+    __device__ static inline int head(int n) { return n; }
+    __device__ static inline int group_dim(int j, int n, int kg) { return 16 * j + 4 * kg; }
+    __device__ static inline void gather(const f32x4_t (&ot)[ACC], f32x4_t (&o)[GROUPS]) {
+#pragma unroll
+        for (int j = 0; j < GROUPS; ++j) o[j] = ot[j];
+    }
+};
+
 template <typename T, int D>
 constexpr int waves_of() { return decode_waves(sizeof(T), D); }
 template <typename T, int D>
@@ -595,7 +732,7 @@ constexpr int page_bytes_of() { return kPage * D * (int)sizeof(T); }
 // heads: the two-term P of four or eight heads costs the matrix cores less.  float32:
 // as far as one product's columns go.
 template <typename T>
-constexpr bool quad_heads(int G) { return sizeof(T) == 2 ? G <= 2 : G <= 4; }
+constexpr bool quad_heads(int G) { return sizeof(T) == 1 ? false : sizeof(T) == 2 ? G <= 2 : G <= 4; }
 
 // Calls whose values go to registers as soon as they are there (8 or 16 of them), so
 // that the next page is requested whole before this one's weights are formed: a
@@ -603,7 +740,7 @@ constexpr bool quad_heads(int G) { return sizeof(T) == 2 ? G <= 2 : G <= 4; }
 // equal runs of d = 128, which it would take past the 96 registers that leave other
 // kernels' waves room beside two workgroups (107 with one query head, for 1 %).
 template <typename T>
-constexpr bool early_values(int D, int OWN) { return sizeof(T) == 2 && (D == 64 || OWN > 0); }
+constexpr bool early_values(int D, int OWN) { return sizeof(T) == 1 || (sizeof(T) == 2 && (D == 64 || OWN > 0)); }
 
 // One page slice into LDS: instruction q takes at(q) (less 1024 (q % 4)) to
 // stage + 1024 q (the immediate offset moves source and destination).
@@ -624,7 +761,7 @@ __device__ inline void load_page(At at, char *stage, bool aligned, int lane) {
     for (int q = 0; q < LOADS; q += 4) {
         lds_void_t *const to = (lds_void_t *)(stage + q * 1024);
         __builtin_amdgcn_global_load_lds((global_cvoid_t *)at(q), to, 16, 0, kCpolNT);
-        __builtin_amdgcn_global_load_lds((global_cvoid_t *)at(q + 1), to, 16, 1024, kCpolNT);
+        if constexpr (LOADS > 1) __builtin_amdgcn_global_load_lds((global_cvoid_t *)at(q + 1), to, 16, 1024, kCpolNT);
         if constexpr (LOADS > 2) {
             __builtin_amdgcn_global_load_lds((global_cvoid_t *)at(q + 2), to, 16, 2048, kCpolNT);
             __builtin_amdgcn_global_load_lds((global_cvoid_t *)at(q + 3), to, 16, 3072, kCpolNT);
@@ -655,13 +792,15 @@ __device__ inline void store_out(float *p, const f32x4_t &o, float l) {
 template <typename T, int D, int OWN>
 constexpr int decode_occupancy() {
     if (waves_of<T, D>() < 8) return 2;
-    if (OWN == 0) return 4;
-    return OWN < waves_of<T, D>() ? 6 : sizeof(T) == 2 ? 5 : 4;
+    if (OWN == 0 || (sizeof(T) == 1 && D == 128)) return 4;
+    return OWN < waves_of<T, D>() ? 6 : sizeof(T) <= 2 ? 5 : 4;
 }
 
 // MODE 0: decode attention; 1: gp_decode_step with the step's new token (the
 // summary update is in the merge pass); 2: the private tails of
-// gp_decode_attention_shared.
+// gp_decode_attention_shared; 3: attention over listed pages
+// (gp_decode_attention_pages), the list of a request and KV head in the place of the
+// request's pages.
 //
 // Per wave one LDS page of keys and one of values, filled by direct-to-LDS
 // loads, each instruction one contiguous 1 KiB of the head's slice; the keys
@@ -677,7 +816,8 @@ __global__ __launch_bounds__((64 * (OWN ? OWN : waves_of<T, D>())))
     __attribute__((amdgpu_waves_per_eu(decode_occupancy<T, D, OWN>()))) void
 decode_kernel(DecodeArgs a) {
     static_assert(!OWN || MODE != 2, "a shared-prefix call is always merged");
-    constexpr bool STEP = MODE == 1, PREFIX = MODE == 2;
+    constexpr bool STEP = MODE == 1, PREFIX = MODE == 2, LISTED = MODE == 3, SCALED = sizeof(T) == 1;
+    using E = typename Elem<T>::type;                 // of queries and outputs
     using Pg = Page<T, D, quad_heads<T>(G)>;
     constexpr int NW = OWN ? OWN : waves_of<T, D>();
     constexpr int NT = 64 * NW;
@@ -706,7 +846,7 @@ decode_kernel(DecodeArgs a) {
         r = wg;
         m_in = scalar_load(a.seq_lens, r);
         P_in = scalar_load(a.num_pages, r);
-        const ReqView v = req_view<STEP, PREFIX>(a, r, m_in, P_in);
+        const ReqView v = req_view<STEP, PREFIX, LISTED>(a, r, m_in, P_in);
         const int run = cdiv(v.n, NW);
         f0 = min(wave * run, v.n);
         f1 = v.held ? f0 : min(f0 + run, v.n);
@@ -717,7 +857,7 @@ decode_kernel(DecodeArgs a) {
             a.lens[2 * R + r] = a.lens[3 * R + r] = a.lens[4 * R + r] = 0;
         }
         if (v.n == 0 && !v.held) {                    // no tokens
-            T *o = reinterpret_cast<T *>(a.out) + ((size_t)r * Hq + (size_t)h * G) * D;
+            E *o = reinterpret_cast<E *>(a.out) + ((size_t)r * Hq + (size_t)h * G) * D;
             for (int i = 4 * tid; i < G * D; i += 4 * NT) store_out(o + i, f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0.0f);
         }
     } else {
@@ -728,7 +868,7 @@ decode_kernel(DecodeArgs a) {
         int any_long = 0;                                 // (sign) a request of the last block has too many pages for a workgroup
         auto scan_block = [&](int base, int acc) {        // inclusive sums of the block's requests; its end
             const int r = min(base + tid, R - 1), sl = a.seq_lens[r], np = a.num_pages[r];
-            const int x = base + tid < R ? req_view<STEP, PREFIX>(a, r, sl, np).n : 0;
+            const int x = base + tid < R ? req_view<STEP, PREFIX, LISTED>(a, r, sl, np).n : 0;
             const int incl = wave_scan(x), mark = __ballot(x > kDecodeOwnRun * NW) ? 1 << 31 : 0;
             if (base > 0) __syncthreads();                // (the previous block has been read)
             if (lane == 63) s_sum[wave] = incl | mark;
@@ -765,7 +905,7 @@ decode_kernel(DecodeArgs a) {
             int acc = 0;
             for (int base = 0; base < R; base += 64) {
                 const int r = base + lane;
-                const ReqView v = req_view<STEP, PREFIX>(a, min(r, R - 1));
+                const ReqView v = req_view<STEP, PREFIX, LISTED>(a, min(r, R - 1));
                 const int np = r < R ? v.n : 0, incl = wave_scan(np), a0 = acc + incl - np;
                 acc += __builtin_amdgcn_readlane(incl, 63);
                 if (base / 64 % NW != wave || r >= R) continue;
@@ -781,7 +921,7 @@ decode_kernel(DecodeArgs a) {
                     if (!(PREFIX && v.base > 0)) a.lens[4 * R + r] = 0;   // (else: the wave that begins the request)
                 }
                 if (np == 0 && !v.held) {
-                    T *o = reinterpret_cast<T *>(a.out) + ((size_t)r * Hq + (size_t)h * G) * D;
+                    E *o = reinterpret_cast<E *>(a.out) + ((size_t)r * Hq + (size_t)h * G) * D;
                     for (int i = 0; i < G * D; i += 4) store_out(o + i, f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}, 0.0f);
                 }
             }
@@ -794,7 +934,7 @@ decode_kernel(DecodeArgs a) {
             r = wg;
             m_in = uni(s_len[r]);
             P_in = uni(s_np[r]);
-            const int n_ = uni(req_view<STEP, PREFIX>(a, r, m_in, P_in).n), run = cdiv(n_, NW);
+            const int n_ = uni(req_view<STEP, PREFIX, LISTED>(a, r, m_in, P_in).n), run = cdiv(n_, NW);
             a0 = uni(s_incl[r]) - n_;
             f0 = a0 + min(wave * run, n_);
             f1 = a0 + min((wave + 1) * run, n_);
@@ -811,7 +951,7 @@ decode_kernel(DecodeArgs a) {
                     r = base + l;
                     m_in = uni(s_len[l]);
                     P_in = uni(s_np[l]);
-                    a0 = uni(s_incl[l]) - uni(req_view<STEP, PREFIX>(a, r, m_in, P_in).n);
+                    a0 = uni(s_incl[l]) - uni(req_view<STEP, PREFIX, LISTED>(a, r, m_in, P_in).n);
                 }
             }
         }
@@ -845,7 +985,18 @@ decode_kernel(DecodeArgs a) {
     bool whole = false;                               // the part begins with the request's first page
     const int32_t *row = nullptr;
     int idn = -1;                                     // page id at the cursor, requested ahead
-    auto request_id = [&]() { idn = scalar_load(row, min(max(base + p, 0), a.max_pages - 1)); };
+    // LISTED: the request's list, its entry at the cursor (a logical page), and the one after it
+    const int32_t *list = nullptr;
+    int lgn = 0, lg1 = 0;
+    auto request_id = [&]() {
+        if constexpr (LISTED) {
+            lgn = lg1;
+            idn = scalar_load(row, min(max(lgn, 0), a.max_pages - 1));
+            lg1 = scalar_load(list, min(p + 1, a.list_width - 1));
+        } else {
+            idn = scalar_load(row, min(max(base + p, 0), a.max_pages - 1));
+        }
+    };
     // enters request r (uniform) at its covered page `from`; the step's new token
     // goes into the cache here, before the page that takes it is requested
     auto enter = [&](const ReqView &v, int from) {
@@ -856,6 +1007,10 @@ decode_kernel(DecodeArgs a) {
         pend = min(nseg, f1 - a0);
         whole = from == 0;
         row = a.page_table + (size_t)r * a.max_pages;
+        if constexpr (LISTED) {
+            list = a.list + ((size_t)r * Hkv + h) * a.list_width;
+            lg1 = scalar_load(list, from);
+        }
         if constexpr (PREFIX) {
             if (base > 0 && whole) {
                 const int32_t *lead = nullptr;
@@ -897,7 +1052,7 @@ decode_kernel(DecodeArgs a) {
                 P_in = scalar_load(a.num_pages, r);
             }
             known = false;
-            const ReqView v = req_view<STEP, PREFIX>(a, r, m_in, P_in);
+            const ReqView v = req_view<STEP, PREFIX, LISTED>(a, r, m_in, P_in);
             const int n_ = uni(v.n);
             if (!v.held && n_ > from) {
                 enter(v, from);
@@ -915,7 +1070,7 @@ decode_kernel(DecodeArgs a) {
     // addresses kept across the loop would cost registers)
     const uint32_t q_at = (uint32_t)(min(hn, G - 1) * D + Pg::qdim(0, n, kg));
     auto load_q = [&](int rr) {
-        const T *src = reinterpret_cast<const T *>(a.q) + ((size_t)rr * Hq + (size_t)h * G) * D;
+        const E *src = reinterpret_cast<const E *>(a.q) + ((size_t)rr * Hq + (size_t)h * G) * D;
 #pragma unroll
         for (int j = 0; j < Pg::QREGS; ++j) {
             const u32x4_t x = load16(src + (q_at + (uint32_t)(Pg::qdim(j, 0, 0))));
@@ -941,7 +1096,7 @@ decode_kernel(DecodeArgs a) {
         __asm__ volatile("" : "+v"(nn), "+v"(dd));
         if (hn < G) {
             if (direct) {
-                T *o = reinterpret_cast<T *>(a.out) + ((size_t)rr * Hq + (size_t)h * G) * D;
+                E *o = reinterpret_cast<E *>(a.out) + ((size_t)rr * Hq + (size_t)h * G) * D;
                 const uint32_t at = nn * D + dd;
 #pragma unroll
                 for (int j = 0; j < Pg::GROUPS; ++j)
@@ -968,7 +1123,8 @@ decode_kernel(DecodeArgs a) {
     bool open_first = false, open_last = false, open_tail = false;
     // A page on its way: where it is and whose it is.
     struct Ahead {
-        int phys, r, p, base, m_attn;
+        int phys, r, p, base, m_attn;                 // (LISTED: p the logical page)
+        float ks, vs;                                 // SCALED: of its keys and values
         bool valid, last, first_of, ends;             // last page of the wave's part; part begins / ends the request
     };
     // the page at the cursor (r, p), then the cursor to the next page
@@ -986,6 +1142,16 @@ decode_kernel(DecodeArgs a) {
         x.ends = pend == nseg;
         if (more) {
             x.phys = idn >= 0 && idn < a.pool_pages ? idn : -1;
+            if constexpr (LISTED) {
+                const bool in = lgn >= 0 && lgn < cdiv(m_attn, kPage);
+                x.p = in ? lgn : 0;
+                if (!in) x.phys = -1;
+            }
+            if constexpr (SCALED) {
+                const int64_t at = (int64_t)max(x.phys, 0) * Hkv + h;
+                x.ks = scalar_load(a.k_scale, at);
+                x.vs = scalar_load(a.v_scale, at);
+            }
             if (!x.last) {
                 ++p;
                 request_id();
@@ -1002,7 +1168,7 @@ decode_kernel(DecodeArgs a) {
         load_q(r);
         clear();
         // cur is computed, nxt takes its place in LDS (the first round only requests)
-        Ahead cur = {-1, 0, 0, 0, 0, false, false, false, false};
+        Ahead cur = {-1, 0, 0, 0, 0, 1.0f, 1.0f, false, false, false, false};
         while (true) {
             const Ahead nxt = take();
             const bool has = cur.phys >= 0, has1 = nxt.phys >= 0;
@@ -1028,11 +1194,14 @@ decode_kernel(DecodeArgs a) {
             if (has1) request_keys(nxt.phys);
             if (EARLY && has1) request_values(nxt.phys);
             if (has) {
-                // online softmax of the lane's head over tokens 4 kg + e
+                // online softmax of the lane's head over tokens t0 + e
+                const int t0 = Pg::token0(kg);
+                float qscale = a.qscale;
+                if constexpr (SCALED) qscale *= cur.ks;
                 float sc[4], ml = kNegInf;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    sc[e] = 4 * kg + e < ntok ? sx[e] * a.qscale : kNegInf;
+                    sc[e] = t0 + e < ntok ? sx[e] * qscale : kNegInf;
                     ml = fmaxf(ml, sc[e]);
                 }
                 const float mn = fmaxf(mrun, cross_max(ml));
@@ -1053,7 +1222,7 @@ decode_kernel(DecodeArgs a) {
                     // float32: the distance to the maximum rounded once, not the score, the
                     // scale and the distance each (a third of the output's error at d = 64)
                     if constexpr (sizeof(T) == 4)
-                        sc[e] = 4 * kg + e < ntok ? fmaf(sx[e], a.qscale_lo, fmaf(sx[e], a.qscale, -top)) : kNegInf;
+                        sc[e] = t0 + e < ntok ? fmaf(sx[e], a.qscale_lo, fmaf(sx[e], a.qscale, -top)) : kNegInf;
                     else
                         sc[e] -= top;
                     lowest = fminf(lowest, sc[e]);
@@ -1062,7 +1231,7 @@ decode_kernel(DecodeArgs a) {
                     lowest = 0.0f;
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (4 * kg + e < ntok) lowest = fminf(lowest, sc[e]);
+                        if (t0 + e < ntok) lowest = fminf(lowest, sc[e]);
                 }
                 if (__any(lowest < -126.0f)) {
 #pragma unroll
@@ -1072,6 +1241,10 @@ decode_kernel(DecodeArgs a) {
                     for (int e = 0; e < 4; ++e) sc[e] = __builtin_amdgcn_exp2f(sc[e]);
                 }
                 lrun += (sc[0] + sc[1]) + (sc[2] + sc[3]);
+                if constexpr (SCALED) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[e] *= cur.vs;
+                }
                 if constexpr (!EARLY) {
                     // the values: requested after them are the next page's keys
                     __builtin_amdgcn_sched_barrier(0);
@@ -1125,7 +1298,7 @@ decode_kernel(DecodeArgs a) {
     // requests, of two or three waves, the loop is the shorter one.
     auto fold = [&](int w0, int w1, int rr, bool more_, bool direct) {
         float *pt = part_of(rr);
-        T *out = reinterpret_cast<T *>(a.out) + ((size_t)rr * Hq + (size_t)h * G) * D;
+        E *out = reinterpret_cast<E *>(a.out) + ((size_t)rr * Hq + (size_t)h * G) * D;
         constexpr int EPT = (G * D + NT - 1) / NT;
         float M[EPT], Ls[EPT], Os[EPT];
 #pragma unroll
@@ -1173,7 +1346,7 @@ decode_kernel(DecodeArgs a) {
             const int i = tid + e * NT, g = i / D, dd = i % D;
             if (i >= G * D) continue;
             if (direct) {
-                Traits<T>::store(out + i, divided(Os[e], Ls[e]));
+                Traits<E>::store(out + i, divided(Os[e], Ls[e]));
             } else {
                 pt[(size_t)g * (D + 2) + dd] = Os[e];
                 if (dd == 0) store8(pt + (size_t)g * (D + 2) + D, M[e], Ls[e]);
@@ -1625,7 +1798,45 @@ hipError_t launch_g(int G, const DecodeArgs &a, int stages, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Attention over an 8-bit pool, over listed pages, or both: no token, no prefix.
+template <typename T, int D, int MODE>
+hipError_t launch_read(int G, const DecodeArgs &a, hipStream_t s) {
+    using E = typename Elem<T>::type;
+    const dim3 grid(a.Hkv, a.W), mgrid(a.Hkv, a.R);
+    constexpr int NW = waves_of<T, D>(), NT = 64 * NW;
+    constexpr int NN = page_bytes_of<T, D>() <= 2048 ? 4 : NW;
+    const int columns = MODE == 3 ? a.list_width : a.max_pages;
+    const bool own = decode_own(columns, a.R, a.Hkv, page_bytes_of<T, D>(), NW, quad_heads<T>(G));
+    const bool narrow = own && decode_own_narrow(a.R, a.Hkv), wide = (int64_t)a.Hkv * a.R < kWideMerge;
+    switch (G) {
+#define GP_CASE(GG)                                                                \
+    case GG:                                                                       \
+        if (own && NN < NW && narrow) decode_kernel<T, D, GG, MODE, NN><<<mgrid, 64 * NN, 0, s>>>(a); \
+        else if (own) decode_kernel<T, D, GG, MODE, NW><<<mgrid, NT, 0, s>>>(a);    \
+        else {                                                                     \
+            decode_kernel<T, D, GG, MODE, 0><<<grid, NT, 0, s>>>(a);                \
+            if (wide) merge_kernel<E, D, GG, 1024><<<mgrid, 1024, 0, s>>>(a);       \
+            else merge_kernel<E, D, GG, 256><<<mgrid, 256, 0, s>>>(a);              \
+        }                                                                          \
+        break;
+        GP_CASE(1) GP_CASE(2) GP_CASE(4) GP_CASE(8)
+#undef GP_CASE
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
 }  // namespace
+
+hipError_t launch_decode_q8(int D, int G, const DecodeArgs &a, hipStream_t s) {
+    if (a.list) return D == 128 ? launch_read<E4m3, 128, 3>(G, a, s) : launch_read<E4m3, 64, 3>(G, a, s);
+    return D == 128 ? launch_read<E4m3, 128, 0>(G, a, s) : launch_read<E4m3, 64, 0>(G, a, s);
+}
+
+hipError_t launch_decode_pages(gp_dtype_t dt, int D, int G, const DecodeArgs &a, hipStream_t s) {
+    if (dt == GP_BF16) return D == 128 ? launch_read<uint16_t, 128, 3>(G, a, s) : launch_read<uint16_t, 64, 3>(G, a, s);
+    return D == 128 ? launch_read<float, 128, 3>(G, a, s) : launch_read<float, 64, 3>(G, a, s);
+}
 
 hipError_t launch_decode(gp_dtype_t dt, int D, int G, const DecodeArgs &a, int stages, hipStream_t s) {
     if (dt == GP_BF16)

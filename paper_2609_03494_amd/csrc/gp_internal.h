@@ -140,6 +140,11 @@ __host__ __device__ inline DecodeWs decode_ws(int R, int Hq, int Hkv, int D, int
     return w;
 }
 
+// Scores of a page selection, one per KV head and table column.
+__host__ __device__ inline size_t select_ws(int R, int Hkv, int max_pages) {
+    return align_up((size_t)R * Hkv * max_pages * sizeof(float));
+}
+
 struct ScoreWs {
     size_t cand, expz, part, weights, total;
     int cmax, nch;
@@ -245,6 +250,9 @@ struct DecodeArgs {
     int R, Hkv, max_pages, pool_pages, W, W1, min_run, slots, pslots;   // W1: workgroups per KV head that fit at once
     float qscale;      // scale * log2(e); float32 caches: rounded down, and the rest of it
     float qscale_lo;   // (> 0, so that an infinite score times it keeps its sign)
+    const float *k_scale, *v_scale;   // 8-bit pools: [pool_pages][Hkv]
+    const int32_t *list;              // listed pages: [R][Hkv][list_width] logical page indices (nullptr: all pages)
+    int list_width;
 };
 
 struct SummaryArgs {
@@ -266,6 +274,36 @@ struct AppendArgs {
     float *qstate;
     int R, Hq, Hkv, M, max_pages, pool_pages, n_layers;
     double beta_s, beta_l;
+};
+
+// gp_append_rope: n_r new tokens per request, rotated on their way.
+struct RopeArgs {
+    void *k, *v;
+    float *k_scale, *v_scale;         // 8-bit pools
+    const int32_t *page_table, *num_pages;
+    int32_t *seq_lens, *positions;
+    const int32_t *start;             // [R + 1] first token of each request; nullptr: one token each
+    const void *q, *k_new, *v_new;
+    void *q_out;                      // nullptr: no queries
+    int64_t q_stride, k_stride, v_stride;   // elements from token to token
+    int R, T, Hq, Hkv, max_pages, pool_pages;
+    double turns[64];                 // theta^(-2 i / d) / (2 pi): turns per position of rotary pair i
+};
+
+struct BoundsArgs {
+    const void *k;
+    const float *k_scale;             // 8-bit pools
+    const int32_t *page_table, *num_pages, *seq_lens, *from;
+    void *bounds;
+    int R, Hkv, max_pages, pool_pages, max_update;
+};
+
+struct SelectArgs {
+    const void *bounds, *q;
+    const int32_t *page_table, *num_pages, *seq_lens;
+    float *scores;                    // [R][Hkv][max_pages]
+    int32_t *selected;                // [R][Hkv][budget]
+    int R, Hkv, max_pages, pool_pages, budget, keep_first, keep_last;
 };
 
 struct ScoreArgs {
@@ -317,6 +355,12 @@ struct LayerPtrs {
 hipError_t launch_summaries(gp_dtype_t dt, const SummaryArgs &a, hipStream_t s);
 hipError_t launch_append(gp_dtype_t dt, int D, const AppendArgs &a, hipStream_t s);
 hipError_t launch_decode(gp_dtype_t dt, int D, int G, const DecodeArgs &a, int stages, hipStream_t s);
+hipError_t launch_decode_q8(int D, int G, const DecodeArgs &a, hipStream_t s);
+hipError_t launch_decode_pages(gp_dtype_t dt, int D, int G, const DecodeArgs &a, hipStream_t s);
+// cache: element bytes of the pool (1: e4m3 codes, 2, 4)
+hipError_t launch_rope(int cache, int D, const RopeArgs &a, bool advance, hipStream_t s);
+hipError_t launch_bounds(int cache, int D, const BoundsArgs &a, hipStream_t s);
+hipError_t launch_select(gp_dtype_t dt, int D, int G, const SelectArgs &a, hipStream_t s);
 hipError_t launch_score(gp_dtype_t dt, int D, int G, const ScoreArgs &a, int stages, hipStream_t s);
 // Stages of the boundary apply (selection, decision, compaction).
 constexpr int kStageSelect = 1, kStageDecide = 2, kStageCompact = 4;
