@@ -255,7 +255,11 @@ gp_status_t decode_call(const gp_kv_layer_t *kv, const gp_page_state_t *ps, cons
     a.max_pages = ps->max_pages;
     a.pool_pages = kv->pool_pages;
     a.W = w.W;
-    a.W1 = std::max(1, std::min(w.W, kDecodeResident / kv->num_kv_heads));
+    if (kv8)                                          // the split counts pairs of pages
+        a.W = std::min(w.W, decode_ws(ps->num_reqs, num_q_heads, kv->num_kv_heads, kv->head_dim,
+                                      cdiv(listed ? budget : ps->max_pages, 2),
+                                      decode_waves(elem_bytes(kv->dtype), kv->head_dim)).W);
+    a.W1 = std::max(1, std::min(a.W, kDecodeResident / kv->num_kv_heads));
     a.min_run = kDecodeMinRun;
     a.slots = w.slots;
     a.pslots = w.pslots;

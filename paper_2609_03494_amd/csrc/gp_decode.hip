@@ -26,6 +26,8 @@
 // 2 * d * sizeof(elem) (K and V), plus the page-table entries, q and out.  A
 // copy of the kernel's loads without arithmetic (equal runs, 4 KiB head slices
 // of randomly placed pages) reads 6.5-6.9 TB/s; a plain streaming read 7.04.
+#include <limits.h>
+
 #include "gp_internal.h"
 
 namespace gp {
@@ -115,6 +117,22 @@ __device__ inline void lds_read8(uint32_t a0, uint32_t a1, uint32_t a2, uint32_t
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(x0), "=&v"(x1), "=&v"(x2), "=&v"(x3) : "v"(a0), "v"(a1), "v"(a2), "v"(a3) : "memory");
 }
+// 16 bytes at a0 and a1 (x) and at OFF past them (y); 8 bytes at az (z) and 256 past it (w)
+template <int OFF>
+__device__ inline void lds_read16_pair(uint32_t a0, uint32_t a1, uint32_t az, u32x4_t (&x)[2], u32x4_t (&y)[2], u32x2_t &z, u32x2_t &w) {
+    __asm__ volatile(
+        "ds_read_b128 %0, %6\n\tds_read_b128 %1, %7\n\tds_read_b128 %2, %6 offset:%9\n\t"
+        "ds_read_b128 %3, %7 offset:%9\n\tds_read_b64 %4, %8\n\tds_read_b64 %5, %8 offset:256\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(y[0]), "=&v"(y[1]), "=&v"(z), "=&v"(w)
+        : "v"(a0), "v"(a1), "v"(az), "i"(OFF) : "memory");
+}
+template <int OFF>
+__device__ inline void lds_read16_pair(uint32_t a0, uint32_t az, u32x4_t (&x)[1], u32x4_t (&y)[1], u32x2_t &z, u32x2_t &w) {
+    __asm__ volatile(
+        "ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:%6\n\tds_read_b64 %2, %5\n\tds_read_b64 %3, %5 offset:256\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(y[0]), "=&v"(z), "=&v"(w) : "v"(a0), "v"(az), "i"(OFF) : "memory");
+}
 // four transposed 8-bit reads (ds_read_b64_tr_b8)
 __device__ inline void lds_read_tr8(uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, u32x2_t &x0, u32x2_t &x1,
                                     u32x2_t &x2, u32x2_t &x3) {
@@ -191,7 +209,9 @@ struct ReqView {
     bool held, room;
 };
 
-template <bool STEP, bool PREFIX, bool LISTED = false>
+// LISTED: the request's list of pages in the place of its pages.  PAIR: n counts
+// pairs of pages.
+template <bool STEP, bool PREFIX, bool LISTED = false, bool PAIR = false>
 __device__ inline ReqView req_view(const DecodeArgs &a, int r, int m_in, int P_in) {
     ReqView v;
     const int P = min(max(P_in, 0), a.max_pages);
@@ -220,11 +240,12 @@ __device__ inline ReqView req_view(const DecodeArgs &a, int r, int m_in, int P_i
     }
     v.n = cdiv(v.m_attn, kPage) - v.base;
     if constexpr (LISTED) v.n = min(v.n, a.list_width);
+    if constexpr (PAIR) v.n = cdiv(v.n, 2);
     return v;
 }
-template <bool STEP, bool PREFIX, bool LISTED = false>
+template <bool STEP, bool PREFIX, bool LISTED = false, bool PAIR = false>
 __device__ inline ReqView req_view(const DecodeArgs &a, int r) {
-    return req_view<STEP, PREFIX, LISTED>(a, r, a.seq_lens[r], a.num_pages[r]);
+    return req_view<STEP, PREFIX, LISTED, PAIR>(a, r, a.seq_lens[r], a.num_pages[r]);
 }
 
 // The page of K or V that one wave has in flight, by element type: how it is
@@ -294,8 +315,6 @@ struct PageBf16 {
     static constexpr int WAVES = decode_waves(2, D);  // per workgroup: 64 KiB of pages at most
     static constexpr int RPI = 64 / UPR;              // rows per load instruction
     static constexpr int KK = D / 32;                 // product steps over the head dims
-    // the first of the four tokens whose scores a lane of row kg holds
-    __device__ static inline int token0(int kg) { return 4 * kg; }
 
     // byte offset of this lane's unit in load instruction q of keys or values,
     // less 1024 q (the instruction's immediate): row R = q RPI + lane / UPR, unit
@@ -456,7 +475,6 @@ struct Page<float, D, false> {
     static constexpr int RPI = 64 / UPR;
     static constexpr int NJ = D / 16;                 // key units per lane
     static constexpr int DT = D / 16, ACC = DT;
-    __device__ static inline int token0(int kg) { return 4 * kg; }
 
     __device__ static inline uint32_t koff(int lane) {
         return (uint32_t)(lane / UPR * UPR + ((lane % UPR) ^ (lane / UPR))) * 16;
@@ -548,7 +566,6 @@ struct Page<float, D, true> : QuadOut<D> {
     static constexpr int RPI = 64 / UPR;
     static constexpr int NJ = D / 16, NU = D / 64;
     static constexpr int ACC = QuadOut<D>::ACC;
-    __device__ static inline int token0(int kg) { return 4 * kg; }
 
     __device__ static inline uint32_t koff(int lane) {
         const int R = lane / UPR;                     // (% 4, of the first instruction's rows)
@@ -611,24 +628,29 @@ struct Page<float, D, true> : QuadOut<D> {
     }
 };
 
-// e4m3, any number of query heads.  Every e4m3 value is a bfloat16 value, so both
-// products run on v_mfma_f32_16x16x32_bf16 with widened keys and values and lose
-// nothing to the format; the page's two scales meet the sixteen scores and the
-// weights, not the elements.  Row R of the key operand is token 8 (a & 1) + 4 (a >>
-// 1) + R % 4 with a = R / 4, so that lane rows kg and kg ^ 2 hold the scores of eight
-// consecutive tokens, 8 (kg & 1) .. + 7.  P V then takes one product per 16 dims: its
-// contraction of 32 is the sixteen tokens twice, with the bfloat16 high terms of P in
-// rows 0 and 1 and the low ones in rows 2 and 3 (hi + lo carry the float32 weight to
-// about 2^-17), against the same values; two v_permlane32_swap put the terms in place.
-// Half the matrix cycles of the bfloat16 page, whose two terms are two products.
-// A contraction step takes half a 16-byte unit of keys, so a lane's units are whole
-// reads.  Units are swizzled, u ^ R % 8 (d = 64, where two rows share the banks of one:
-// u ^ (R ^ R / 4) % 4), so that the rows of a read fall on distinct banks.
+// e4m3, any number of query heads: pages in pairs (the second half of a pair may
+// have no tokens).  Every e4m3 value is a bfloat16 value, so both products run on
+// v_mfma_f32_16x16x32_bf16 with widened keys and values and lose nothing to the
+// format; a page's two scales meet its scores and weights, not its elements.
+// Row R of a page's key operand is token 8 (a & 1) + 4 (a >> 1) + R % 4 with a = R /
+// 4, so that lane rows kg and kg ^ 2 hold the scores of eight consecutive tokens, 8
+// (kg & 1) .. + 7.  A product of P.V takes the 32 tokens of the pair: rows 0 and 1 of
+// the lanes bring the first page's values, rows 2 and 3 the second's, and
+// v_permlane32_swap puts the weights of the two pages, as they leave the scores, into
+// that order.  P in two bfloat16 terms (its float32 value to about 2^-17), a product
+// each.  One page at a time (the sixteen tokens twice, with both terms in one
+// product) every value was widened in two lanes and a page cost 190 vector
+// instructions; now 90, and the softmax is formed once per pair.
+// A contraction step of the scores takes half a 16-byte unit of keys, so a lane's
+// units are whole reads.  Units are swizzled, u ^ R % 8 (d = 64, where two rows share
+// the banks of one: u ^ (R ^ R / 4) % 4), so that the rows of a read fall on distinct
+// banks.
 template <int D>
 struct Page<E4m3, D, false> {
     static constexpr int UPR = D / 16;                // 16-byte units per row
-    static constexpr int BYTES = kPage * D;
-    static constexpr int LOADS = BYTES / 1024;        // 2 or 1
+    static constexpr int HALF = kPage * D;            // keys or values of one page and head
+    static constexpr int BYTES = 2 * HALF;            // ... of the pair
+    static constexpr int LOADS = HALF / 1024;         // per page: 2 or 1
     static constexpr int KK = D / 32, NJ = D / 64;
     static constexpr int DT = D / 16, ACC = DT;
     __device__ static inline int swizzle(int R) { return D == 128 ? R & 7 : (R ^ R >> 2) & 3; }
@@ -640,17 +662,18 @@ struct Page<E4m3, D, false> {
     static constexpr uint32_t kflip(int) { return 0; }
     __device__ static inline uint32_t voff(int lane) { return koff(lane); }
     static constexpr uint32_t vflip(int) { return 0; }
+    // the first of the four tokens of a page whose scores a lane of row kg holds
     __device__ static inline int token0(int kg) { return 8 * (kg & 1) + 4 * (kg >> 1); }
     __device__ static inline uint32_t kread(int n, int kg) {
         const int R = token0(n / 4) + n % 4;
         return (R * UPR + (kg ^ swizzle(R))) * 16;
     }
     // transposed reads, to be xored with 16 t (tile t): lane j of a group of 16 names
-    // eight bytes (half j % 2) of row 8 (kg & 1) + j / 2; lane n receives dim 16 t + n
-    // of the eight rows
+    // eight bytes (half j % 2) of row 8 (kg & 1) + j / 2 of page kg >> 1; lane n
+    // receives dim 16 t + n of the eight rows
     __device__ static inline uint32_t vread(int n, int kg) {
         const int R = 8 * (kg & 1) + n / 2;
-        return (R * UPR + swizzle(R)) * 16 + (n & 1) * 8;
+        return (kg >> 1) * HALF + (R * UPR + swizzle(R)) * 16 + (n & 1) * 8;
     }
     // Q of the lane's head: operand 2 j + s is half s of key unit kg + 4 j
     static constexpr int QREGS = KK;
@@ -669,17 +692,22 @@ struct Page<E4m3, D, false> {
         }
         return y;
     }
-    __device__ static inline f32x4_t scores(uint32_t ka, const u32x4_t (&q)[QREGS]) {
-        u32x4_t kx[2];
-        lds_read16(ka, ka ^ (NJ - 1) * 64, kx[0], kx[1]);     // (d = 64: one unit, read twice)
-        f32x4_t st = {0.0f, 0.0f, 0.0f, 0.0f};
+    typedef u32x4_t k_t;
+    // the keys of both pages, and the scales of their keys and values
+    __device__ static inline void read_keys(uint32_t ka, uint32_t sa, k_t (&x)[2][NJ], u32x2_t &ks, u32x2_t &vs) {
+        if constexpr (NJ == 2) lds_read16_pair<HALF>(ka, ka ^ 64, sa, x[0], x[1], ks, vs);
+        else lds_read16_pair<HALF>(ka, sa, x[0], x[1], ks, vs);
+    }
+    __device__ static inline void scores(const k_t (&x)[2][NJ], const u32x4_t (&q)[QREGS], f32x4_t (&st)[2]) {
+        st[0] = st[1] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
             for (int s = 0; s < 2; ++s)
-                st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(u32x2_t{kx[j][2 * s], kx[j][2 * s + 1]}),
-                                                             __builtin_bit_cast(bf16x8_t, q[2 * j + s]), st, 0, 0, 0);
-        return st;
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    st[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(u32x2_t{x[c][j][2 * s], x[c][j][2 * s + 1]}),
+                                                                    __builtin_bit_cast(bf16x8_t, q[2 * j + s]), st[c], 0, 0, 0);
     }
     static constexpr int VREGS = DT;
     typedef u32x2_t v_t;
@@ -688,32 +716,48 @@ struct Page<E4m3, D, false> {
         for (int t = 0; t < DT; t += 4)
             lds_read_tr8(va ^ 16 * t, va ^ 16 * (t + 1), va ^ 16 * (t + 2), va ^ 16 * (t + 3), vx[t], vx[t + 1], vx[t + 2], vx[t + 3]);
     }
-    // p: the weights times the values' scale.  A slot past the last token may hold a
-    // NaN: it reads as zero.
-    __device__ static inline void weigh(uint32_t, v_t (&vx)[VREGS], bool, const float (&p)[4], int ntok, f32x4_t (&ot)[DT],
-                                        int kg) {
-        bf16x4s_t phi, plo;
+    __device__ static inline uint32_t pack(float x, float y) {
+        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)x, (__bf16)y});
+    }
+    // p: the weights of the two pages times their values' scales; n: their tokens.  A
+    // slot past the last token may hold a NaN: it reads as zero.
+    __device__ static inline void weigh(v_t (&vx)[VREGS], const float (&p)[2][4], int n0, int n1, f32x4_t (&ot)[DT], int kg) {
+        u32x2_t hi[2], lo[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const __bf16 hb = (__bf16)p[e];               // round to nearest even
-            phi[e] = __builtin_bit_cast(short, hb);
-            plo[e] = __builtin_bit_cast(short, (__bf16)(p[e] - (float)hb));   // p - hi is exact in float32
-        }
-        const u32x2_t hi = __builtin_bit_cast(u32x2_t, phi), lo = __builtin_bit_cast(u32x2_t, plo);
-        // lower half of the wave: hi of tokens 8 (kg & 1) + 0 .. 3, + 4 .. 7; upper half: lo
-        const auto w0 = __builtin_amdgcn_permlane32_swap(hi[0], lo[0], false, false);
-        const auto w1 = __builtin_amdgcn_permlane32_swap(hi[1], lo[1], false, false);
-        const bf16x8_t b = __builtin_bit_cast(bf16x8_t, u32x4_t{w0[0], w1[0], w0[1], w1[1]});
-        u32x2_t keep = {~0u, ~0u};
-        if (ntok < kPage) {                               // wave-uniform
-            const int k = ntok - 8 * (kg & 1);            // rows of the lane that hold tokens
-            keep[0] = k >= 4 ? ~0u : k <= 0 ? 0u : (1u << 8 * k) - 1;
-            keep[1] = k >= 8 ? ~0u : k <= 4 ? 0u : (1u << 8 * (k - 4)) - 1;
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float x = p[c][2 * i], y = p[c][2 * i + 1];
+                const uint32_t u = pack(x, y);            // round to nearest even
+                hi[c][i] = u;
+                lo[c][i] = pack(x - bf16_lo(u), y - bf16_hi(u));     // p - hi is exact in float32
+            }
+        // lower half of the wave: tokens 8 (kg & 1) + 0 .. 3, + 4 .. 7 of the first page; upper half: of the second
+        auto both = [](const u32x2_t &x, const u32x2_t &y) {
+            const auto w0 = __builtin_amdgcn_permlane32_swap(x[0], y[0], false, false);
+            const auto w1 = __builtin_amdgcn_permlane32_swap(x[1], y[1], false, false);
+            return __builtin_bit_cast(bf16x8_t, u32x4_t{w0[0], w1[0], w0[1], w1[1]});
+        };
+        const bf16x8_t bhi = both(hi[0], hi[1]), blo = both(lo[0], lo[1]);
+        if (n0 + n1 < 2 * kPage) {                        // wave-uniform
+            const int k = (kg >> 1 ? n1 : n0) - 8 * (kg & 1);     // rows of the lane that hold tokens
+            const uint32_t k0 = k >= 4 ? ~0u : k <= 0 ? 0u : (1u << 8 * k) - 1;
+            const uint32_t k1 = k >= 8 ? ~0u : k <= 4 ? 0u : (1u << 8 * (k - 4)) - 1;
+#pragma unroll
+            for (int t = 0; t < DT; ++t) vx[t] = u32x2_t{vx[t][0] & k0, vx[t][1] & k1};
         }
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
-            ot[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(u32x2_t{vx[t][0] & keep[0], vx[t][1] & keep[1]}), b, ot[t],
-                                                            0, 0, 0);
+        for (int t0 = 0; t0 < DT; t0 += 4) {              // (the two products of a tile apart: the second waits for the first)
+            bf16x8_t v[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                v[t] = widen(vx[t0 + t]);
+                ot[t0 + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], bhi, ot[t0 + t], 0, 0, 0);
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t) ot[t0 + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], blo, ot[t0 + t], 0, 0, 0);
+        }
     }
     static constexpr int GROUPS = DT;
     __device__ static inline int head(int n) { return n; }
@@ -727,7 +771,7 @@ struct Page<E4m3, D, false> {
 template <typename T, int D>
 constexpr int waves_of() { return decode_waves(sizeof(T), D); }
 template <typename T, int D>
-constexpr int page_bytes_of() { return kPage * D * (int)sizeof(T); }
+constexpr int page_bytes_of() { return kPage * D * (sizeof(T) == 1 ? 2 : (int)sizeof(T)); }     // (of a pair of 8-bit pages)
 // The query heads per KV head of which P.V runs in QUAD products.  bfloat16, more
 // heads: the two-term P of four or eight heads costs the matrix cores less.  float32:
 // as far as one product's columns go.
@@ -740,7 +784,7 @@ constexpr bool quad_heads(int G) { return sizeof(T) == 1 ? false : sizeof(T) == 
 // equal runs of d = 128, which it would take past the 96 registers that leave other
 // kernels' waves room beside two workgroups (107 with one query head, for 1 %).
 template <typename T>
-constexpr bool early_values(int D, int OWN) { return sizeof(T) == 1 || (sizeof(T) == 2 && (D == 64 || OWN > 0)); }
+constexpr bool early_values(int D, int OWN) { return sizeof(T) == 2 && (D == 64 || OWN > 0); }
 
 // One page slice into LDS: instruction q takes at(q) (less 1024 (q % 4)) to
 // stage + 1024 q (the immediate offset moves source and destination).
@@ -793,7 +837,8 @@ template <typename T, int D, int OWN>
 constexpr int decode_occupancy() {
     if (waves_of<T, D>() < 8) return 2;
     if (OWN == 0 || (sizeof(T) == 1 && D == 128)) return 4;
-    return OWN < waves_of<T, D>() ? 6 : sizeof(T) <= 2 ? 5 : 4;
+    if (sizeof(T) == 1) return 5;
+    return OWN < waves_of<T, D>() ? 6 : sizeof(T) == 2 ? 5 : 4;
 }
 
 // MODE 0: decode attention; 1: gp_decode_step with the step's new token (the
@@ -816,7 +861,8 @@ __global__ __launch_bounds__((64 * (OWN ? OWN : waves_of<T, D>())))
     __attribute__((amdgpu_waves_per_eu(decode_occupancy<T, D, OWN>()))) void
 decode_kernel(DecodeArgs a) {
     static_assert(!OWN || MODE != 2, "a shared-prefix call is always merged");
-    constexpr bool STEP = MODE == 1, PREFIX = MODE == 2, LISTED = MODE == 3, SCALED = sizeof(T) == 1;
+    constexpr bool STEP = MODE == 1, PREFIX = MODE == 2, LISTED = MODE == 3;
+    constexpr bool PAIR = sizeof(T) == 1;             // 8-bit pages go in pairs: "page" below is a pair, places in the list count pairs
     using E = typename Elem<T>::type;                 // of queries and outputs
     using Pg = Page<T, D, quad_heads<T>(G)>;
     constexpr int NW = OWN ? OWN : waves_of<T, D>();
@@ -828,6 +874,9 @@ decode_kernel(DecodeArgs a) {
     constexpr int STAGE = 2 * Pg::BYTES;
     static_assert(G * D * 4 <= STAGE, "merge buffer");
     __shared__ __attribute__((aligned(1024))) char s_wave[NW][STAGE];
+    // PAIR: scales of 64 pages' keys and values; the next 64 page ids (LISTED: list entries)
+    __shared__ __attribute__((aligned(16))) float s_scale[PAIR ? NW : 1][2][64];
+    __shared__ int s_ids[PAIR ? NW : 1][64];
     __shared__ float s_ml[NW][G][2];                  // (max, sum) of each wave's open part
     __shared__ int s_open[NW][3];                     // its request; flags first page 1, last page 2, tail 4; request written
 
@@ -846,7 +895,7 @@ decode_kernel(DecodeArgs a) {
         r = wg;
         m_in = scalar_load(a.seq_lens, r);
         P_in = scalar_load(a.num_pages, r);
-        const ReqView v = req_view<STEP, PREFIX, LISTED>(a, r, m_in, P_in);
+        const ReqView v = req_view<STEP, PREFIX, LISTED, PAIR>(a, r, m_in, P_in);
         const int run = cdiv(v.n, NW);
         f0 = min(wave * run, v.n);
         f1 = v.held ? f0 : min(f0 + run, v.n);
@@ -868,7 +917,7 @@ decode_kernel(DecodeArgs a) {
         int any_long = 0;                                 // (sign) a request of the last block has too many pages for a workgroup
         auto scan_block = [&](int base, int acc) {        // inclusive sums of the block's requests; its end
             const int r = min(base + tid, R - 1), sl = a.seq_lens[r], np = a.num_pages[r];
-            const int x = base + tid < R ? req_view<STEP, PREFIX, LISTED>(a, r, sl, np).n : 0;
+            const int x = base + tid < R ? req_view<STEP, PREFIX, LISTED, PAIR>(a, r, sl, np).n : 0;
             const int incl = wave_scan(x), mark = __ballot(x > kDecodeOwnRun * NW) ? 1 << 31 : 0;
             if (base > 0) __syncthreads();                // (the previous block has been read)
             if (lane == 63) s_sum[wave] = incl | mark;
@@ -890,7 +939,7 @@ decode_kernel(DecodeArgs a) {
         };
         int U = 0;
         for (int base = 0; base < R; base += NT) U = uni(scan_block(base, U));
-        const int L = max(max(a.min_run, cdiv(U, a.W * NW)), min(kDecodeShortRun, cdiv(U, a.W1 * NW)));
+        const int L = max(max(a.min_run, cdiv(U, a.W * NW)), min(PAIR ? kDecodeShortPairs : kDecodeShortRun, cdiv(U, a.W1 * NW)));
         // Short requests in a wide table, few enough for a workgroup each, take one each,
         // as OWN: nothing to merge, and the merge launch finds that at once.  Up to
         // kDecodeOwnRun pages per wave; us a call at 512 table columns, equal runs and so:
@@ -905,7 +954,7 @@ decode_kernel(DecodeArgs a) {
             int acc = 0;
             for (int base = 0; base < R; base += 64) {
                 const int r = base + lane;
-                const ReqView v = req_view<STEP, PREFIX, LISTED>(a, min(r, R - 1));
+                const ReqView v = req_view<STEP, PREFIX, LISTED, PAIR>(a, min(r, R - 1));
                 const int np = r < R ? v.n : 0, incl = wave_scan(np), a0 = acc + incl - np;
                 acc += __builtin_amdgcn_readlane(incl, 63);
                 if (base / 64 % NW != wave || r >= R) continue;
@@ -934,7 +983,7 @@ decode_kernel(DecodeArgs a) {
             r = wg;
             m_in = uni(s_len[r]);
             P_in = uni(s_np[r]);
-            const int n_ = uni(req_view<STEP, PREFIX, LISTED>(a, r, m_in, P_in).n), run = cdiv(n_, NW);
+            const int n_ = uni(req_view<STEP, PREFIX, LISTED, PAIR>(a, r, m_in, P_in).n), run = cdiv(n_, NW);
             a0 = uni(s_incl[r]) - n_;
             f0 = a0 + min(wave * run, n_);
             f1 = a0 + min((wave + 1) * run, n_);
@@ -951,33 +1000,34 @@ decode_kernel(DecodeArgs a) {
                     r = base + l;
                     m_in = uni(s_len[l]);
                     P_in = uni(s_np[l]);
-                    a0 = uni(s_incl[l]) - uni(req_view<STEP, PREFIX, LISTED>(a, r, m_in, P_in).n);
+                    a0 = uni(s_incl[l]) - uni(req_view<STEP, PREFIX, LISTED, PAIR>(a, r, m_in, P_in).n);
                 }
             }
         }
     }
 
     char *const mine = s_wave[wave];
-    const size_t page_bytes = (size_t)Hkv * Pg::BYTES;
-    const char *const kpool = reinterpret_cast<const char *>(a.k) + (size_t)h * Pg::BYTES;
-    const char *const vpool = reinterpret_cast<const char *>(a.v) + (size_t)h * Pg::BYTES;
+    constexpr int SLICE = PAIR ? Pg::BYTES / 2 : Pg::BYTES;
+    const size_t page_bytes = (size_t)Hkv * SLICE;
+    const char *const kpool = reinterpret_cast<const char *>(a.k) + (size_t)h * SLICE;
+    const char *const vpool = reinterpret_cast<const char *>(a.v) + (size_t)h * SLICE;
     // this lane's offsets in a page slice and in its LDS copy.  (Made opaque on
     // each page: hoisted out of the loop, their variants for every instruction
     // would take two dozen registers and push the kernel past the 96 that leave
     // room for other kernels' waves beside two of its workgroups.)
     uint32_t ko = Pg::koff(lane), vo = Pg::voff(lane);
     uint32_t kr = lds_addr(mine) + Pg::kread(n, kg), vr = lds_addr(mine) + Pg::BYTES + Pg::vread(n, kg);
-    auto request_keys = [&](int phys) {
+    auto request_keys = [&](int phys, int to = 0) {
         const char *src = kpool + (size_t)phys * page_bytes;
         __asm__ volatile("" : "+v"(ko));
-        load_page<LOADS, sizeof(T) == 4>([&](int q) { return src + (size_t)((ko ^ Pg::kflip(q)) + (q - q % 4) * 1024u); }, mine,
-                                        a.aligned, lane);
+        load_page<LOADS, sizeof(T) == 4>([&](int q) { return src + (size_t)((ko ^ Pg::kflip(q)) + (q - q % 4) * 1024u); },
+                                        mine + to, a.aligned, lane);
     };
-    auto request_values = [&](int phys) {
+    auto request_values = [&](int phys, int to = 0) {
         const char *src = vpool + (size_t)phys * page_bytes;
         __asm__ volatile("" : "+v"(vo));
         load_page<LOADS, sizeof(T) == 4>([&](int q) { return src + (size_t)((vo ^ Pg::vflip(q)) + (q - q % 4) * 1024u); },
-                                        mine + Pg::BYTES, a.aligned, lane);
+                                        mine + Pg::BYTES + to, a.aligned, lane);
     };
 
     // ---- one request's part of the run: pages [p, pend) of its covered pages
@@ -989,12 +1039,46 @@ decode_kernel(DecodeArgs a) {
     const int32_t *list = nullptr;
     int lgn = 0, lg1 = 0;
     auto request_id = [&]() {
-        if constexpr (LISTED) {
+        if constexpr (LISTED && !PAIR) {
             lgn = lg1;
             idn = scalar_load(row, min(max(lgn, 0), a.max_pages - 1));
             lg1 = scalar_load(list, min(p + 1, a.list_width - 1));
-        } else {
+        } else if constexpr (!PAIR) {
             idn = scalar_load(row, min(max(base + p, 0), a.max_pages - 1));
+        }
+    };
+    // PAIR: of the 64 pages (LISTED: list entries) from id0 on, a lane each, the page id
+    // and the tokens it has.  An entry that is no page of the request's has none, and the
+    // id of its pair's other page or, should both be none, page 0: every pair has the same
+    // loads.  The scales of the 64 pages' keys and values go to LDS.  (Ids and scales by scalar
+    // loads, as below, held up the waits for the LDS reads, which count them too: 1.5 us a
+    // pair in an idle chip, 1.3 so.)  The ids are requested a pair ahead, into LDS.
+    int idv = 0, cntv = 0, id0 = 0;
+    auto prefetch_ids = [&]() {
+        if constexpr (PAIR) {
+            const int at = 2 * p + lane;
+            const int32_t *from = LISTED ? list + min(at, a.list_width - 1) : row + min(at, a.max_pages - 1);
+            __builtin_amdgcn_global_load_lds((global_cvoid_t *)from, (lds_void_t *)s_ids[wave], 4, 0, 0);
+        }
+    };
+    auto fetch_ids = [&]() {
+        if constexpr (PAIR) {
+            id0 = 2 * p;
+            const int at = id0 + lane, resident = cdiv(m_attn, kPage);
+            int lg = at, id;
+            const uint32_t from = lds_addr(&s_ids[wave][lane]);
+            __asm__ volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(id) : "v"(from) : "memory");
+            if constexpr (LISTED) {
+                lg = id;
+                id = row[min(max(lg, 0), a.max_pages - 1)];
+            }
+            const bool ok = at < (LISTED ? min(resident, a.list_width) : resident) && lg >= 0 && lg < resident && id >= 0 && id < a.pool_pages;
+            cntv = ok ? min(kPage, m_attn - lg * kPage) : 0;
+            const int mine = ok ? id : -1, other = __builtin_amdgcn_update_dpp(0, mine, 0xb1, 0xf, 0xf, false);    // lane ^ 1
+            idv = ok ? id : max(other, 0);
+            const size_t sc = (size_t)idv * Hkv + h;
+            __builtin_amdgcn_global_load_lds((global_cvoid_t *)(a.k_scale + sc), (lds_void_t *)s_scale[wave][0], 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_cvoid_t *)(a.v_scale + sc), (lds_void_t *)s_scale[wave][1], 4, 0, 0);
         }
     };
     // enters request r (uniform) at its covered page `from`; the step's new token
@@ -1009,8 +1093,9 @@ decode_kernel(DecodeArgs a) {
         row = a.page_table + (size_t)r * a.max_pages;
         if constexpr (LISTED) {
             list = a.list + ((size_t)r * Hkv + h) * a.list_width;
-            lg1 = scalar_load(list, from);
+            if constexpr (!PAIR) lg1 = scalar_load(list, from);
         }
+        if constexpr (PAIR) id0 = INT_MIN / 2;        // (its pages are not fetched yet)
         if constexpr (PREFIX) {
             if (base > 0 && whole) {
                 const int32_t *lead = nullptr;
@@ -1052,7 +1137,7 @@ decode_kernel(DecodeArgs a) {
                 P_in = scalar_load(a.num_pages, r);
             }
             known = false;
-            const ReqView v = req_view<STEP, PREFIX, LISTED>(a, r, m_in, P_in);
+            const ReqView v = req_view<STEP, PREFIX, LISTED, PAIR>(a, r, m_in, P_in);
             const int n_ = uni(v.n);
             if (!v.held && n_ > from) {
                 enter(v, from);
@@ -1124,7 +1209,7 @@ decode_kernel(DecodeArgs a) {
     // A page on its way: where it is and whose it is.
     struct Ahead {
         int phys, r, p, base, m_attn;                 // (LISTED: p the logical page)
-        float ks, vs;                                 // SCALED: of its keys and values
+        int phys2, n0, n1, l;                         // PAIR: the second page, the tokens of each, their place among the 64
         bool valid, last, first_of, ends;             // last page of the wave's part; part begins / ends the request
     };
     // the page at the cursor (r, p), then the cursor to the next page
@@ -1147,11 +1232,6 @@ decode_kernel(DecodeArgs a) {
                 x.p = in ? lgn : 0;
                 if (!in) x.phys = -1;
             }
-            if constexpr (SCALED) {
-                const int64_t at = (int64_t)max(x.phys, 0) * Hkv + h;
-                x.ks = scalar_load(a.k_scale, at);
-                x.vs = scalar_load(a.v_scale, at);
-            }
             if (!x.last) {
                 ++p;
                 request_id();
@@ -1163,12 +1243,160 @@ decode_kernel(DecodeArgs a) {
         }
         return x;
     };
+    // PAIR: the scores sx of both pages, and their values vx, into the request's sums
+    auto add_pair = [&](const Ahead &x, f32x4_t (&sx)[2], typename Pg::v_t (&vx)[Pg::VREGS], const u32x2_t &ks, const u32x2_t &vs) {
+        if constexpr (PAIR) {
+            // online softmax of the lane's head over tokens token0 + e of both pages.  The
+            // scales are positive, so the greatest product is the greatest score's; the
+            // distance to the maximum is rounded once.
+            const float qs[2] = {a.qscale * __uint_as_float(ks[0]), a.qscale * __uint_as_float(ks[1])};
+            if (x.n0 + x.n1 < 2 * kPage) {
+                const int t0 = Pg::token0(kg);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sx[0][e] = t0 + e < x.n0 ? sx[0][e] : kNegInf;
+                    sx[1][e] = t0 + e < x.n1 ? sx[1][e] : kNegInf;
+                }
+            }
+            const float ml = fmaxf(fmaxf(fmaxf(sx[0][0], sx[0][1]), fmaxf(sx[0][2], sx[0][3])) * qs[0],
+                                   fmaxf(fmaxf(sx[1][0], sx[1][1]), fmaxf(sx[1][2], sx[1][3])) * qs[1]);
+            const float mn = fmaxf(mrun, cross_max(ml));
+            const float top = mn == kNegInf ? 0.0f : mn;
+            if (__any(mn != mrun)) {                  // skip while no head's max has moved
+                const float alpha = exp2f(mrun - top);
+                lrun *= alpha;
+#pragma unroll
+                for (int t = 0; t < ACC; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) ot[t][e] *= alpha;
+                mrun = mn;
+            }
+            float sc[2][4];
+            // weights; the instruction by itself flushes those below 2^-126
+            float lowest = 0.0f;
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    sc[c][e] = fmaf(sx[c][e], qs[c], -top);
+                    lowest = fminf(lowest, sc[c][e]);
+                }
+            if (__any(lowest < -126.0f)) {            // (and pairs that are not full)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[c][e] = exp2f(sc[c][e]);
+            } else {
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[c][e] = __builtin_amdgcn_exp2f(sc[c][e]);
+            }
+            lrun += ((sc[0][0] + sc[0][1]) + (sc[0][2] + sc[0][3])) + ((sc[1][0] + sc[1][1]) + (sc[1][2] + sc[1][3]));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sc[0][e] *= __uint_as_float(vs[0]);
+                sc[1][e] *= __uint_as_float(vs[1]);
+            }
+            Pg::weigh(vx, sc, x.n0, x.n1, ot, kg);
+        }
+    };
+    auto take_pair = [&]() {
+        Ahead x = {};
+        x.valid = more;
+        x.r = r;
+        x.last = p + 1 >= pend;
+        x.first_of = whole;
+        x.ends = pend == nseg;
+        if constexpr (PAIR) {
+            if (more) {
+                if (2 * p - id0 >= 64) fetch_ids();
+                x.l = 2 * p - id0;
+                x.phys = __builtin_amdgcn_readlane(idv, x.l);
+                x.phys2 = __builtin_amdgcn_readlane(idv, x.l + 1);
+                x.n0 = __builtin_amdgcn_readlane(cntv, x.l);
+                x.n1 = __builtin_amdgcn_readlane(cntv, x.l + 1);
+                if (!x.last) {
+                    ++p;
+                } else {
+                    a0 += nseg;
+                    ++r;
+                    more = seek(0, false);
+                }
+                if (more && 2 * p - id0 >= 64) prefetch_ids();
+            }
+        }
+        return x;
+    };
     if (f0 < f1) more = seek(f0 - a0, true);
-    if (more) {
+    if constexpr (PAIR) {
+        if (more) {
+            prefetch_ids();
+            load_q(r);
+            clear();
+            const uint32_t sr = lds_addr(s_scale[wave]);
+            __builtin_amdgcn_s_waitcnt(kWaitVm0);
+            Ahead cur = take_pair();
+            request_keys(cur.phys);
+            request_keys(cur.phys2, Pg::HALF);
+            request_values(cur.phys);
+            request_values(cur.phys2, Pg::HALF);
+            // Keys and values go to registers as soon as they are there, so that the next
+            // pair's are on their way while this one's are computed.
+            while (true) {
+                typename Pg::k_t kx[2][Pg::NJ];
+                typename Pg::v_t vx[Pg::VREGS];
+                f32x4_t sx[2];
+                u32x2_t ks, vs;
+                // the keys (and, before them, the scales): requested after them are the values
+                __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_waitcnt(wait_vm(2 * LOADS));
+                __builtin_amdgcn_sched_barrier(0);
+                __asm__ volatile("" : "+v"(kr));
+                Pg::read_keys(kr, sr + 4 * cur.l, kx, ks, vs);
+                __builtin_amdgcn_sched_barrier(0);
+                const Ahead nxt = take_pair();
+                if (nxt.valid) {                      // wave-uniform
+                    request_keys(nxt.phys);
+                    request_keys(nxt.phys2, Pg::HALF);
+                }
+                Pg::scores(kx, q, sx);
+                // the values: requested after them are the next pair's keys
+                __builtin_amdgcn_sched_barrier(0);
+                if (nxt.valid) __builtin_amdgcn_s_waitcnt(wait_vm(2 * LOADS));
+                else __builtin_amdgcn_s_waitcnt(kWaitVm0);
+                __builtin_amdgcn_sched_barrier(0);
+                __asm__ volatile("" : "+v"(vr));
+                Pg::read_values(vr, kg, vx);
+                __builtin_amdgcn_sched_barrier(0);
+                if (nxt.valid) {
+                    request_values(nxt.phys);
+                    request_values(nxt.phys2, Pg::HALF);
+                }
+                if (cur.n0 + cur.n1 > 0) add_pair(cur, sx, vx, ks, vs);
+                __builtin_amdgcn_sched_barrier(0);
+                if (cur.last) {
+                    const bool all = cur.first_of && cur.ends;        // the wave has the whole request
+                    if (!nxt.valid) {
+                        open_first = cur.first_of;
+                        open_last = cur.ends;
+                        if (all) finish(cur.r, true);
+                        else open_r = cur.r;
+                        break;
+                    }
+                    finish(cur.r, all);
+                    if (!cur.first_of) wrote_r = cur.r;
+                    load_q(nxt.r);
+                    clear();
+                }
+                cur = nxt;
+            }
+        }
+    } else if (more) {
         load_q(r);
         clear();
         // cur is computed, nxt takes its place in LDS (the first round only requests)
-        Ahead cur = {-1, 0, 0, 0, 0, 1.0f, 1.0f, false, false, false, false};
+        Ahead cur = {-1, 0, 0, 0, 0, -1, 0, 0, 0, false, false, false, false};
         while (true) {
             const Ahead nxt = take();
             const bool has = cur.phys >= 0, has1 = nxt.phys >= 0;
@@ -1194,14 +1422,11 @@ decode_kernel(DecodeArgs a) {
             if (has1) request_keys(nxt.phys);
             if (EARLY && has1) request_values(nxt.phys);
             if (has) {
-                // online softmax of the lane's head over tokens t0 + e
-                const int t0 = Pg::token0(kg);
-                float qscale = a.qscale;
-                if constexpr (SCALED) qscale *= cur.ks;
+                // online softmax of the lane's head over tokens 4 kg + e
                 float sc[4], ml = kNegInf;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    sc[e] = t0 + e < ntok ? sx[e] * qscale : kNegInf;
+                    sc[e] = 4 * kg + e < ntok ? sx[e] * a.qscale : kNegInf;
                     ml = fmaxf(ml, sc[e]);
                 }
                 const float mn = fmaxf(mrun, cross_max(ml));
@@ -1222,7 +1447,7 @@ decode_kernel(DecodeArgs a) {
                     // float32: the distance to the maximum rounded once, not the score, the
                     // scale and the distance each (a third of the output's error at d = 64)
                     if constexpr (sizeof(T) == 4)
-                        sc[e] = t0 + e < ntok ? fmaf(sx[e], a.qscale_lo, fmaf(sx[e], a.qscale, -top)) : kNegInf;
+                        sc[e] = 4 * kg + e < ntok ? fmaf(sx[e], a.qscale_lo, fmaf(sx[e], a.qscale, -top)) : kNegInf;
                     else
                         sc[e] -= top;
                     lowest = fminf(lowest, sc[e]);
@@ -1231,7 +1456,7 @@ decode_kernel(DecodeArgs a) {
                     lowest = 0.0f;
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (t0 + e < ntok) lowest = fminf(lowest, sc[e]);
+                        if (4 * kg + e < ntok) lowest = fminf(lowest, sc[e]);
                 }
                 if (__any(lowest < -126.0f)) {
 #pragma unroll
@@ -1241,10 +1466,6 @@ decode_kernel(DecodeArgs a) {
                     for (int e = 0; e < 4; ++e) sc[e] = __builtin_amdgcn_exp2f(sc[e]);
                 }
                 lrun += (sc[0] + sc[1]) + (sc[2] + sc[3]);
-                if constexpr (SCALED) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[e] *= cur.vs;
-                }
                 if constexpr (!EARLY) {
                     // the values: requested after them are the next page's keys
                     __builtin_amdgcn_sched_barrier(0);
@@ -1805,8 +2026,9 @@ hipError_t launch_read(int G, const DecodeArgs &a, hipStream_t s) {
     const dim3 grid(a.Hkv, a.W), mgrid(a.Hkv, a.R);
     constexpr int NW = waves_of<T, D>(), NT = 64 * NW;
     constexpr int NN = page_bytes_of<T, D>() <= 2048 ? 4 : NW;
-    const int columns = MODE == 3 ? a.list_width : a.max_pages;
-    const bool own = decode_own(columns, a.R, a.Hkv, page_bytes_of<T, D>(), NW, quad_heads<T>(G));
+    const int pages = MODE == 3 ? a.list_width : a.max_pages, columns = sizeof(T) == 1 ? cdiv(pages, 2) : pages;
+    const bool own = sizeof(T) == 1 ? decode_own_pairs(cdiv(columns, NW), a.R, a.Hkv)
+                                    : decode_own(columns, a.R, a.Hkv, page_bytes_of<T, D>(), NW, quad_heads<T>(G));
     const bool narrow = own && decode_own_narrow(a.R, a.Hkv), wide = (int64_t)a.Hkv * a.R < kWideMerge;
     switch (G) {
 #define GP_CASE(GG)                                                                \

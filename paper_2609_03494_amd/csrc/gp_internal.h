@@ -24,6 +24,9 @@ constexpr int kDecodeWorkgroups = GP_DECODE_WORKGROUPS;    // decode workgroups 
 #endif
 constexpr int kDecodeMinRun = GP_DECODE_MIN_RUN;           // pages a decode wave takes at least
 constexpr int kDecodeShortRun = 8;        // runs up to this many pages: one round of workgroups only
+// ... of 8-bit pages, in pairs (64 requests of 128-256 pages, 32/8 heads, d 64: 43.7 us, 50.3
+// with 8; 200 of 96-192: 91.7, with 8 99.9, with 24 106.6; d 128 within 3 % from 8 to 48)
+constexpr int kDecodeShortPairs = 48;
 constexpr int kDecodeOwnRun = 6;          // pages per wave up to which all requests take a workgroup each (see decode_kernel)
 constexpr int kDecodeResident = 512;      // decode workgroups that 256 CUs hold at once
 #ifndef GP_WIDE_MERGE
@@ -80,6 +83,17 @@ __host__ __device__ inline bool decode_own(int max_pages, int R, int Hkv, int pa
 // tokens: 256 requests 15.8 us against 20.3, 128 10.3 against 11.2; 16 requests of up
 // to 500 tokens the other way round, 9.8 against 8.1).
 __host__ __device__ inline bool decode_own_narrow(int R, int Hkv) { return (int64_t)R * Hkv >= 512; }
+
+// ... for 8-bit pages, which go in pairs (per: pairs per wave at most): a pair takes 1.0
+// us (d 64) or 1.3 (d 128) in a wave on its own.  Up to seven in any batch (one request
+// of 32/8 heads: 96 pages 12.5 us a call against 15.5 in equal runs, 128 14.9 and 12.9;
+// d 128), up to twelve with pairs for half the chip (16 of 96-192 pages, 32/8: 23.7 and
+// 23.7, of 112-224 26.6 and 24.7), up to sixteen with two workgroups per CU (64 of
+// 128-256, 32/8: 68.8 and 73.5).
+__host__ __device__ inline bool decode_own_pairs(int per, int R, int Hkv) {
+    const int64_t pairs = (int64_t)R * Hkv;
+    return per <= (pairs >= 448 ? 16 : pairs >= 128 ? 12 : 7);
+}
 
 struct DecodeWs {
     size_t partial, lens, prefix, total;
@@ -140,9 +154,10 @@ __host__ __device__ inline DecodeWs decode_ws(int R, int Hq, int Hkv, int D, int
     return w;
 }
 
-// Scores of a page selection, one per KV head and table column.
+// Scores of a page selection, one per KV head and table column, and room for the
+// last thread's whole reads.
 __host__ __device__ inline size_t select_ws(int R, int Hkv, int max_pages) {
-    return align_up((size_t)R * Hkv * max_pages * sizeof(float));
+    return align_up((size_t)R * Hkv * max_pages * sizeof(float) + 64);
 }
 
 struct ScoreWs {
@@ -304,6 +319,7 @@ struct SelectArgs {
     float *scores;                    // [R][Hkv][max_pages]
     int32_t *selected;                // [R][Hkv][budget]
     int R, Hkv, max_pages, pool_pages, budget, keep_first, keep_last;
+    int wave_pages;                   // pages that a wave scores (set at launch)
 };
 
 struct ScoreArgs {
