@@ -189,6 +189,9 @@ class KVLayer:
         return _KVLayer(_ptr(self.k), _ptr(self.v), pool, hkv, b, d, _dtype_code(self.k))
 
 
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+
+
 @dataclass
 class KV8Layer:
     """An 8-bit cache: K and V pools [pool_pages, num_kv_heads, 16, head_dim] of e4m3
@@ -199,14 +202,14 @@ class KV8Layer:
     v_scale: torch.Tensor
 
     def c(self) -> _KV8Layer:
-        pool, hkv, b, d = self.k.shape
-        for t in (self.k, self.v):
-            if t.dtype not in (torch.float8_e4m3fn, torch.uint8) or t.shape != self.k.shape:
-                raise ValueError("8-bit pools: two tensors of one shape, float8_e4m3fn or uint8")
-        for t in (self.k_scale, self.v_scale):
-            if t.dtype != torch.float32 or tuple(t.shape) != (pool, hkv):
-                raise ValueError("scales of an 8-bit cache: float32 [pool_pages, num_kv_heads]")
-        return _KV8Layer(_ptr(self.k), _ptr(self.v), _ptr(self.k_scale), _ptr(self.v_scale), pool, hkv, b, d)
+        k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
+        shape = k.shape
+        if v.shape != shape or k.dtype not in _CODES or v.dtype not in _CODES:
+            raise ValueError("8-bit pools: two tensors of one shape, float8_e4m3fn or uint8")
+        pool, hkv, b, d = shape
+        if ks.dtype != torch.float32 or vs.dtype != torch.float32 or ks.shape != (pool, hkv) or vs.shape != (pool, hkv):
+            raise ValueError("scales of an 8-bit cache: float32 [pool_pages, num_kv_heads]")
+        return _KV8Layer(_ptr(k), _ptr(v), _ptr(ks), _ptr(vs), pool, hkv, b, d)
 
 
 @dataclass
@@ -425,31 +428,31 @@ def gp_append_step(layers: list[KVLayer], ps: PageState, positions: torch.Tensor
     _check(st, "gp_append_step")
 
 
-def _rows(t: torch.Tensor, name: str) -> int:
-    """The stride from row to row of [tokens, heads, head_dim], contiguous within a row."""
-    if t.dim() != 3 or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
-        raise ValueError(f"{name}: [tokens, heads, head_dim], the heads of a token side by side")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
-
-
 def _append_rope(name, kv, dtype, ps, positions, k_new, v_new, rope_theta, q, q_out, tok_start, advance, stream):
-    _, hkv, _, d = kv.k.shape
-    T = k_new.shape[0]
-    for t, heads, what in ((k_new, hkv, "k_new"), (v_new, hkv, "v_new"), (q, None, "q")):
-        if t is not None and (t.dtype != dtype or t.dim() != 3 or t.shape[0] != T or t.shape[2] != d or
-                              (heads is not None and t.shape[1] != heads)):
-            raise ValueError(f"{name}: {what} [tokens, heads, head_dim], {dtype}")
-    if q is not None and (q_out is None or q_out.dtype != dtype or q_out.shape != q.shape):
-        raise ValueError(f"{name}: q_out of q's shape and dtype")
-    if tok_start is not None and (tok_start.dtype != torch.int32 or tok_start.numel() != ps.page_table.shape[0] + 1):
-        raise ValueError(f"{name}: tok_start [num_reqs + 1] int32")
     c_kv, c_ps = kv.c(), ps.c()
-    st = getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(positions), _ptr(tok_start), T,
-                               None if q is None else q.data_ptr(), 0 if q is None else _rows(q, "q"),
-                               None if q is None else _ptr(q_out), k_new.data_ptr(), _rows(k_new, "k_new"),
-                               v_new.data_ptr(), _rows(v_new, "v_new"), 0 if q is None else q.shape[1],
-                               float(rope_theta), int(bool(advance)), _stream(stream))
+    d, shape = c_kv.head_dim, k_new.shape
+    T = shape[0]
+    if shape != (T, c_kv.num_kv_heads, d) or v_new.shape != shape or k_new.dtype != dtype or v_new.dtype != dtype:
+        raise ValueError(f"{name}: k_new and v_new [tokens, {c_kv.num_kv_heads}, {d}], {dtype}")
+    Hq = q_ptr = qo_ptr = q_row = 0
+    if q is not None:
+        Hq = q.shape[1] if q.dim() == 3 else 0
+        if q.shape != (T, Hq, d) or q.dtype != dtype or q_out is None or q_out.shape != q.shape or q_out.dtype != dtype:
+            raise ValueError(f"{name}: q and q_out [tokens, heads, {d}], {dtype}")
+        q_ptr, qo_ptr, q_row = q.data_ptr(), _ptr(q_out), _row(q.stride(), T, Hq, d, name)
+    if tok_start is not None and (tok_start.dtype != torch.int32 or tok_start.numel() != c_ps.num_reqs + 1):
+        raise ValueError(f"{name}: tok_start [num_reqs + 1] int32")
+    st = getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(positions), _ptr(tok_start), T, q_ptr, q_row,
+                               qo_ptr, k_new.data_ptr(), _row(k_new.stride(), T, shape[1], d, name), v_new.data_ptr(),
+                               _row(v_new.stride(), T, shape[1], d, name), Hq, rope_theta, bool(advance), _stream(stream))
     _check(st, name)
+
+
+def _row(strides, T: int, heads: int, d: int, name: str) -> int:
+    """The stride from token to token of [tokens, heads, head_dim]: any, a token's own elements side by side."""
+    if strides[2] != 1 or (heads > 1 and strides[1] != d):
+        raise ValueError(f"{name}: the heads of a token lie side by side")
+    return strides[0] if T > 1 else heads * d
 
 
 def gp_append_rope(kv: KVLayer, ps: PageState, positions: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
@@ -488,14 +491,13 @@ def gp_decode_attention_q8(kv: KV8Layer, ps: PageState, q_post: torch.Tensor, sc
 
 
 def _page_bounds(name, kv, dtype, ps, bounds, from_tokens, max_update, stream):
-    pool, hkv, _, d = kv.k.shape
-    if bounds.dtype != dtype or tuple(bounds.shape) != (pool, hkv, 2, d):
-        raise ValueError(f"{name}: bounds [pool_pages, num_kv_heads, 2, head_dim], {dtype}")
-    if from_tokens is not None and (from_tokens.dtype != torch.int32 or from_tokens.numel() != ps.page_table.shape[0]):
-        raise ValueError(f"{name}: from_tokens [num_reqs] int32")
     c_kv, c_ps = kv.c(), ps.c()
-    _check(getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(from_tokens), int(max_update),
-                                 _ptr(bounds), _stream(stream)), name)
+    if bounds.dtype != dtype or bounds.shape != (c_kv.pool_pages, c_kv.num_kv_heads, 2, c_kv.head_dim):
+        raise ValueError(f"{name}: bounds [pool_pages, num_kv_heads, 2, head_dim], {dtype}")
+    if from_tokens is not None and (from_tokens.dtype != torch.int32 or from_tokens.numel() != c_ps.num_reqs):
+        raise ValueError(f"{name}: from_tokens [num_reqs] int32")
+    _check(getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(from_tokens), max_update, _ptr(bounds),
+                                 _stream(stream)), name)
 
 
 def gp_page_bounds(kv: KVLayer, ps: PageState, bounds: torch.Tensor, from_tokens: torch.Tensor | None = None,
@@ -511,19 +513,20 @@ def gp_page_bounds_q8(kv: KV8Layer, ps: PageState, bounds: torch.Tensor, from_to
 
 
 def _lists(selected: torch.Tensor, R: int, Hkv: int) -> int:
-    if selected.dtype != torch.int32 or selected.dim() != 3 or selected.shape[0] != R or selected.shape[1] != Hkv:
+    shape = selected.shape
+    if selected.dtype != torch.int32 or len(shape) != 3 or shape[:2] != (R, Hkv):
         raise ValueError("selected: int32 [num_reqs, num_kv_heads, budget]")
-    return selected.shape[2]
+    return shape[2]
 
 
 def gp_select_pages(bounds: torch.Tensor, ps: PageState, q_post: torch.Tensor, keep_first: int, keep_last: int,
                     selected: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
     """The logical pages each request and KV head is to read, into selected [R, Hkv, budget] int32."""
-    pool, hkv, _, d = bounds.shape
-    R, Hq, _ = q_post.shape
-    budget = _lists(selected, R, hkv)
     c_ps = ps.c()
-    if pool != c_ps.pool_pages or R != c_ps.num_reqs or q_post.shape[2] != d:
+    pool, hkv, two, d = bounds.shape
+    R, Hq, dq = q_post.shape
+    budget = _lists(selected, R, hkv)
+    if pool != c_ps.pool_pages or R != c_ps.num_reqs or dq != d or two != 2:
         raise ValueError("gp_select_pages: bounds [pool_pages, Hkv, 2, d] and q_post [R, Hq, d] of the page state")
     st = load().gp_select_pages(_ptr(bounds), _dtype_code(bounds), ctypes.byref(c_ps),
                                 _of(q_post, bounds.dtype, "q_post"), Hq, hkv, d, budget, keep_first, keep_last,
@@ -532,8 +535,8 @@ def gp_select_pages(bounds: torch.Tensor, ps: PageState, q_post: torch.Tensor, k
 
 
 def _decode_pages(name, kv, dtype, ps, selected, q_post, scale, out, ws, stream):
-    budget = _lists(selected, ps.page_table.shape[0], kv.k.shape[1])
     c_kv, c_ps = kv.c(), ps.c()
+    budget = _lists(selected, c_ps.num_reqs, c_kv.num_kv_heads)
     _check(getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(selected), budget,
                                  _of(q_post, dtype, "q_post"), q_post.shape[1], scale, _of(out, dtype, "out"), _ptr(ws),
                                  ws.numel(), _stream(stream)), name)
