@@ -2026,7 +2026,11 @@ hipError_t launch_read(int G, const DecodeArgs &a, hipStream_t s) {
     const dim3 grid(a.Hkv, a.W), mgrid(a.Hkv, a.R);
     constexpr int NW = waves_of<T, D>(), NT = 64 * NW;
     constexpr int NN = page_bytes_of<T, D>() <= 2048 ? 4 : NW;
-    const int pages = MODE == 3 ? a.list_width : a.max_pages, columns = sizeof(T) == 1 ? cdiv(pages, 2) : pages;
+    // the rules were measured on requests of half to all of the table's width; lists are as
+    // long as they are wide, so equal runs and their merge cost a third more there, a
+    // workgroup per request the same (16 lists of 200 pages, 8 KV heads, 8 bits, d 64: 23.5 us
+    // and 20.0)
+    const int pages = MODE == 3 ? cdiv(3 * a.list_width, 4) : a.max_pages, columns = sizeof(T) == 1 ? cdiv(pages, 2) : pages;
     const bool own = sizeof(T) == 1 ? decode_own_pairs(cdiv(columns, NW), a.R, a.Hkv)
                                     : decode_own(columns, a.R, a.Hkv, page_bytes_of<T, D>(), NW, quad_heads<T>(G));
     const bool narrow = own && decode_own_narrow(a.R, a.Hkv), wide = (int64_t)a.Hkv * a.R < kWideMerge;

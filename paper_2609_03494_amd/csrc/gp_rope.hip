@@ -33,10 +33,19 @@ typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 typedef u32x4_t u32x4_e2_t __attribute__((aligned(2)));
 typedef u32x4_t u32x4_e4_t __attribute__((aligned(4)));
-__device__ inline u32x4_t load16(const uint16_t *p) { return *reinterpret_cast<const u32x4_e2_t *>(p); }
-__device__ inline u32x4_t load16(const float *p) { return *reinterpret_cast<const u32x4_e4_t *>(p); }
-__device__ inline void store16(uint16_t *p, const u32x4_t &x) { *reinterpret_cast<u32x4_e2_t *>(p) = x; }
-__device__ inline void store16(float *p, const u32x4_t &x) { *reinterpret_cast<u32x4_e4_t *>(p) = x; }
+template <typename E>
+using Piece = typename std::conditional<sizeof(E) == 4, u32x4_e4_t, u32x4_e2_t>::type;
+// 16 bytes; STREAM: past the caches
+template <bool STREAM, typename E>
+__device__ inline u32x4_t load16(const E *p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const Piece<E> *>(p));
+    else return *reinterpret_cast<const Piece<E> *>(p);
+}
+template <bool STREAM, typename E>
+__device__ inline void store16(E *p, const u32x4_t &x) {
+    if constexpr (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<Piece<E> *>(p));
+    else *reinterpret_cast<Piece<E> *>(p) = x;
+}
 
 // the elements of 16 bytes, widened, and back
 __device__ inline void widen(const u32x4_t &u, float (&x)[8]) {
@@ -128,8 +137,9 @@ __device__ inline uint32_t codes(float a, float b, float c, float d) {
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kBatch = 4;                             // row pieces in flight per thread
 
-// CACHE: bytes of a pool element.
-template <int CACHE, int D>
+// CACHE: bytes of a pool element.  STREAM: the call moves more than the last-level
+// cache holds (see launch_cd).
+template <int CACHE, int D, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     using E = typename std::conditional<CACHE == 4, float, uint16_t>::type;
     constexpr int EPU = 16 / (int)sizeof(E);          // elements per 16 bytes
@@ -194,8 +204,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                     to[k] = reinterpret_cast<E *>(isv ? a.v : a.k) + (((size_t)pid * a.Hkv + h) * kPage + lo + row[k]) * D;
                     turn[k] = !isv;
                 }
-                p[k] = load16(src + u * EPU);
-                q[k] = load16(src + H + u * EPU);
+                p[k] = load16<STREAM>(src + u * EPU);
+                q[k] = load16<STREAM>(src + H + u * EPU);
             }
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
@@ -209,8 +219,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                     p[k] = narrow(xa);
                     q[k] = narrow(xb);
                 }
-                store16(to[k] + u * EPU, p[k]);
-                store16(to[k] + H + u * EPU, q[k]);
+                store16<STREAM>(to[k] + u * EPU, p[k]);
+                store16<STREAM>(to[k] + H + u * EPU, q[k]);
             }
         }
     }
@@ -233,11 +243,13 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
             for (int half = 0; half < 2; ++half)
 #pragma unroll
                 for (int c = 0; c < EH; c += 8)
-                    widen(load16(src + half * H + c), reinterpret_cast<float(&)[8]>(x[half][c]));
+                    widen(load16<STREAM>(src + half * H + c), reinterpret_cast<float(&)[8]>(x[half][c]));
             if (!isv) {
 #pragma unroll
                 for (int e = 0; e < EH; ++e) rotate(x[0][e], x[1][e], s_cs[rr][sub * EH + e]);
             }
+            float *sp = (isv ? a.v_scale : a.k_scale) + (size_t)pid * a.Hkv + h;
+            float old = lo > 0 ? *sp : 0.0f;          // the page held tokens before (wave-uniform; requested with the rows)
             float amax = 0.0f;
 #pragma unroll
             for (int half = 0; half < 2; ++half)
@@ -248,11 +260,9 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                     else x[half][e] = __builtin_nanf("");
                 }
             amax = wave_max(mine ? amax : 0.0f);
-            float *sp = (isv ? a.v_scale : a.k_scale) + (size_t)pid * a.Hkv + h;
-            float scale = scale_for(amax), old = scale;
+            float scale = scale_for(amax);
             uint8_t *page = reinterpret_cast<uint8_t *>(isv ? a.v : a.k) + ((size_t)pid * a.Hkv + h) * kPage * D + slot * D + sub * EH;
-            if (lo > 0) {                             // the page held tokens before (wave-uniform)
-                old = *sp;
+            if (lo > 0) {
                 scale = fmaxf(scale, old);
                 if (scale > old && slot < lo) {       // their codes under the new scale
                     const float f = old / scale;
@@ -300,12 +310,18 @@ __global__ __launch_bounds__(256) void rope_advance_kernel(RopeArgs a) {
 template <int CACHE, int D>
 void launch_cd(const RopeArgs &a, hipStream_t s) {
     const int items = a.start ? a.T / kPage + 2 * a.R : a.R;
-    // heads split so that about 1024 workgroups are there, none with less than a
-    // batch of pieces or one 8-bit job per wave
+    // heads split so that about 1024 workgroups are there, as long as each has a batch of
+    // pieces per thread or, in 8 bits, one job per wave
     const int pieces = (a.start ? kPage : 1) * (a.Hq + 2 * a.Hkv) * (D / 2) / (CACHE == 4 ? 4 : 8);
-    const int most = std::max(1, std::min(cdiv(pieces, kThreads * kBatch), cdiv(2 * a.Hkv, kWaves)));
+    const int most = CACHE == 1 ? cdiv(2 * a.Hkv, kWaves) : cdiv(pieces, kThreads * kBatch);
     const int split = std::max(1, std::min(most, cdiv(1024, items)));
-    rope_kernel<CACHE, D><<<dim3(items, split), kThreads, 0, s>>>(a);
+    // rows past the caches where the call would only displace what others keep there (256
+    // MB): 28 k tokens of 64/8 heads, d 128, 1.7 GB, 349 -> 338 us; chunks in 8 bits, 0.7 GB,
+    // 146 -> 135.  Smaller calls leave the queries there for the attention that follows.
+    const int64_t row = (int64_t)D * (CACHE == 4 ? 4 : 2), bytes = a.T * row * (2 * a.Hq + 3 * a.Hkv);
+    const dim3 grid(items, split);
+    if (bytes > (int64_t)256 << 20) rope_kernel<CACHE, D, true><<<grid, kThreads, 0, s>>>(a);
+    else rope_kernel<CACHE, D, false><<<grid, kThreads, 0, s>>>(a);
 }
 
 }  // namespace
