@@ -545,6 +545,7 @@ typedef struct {
  *  - advance != 0: seq_lens[r] and positions[r] of the requests that took
  *    their tokens then grow by n_r (pass 0 for every layer of a model but the
  *    last, as in gp_decode_step).
+ * At most 2^27 tokens and 8192 KV heads (GP_ERR_UNSUPPORTED).
  * Rows and pools may lie at any multiple of their element's size (8-bit
  * pools: 16 bytes).  Pages that requests share are not copied: the caller
  * gives a request private pages from m_r on.  The page states are read on the
@@ -587,7 +588,8 @@ gp_status_t gp_decode_attention_q8(const gp_kv8_layer_t *kv, const gp_page_state
  * (from_tokens [num_reqs] int32 on the device; NULL: from 0), of each request
  * at most max_update pages, counted from the first (0: no limit; a limit keeps
  * the launch small where the lengths are known, e.g. 1 after a decode step).
- * Other pages' bounds stay as they were.  To be called after tokens went in
+ * Other pages' bounds stay as they were.  At most 8192 KV heads, here and in
+ * gp_select_pages.  To be called after tokens went in
  * and, for all of a request's pages, after a compaction moved its rows.  A
  * held request is left out. */
 gp_status_t gp_page_bounds(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const int32_t *from_tokens,

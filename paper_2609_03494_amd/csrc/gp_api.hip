@@ -384,7 +384,9 @@ gp_status_t rope_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, const 
     if (std::max({k_stride, v_stride, q ? q_stride : 0}) > int64_t(1) << 30) return GP_ERR_INVALID;
     if (ps->num_reqs == 0 || num_tokens == 0) return GP_OK;
     if (!positions || !k_new || !v_new || (q && !q_out)) return GP_ERR_INVALID;
-    if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages || kv->num_kv_heads > 65535) return GP_ERR_UNSUPPORTED;
+    if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages || kv->num_kv_heads > kMaxListedHeads)
+        return GP_ERR_UNSUPPORTED;
+    if (num_tokens > kMaxRopeTokens) return GP_ERR_UNSUPPORTED;
     if (q) {
         const int64_t t = num_tokens - 1;
         if (overlap(q_out, t * qrow + qrow, q, t * q_stride + qrow, e) && !(q == q_out && q_stride == qrow)) return GP_ERR_INVALID;
@@ -431,7 +433,8 @@ gp_status_t bounds_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, cons
     if (max_update < 0) return GP_ERR_INVALID;
     if (ps->num_reqs == 0) return GP_OK;
     if (!bounds) return GP_ERR_INVALID;
-    if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages || kv->num_kv_heads > 65535) return GP_ERR_UNSUPPORTED;
+    if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages || kv->num_kv_heads > kMaxListedHeads)
+        return GP_ERR_UNSUPPORTED;
     BoundsArgs a = {};
     a.k = kv->k;
     a.k_scale = kv8 ? kv8->k_scale : nullptr;
@@ -497,7 +500,7 @@ gp_status_t gp_select_pages(const void *bounds, gp_dtype_t dtype, const gp_page_
         return GP_ERR_INVALID;
     if (ps->num_reqs == 0) return GP_OK;
     if (!bounds || !q_post || !selected || !ws) return GP_ERR_INVALID;
-    if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages || num_kv_heads > 65535) return GP_ERR_UNSUPPORTED;
+    if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages || num_kv_heads > kMaxListedHeads) return GP_ERR_UNSUPPORTED;
     if (ws_bytes < select_ws(ps->num_reqs, num_kv_heads, ps->max_pages)) return GP_ERR_WORKSPACE;
     SelectArgs a = {};
     a.bounds = bounds;

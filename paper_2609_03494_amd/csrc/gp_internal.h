@@ -36,6 +36,8 @@ constexpr int kWideMerge = GP_WIDE_MERGE; // (KV head, request) pairs below whic
 constexpr int kPrefixSlotPages = 64;      // pages of one partial slot of a shared prefix, about
 constexpr int kMaxPrefixSlotPages = 128;  // and at most (LDS id table)
 constexpr int kMaxDecodePages = 8192;     // table width the decode calls accept
+constexpr int kMaxRopeTokens = 1 << 27;   // tokens one gp_append_rope call takes, and
+constexpr int kMaxListedHeads = 8192;     // KV heads it, the page bounds and the selection take: grids below 2^32 threads
 constexpr size_t kScratchBytes = size_t(8) << 20;   // static scratch of gp_decode_attention_noalloc
 constexpr int kMaxBoundaryPages = 4096;                    // table width the boundary calls accept
 constexpr int kMaxBnd = 2048;             // boundary requests one apply, select, decide or compact call takes

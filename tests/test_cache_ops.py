@@ -63,6 +63,8 @@ def test_append_rope_refusals(lib, q8):
     assert _rope(fn, kv(), _ps(), hq=24) == UNSUPPORTED
     assert _rope(fn, kv(), _ps(width=8193)) == UNSUPPORTED
     assert _rope(fn, kv(), _ps(R=65536), tokens=65536) == UNSUPPORTED
+    assert _rope(fn, kv(), _ps(), tokens=(1 << 27) + 1, start=FAKE, q=None) == UNSUPPORTED
+    assert _rope(fn, kv(hkv=8193), _ps(), q=None, k_stride=1 << 21, v_stride=1 << 21) == UNSUPPORTED
     # nothing to do
     assert _rope(fn, kv(), _ps(R=0), tokens=0) == 0
     assert _rope(fn, kv(), _ps(), tokens=0, start=FAKE) == 0

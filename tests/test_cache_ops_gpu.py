@@ -436,6 +436,70 @@ def test_decode_q8_nan_and_bad_pages():
         assert bool(((got[r] - want).abs() <= _attention_tol(want, mag, size, d, BF16)).all()), r
 
 
+@pytest.mark.parametrize("spare", [2, 130])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (3, 3, 64)])
+def test_decode_q8_pages_gone(hq, hkv, d, spare):
+    """Page ids outside the pool, two or more in a row, at a request's ends and all of one's: they add
+    nothing, whatever page 0 and its scales hold."""
+    _say(f"decode q8 pages gone heads {hq}/{hkv} d {d} spare {spare}")
+    gen = torch.Generator().manual_seed(6 + spare)
+    lens = [200, 33, 64, 1500, 16]
+    npages = [-(-m // 16) for m in lens]
+    width = max(npages) + spare
+    kv, pool, table = _q8_cache(lens, npages, hkv, d, gen, width, pow2=False)
+    k64, v64 = _values(kv.k, kv.k_scale), _values(kv.v, kv.v_scale)
+    gone = {0: [0, 1, 2, 5, 12], 1: [2], 2: [0, 1, 2, 3], 3: list(range(40, 71)) + [93], 4: []}
+    ps = _state(table, npages, lens, pool)
+    owner = (table == 0).nonzero()
+    if len(owner):                                        # page 0 belongs to nobody in what follows
+        gone[int(owner[0, 0])].append(int(owner[0, 1]))
+    for r, ps_ in gone.items():
+        for i, p in enumerate(ps_):
+            ps.page_table[r, p] = (-1, pool, -2 ** 31, 2 ** 31 - 1)[i % 4]
+    kv.k[0], kv.v[0], kv.k_scale[0], kv.v_scale[0] = 0x7f, 0xff, NAN, NAN
+    q = torch.randn(len(lens), hq, d, generator=gen).to(BF16)
+    out = torch.empty(len(lens), hq, d, dtype=BF16, device=DEV)
+    gp.gp_decode_attention_q8(kv, ps, q.to(DEV), 0.2, out, gp.workspace(gp.GP_OP_DECODE, len(lens), 0, hq, hkv, d, width, BF16))
+    torch.cuda.synchronize()
+    got = out.cpu().double()
+    for r, m in enumerate(lens):
+        keep = [i for i in range(m) if i // 16 not in gone[r]]
+        if not keep:
+            assert bool((got[r] == 0).all()), r
+            continue
+        want, mag, size = _attention(_tokens(k64, table, r, m)[:, keep], _tokens(v64, table, r, m)[:, keep], q[r].double(), 0.2)
+        assert bool(((got[r] - want).abs() <= _attention_tol(want, mag, size, d, BF16)).all()), r
+
+
+@pytest.mark.parametrize("spare", [2, 130])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (3, 3, 64)])
+def test_decode_q8_small_weights(hq, hkv, d, spare):
+    """A weight of 2^-128 beside one of 1 whose value is zero: the result is that weight times its value, to the
+    2^-150 that a subnormal weight is off (2^-22 of the result), the tokens in one page, in a pair and in two."""
+    _say(f"decode q8 small weights heads {hq}/{hkv} d {d} spare {spare}")
+    lens, gen = [2, 17, 33], torch.Generator().manual_seed(1)
+    npages = [1, 2, 3]
+    kv, pool, table = _q8_cache(lens, npages, hkv, d, gen, 3 + spare)
+    code = lambda x: int(torch.tensor(x).to(torch.float8_e4m3fn).view(torch.uint8))  # noqa: E731
+    for r, m in enumerate(lens):
+        for p in range(npages[r]):
+            pid, t = int(table[r, p]), min(16, m - 16 * p)
+            kv.k[pid, :, :t], kv.v[pid, :, :t] = 0, 0
+            kv.k[pid, :, :t, 0] = code(-384.0)
+            kv.k_scale[pid], kv.v_scale[pid] = 2.0, 2.0 ** 93
+        kv.k[int(table[r, 0]), :, 0, 0] = 0
+        kv.k[int(table[r, (m - 1) // 16]), :, (m - 1) % 16, 0] = code(-64.0)
+        kv.v[int(table[r, (m - 1) // 16]), :, (m - 1) % 16] = code(128.0)
+    q = torch.zeros(3, hq, d, dtype=BF16, device=DEV)
+    q[..., 0] = 1.0
+    out = torch.empty_like(q)
+    gp.gp_decode_attention_q8(kv, _state(table, npages, lens, pool), q, 1.0 / 1.4426950408889634, out,
+                              gp.workspace(gp.GP_OP_DECODE, 3, 0, hq, hkv, d, 3 + spare, BF16))
+    torch.cuda.synchronize()
+    # the float32 scale moves 2^-128 by 128 of its roundings at most, and the result is rounded to bfloat16
+    assert bool(((out.cpu().double() / 2.0 ** -28 - 1).abs() <= 2.0 ** -8).all()), out.flatten()[:4]
+
+
 # -------------------------------------------------------------------- bounds --
 
 def _cache(kind, lens, npages, hkv, d, gen, width):
@@ -525,8 +589,8 @@ def _select64(bounds, table, n, q, hkv, budget, first, last, r):
             box = bounds[table[r, :n].long(), h].double()                 # [n][2][d]
             x = q[r].double().view(hkv, -1, 1, d)[h]
             score = torch.maximum(x * box[:, 0], x * box[:, 1]).sum((0, 2)).float()
-            score = torch.where(score.isnan(), float("inf"), score)
             middle = torch.arange(first, n - last)
+            # (torch sorts NaN as the greatest)
             best = middle[score[middle].sort(dim=0, descending=True, stable=True)[1]][:budget - first - last]
             pick = torch.cat([torch.arange(first), best, torch.arange(n - last, n)]).sort()[0]
         out[h, :len(pick)] = pick.int()
@@ -608,6 +672,35 @@ def test_select_extreme_scores(dtype):
     assert 10 not in got[4, 0].tolist() and 11 not in got[4, 0].tolist()
 
 
+@pytest.mark.parametrize("n,width,budget", [(2000, 2048, 700), (1000, 1000, 300), (8192, 8192, 4000), (600, 700, 3)])
+def test_select_many_alike(n, width, budget):
+    """Hundreds of pages of the same score at the border of the selection: the lowest are taken; beside
+    them others above and below, or NaN, or nothing else."""
+    _say(f"select many alike {n} of {width} budget {budget}")
+    hq, hkv, d = 4, 2, 64
+    gen = torch.Generator().manual_seed(n)
+    pool, table = _paged([n] * 4, width, gen)
+    bounds = torch.ones(pool, hkv, 2, d, dtype=BF16)
+    some = torch.randperm(n, generator=gen)
+    up, down = some[:budget // 3], some[budget // 3:budget // 3 + n // 8]
+    bounds[table[1, up].long()] = 3.0
+    bounds[table[1, down].long()] = torch.randn(len(down), 1, 1, 1, generator=gen).clamp(-2, 0.9).to(BF16)
+    bounds[table[2, some[:n // 2]].long(), :, 1, 5] = NAN
+    bounds[table[3, up].long(), :, 1] = float("inf")
+    bounds[table[3, down].long(), :, 0] = -float("inf")
+    q = torch.ones(4, hq, d, dtype=BF16)
+    sel = torch.empty(4, hkv, budget, dtype=torch.int32, device=DEV)
+    ws = gp.workspace(gp.GP_OP_SELECT, 4, 0, hq, hkv, d, width, BF16)
+    gp.gp_select_pages(bounds.to(DEV), _state(table, [n] * 4, [16 * n - 5] * 4, pool), q.to(DEV), 1, 1, sel, ws)
+    torch.cuda.synchronize()
+    got = sel.cpu()
+    for r in range(4):
+        b = bounds.clone()
+        if r == 3:                                        # a least value of -inf meets no negative query
+            b[..., 0, :] = torch.where(b[..., 0, :].isinf(), torch.zeros(()).to(BF16), b[..., 0, :])
+        assert torch.equal(got[r], _select64(b, table, n, q, hkv, budget, 1, 1, r)), r
+
+
 # --------------------------------------------------------- attention over lists --
 
 @pytest.mark.parametrize("kind,hq,hkv,d", [("bf16", 8, 2, 128), ("bf16", 3, 3, 64), ("f32", 8, 1, 64), ("f32", 4, 2, 128),
@@ -658,7 +751,138 @@ def test_decode_pages(kind, hq, hkv, d, name, budget):
             assert bool(((mine - want).abs() <= tol).all()), (r, h, float(((mine - want).abs() - tol).max()))
 
 
+@pytest.mark.parametrize("kind", ["bf16", "q8"])
+def test_decode_pages_many_requests(kind):
+    """More requests than a block of the split's scan, lists of a few pages."""
+    _say(f"decode pages many requests {kind}")
+    hq, hkv, d, budget = 4, 2, 64, 5
+    gen = torch.Generator().manual_seed(12)
+    lens = [(r * 37) % 150 for r in range(1100)]
+    npages = [-(-m // 16) for m in lens]
+    kv, pool, table, k64, v64 = _cache(kind, lens, npages, hkv, d, gen, max(npages) + 40)
+    sel = torch.randint(-1, 10, (len(lens), hkv, budget), generator=gen).int()
+    q = torch.randn(len(lens), hq, d, generator=gen).to(BF16)
+    for columns in (budget, 80):                          # a workgroup per request, or equal runs of the batch
+        wide = torch.cat([sel, torch.full((len(lens), hkv, columns - budget), -1, dtype=torch.int32)], 2)
+        out = torch.full((len(lens), hq, d), NAN, dtype=BF16, device=DEV)
+        ws = gp.workspace(gp.GP_OP_DECODE, len(lens), 0, hq, hkv, d, columns, BF16)
+        (gp.gp_decode_attention_pages_q8 if kind == "q8" else gp.gp_decode_attention_pages)(
+            kv, _state(table, npages, lens, pool), wide.to(DEV), q.to(DEV), 0.125, out, ws)
+        torch.cuda.synchronize()
+        got = out.cpu().double()
+        for r, m in enumerate(lens):
+            n = -(-m // 16)
+            for h in range(hkv):
+                tok = [16 * p + i for p in wide[r, h, :min(n, columns)].tolist() if 0 <= p < n for i in range(min(16, m - 16 * p))]
+                mine = got[r, 2 * h:2 * h + 2]
+                if not tok:
+                    assert bool((mine == 0).all()), (r, h)
+                    continue
+                want, mag, size = _attention(_tokens(k64, table, r, m)[h:h + 1, tok], _tokens(v64, table, r, m)[h:h + 1, tok],
+                                             q[r, 2 * h:2 * h + 2].double(), 0.125)
+                assert bool(((mine - want).abs() <= _attention_tol(want, mag, size, d, BF16)).all()), (r, h)
+
+
 # --------------------------------------------------------------- all together --
+
+@pytest.mark.parametrize("kind", ["bf16", "q8"])
+def test_pools_past_32_bits(kind):
+    """Pools of more than 2^32 bytes, their last pages used: prompts in, bounds, selection, attention."""
+    hkv, d, hq, budget = 8, 128, 16, 6
+    dt, size = (torch.uint8, 1) if kind == "q8" else (BF16, 2)
+    pool = (2 ** 32 + 2 ** 28) // (hkv * 16 * d * size)
+    _say(f"pools past 32 bits {kind}, {pool} pages")
+    lens = [200, 37]
+    npages = [-(-m // 16) for m in lens]
+    table = torch.full((2, 16), -1, dtype=torch.int32)
+    table[0, :13], table[1, :3] = pool - 1 - torch.arange(13), pool - 20 - torch.arange(3)
+    k, v = (torch.empty(pool, hkv, 16, d, dtype=dt, device=DEV) for _ in range(2))
+    if kind == "q8":
+        kv = gp.KV8Layer(k, v, torch.zeros(pool, hkv, device=DEV), torch.zeros(pool, hkv, device=DEV))
+    else:
+        kv = gp.KVLayer(k, v)
+    bounds = torch.empty(pool, hkv, 2, d, dtype=BF16, device=DEV)
+    ps = _state(table, npages, [0, 0], pool)
+    gen = torch.Generator().manual_seed(5)
+    T = sum(lens)
+    kn, vn = (torch.randn(T, hkv, d, generator=gen).to(BF16) for _ in range(2))
+    q = torch.randn(2, hq, d, generator=gen).to(BF16)
+    q8 = kind == "q8"
+    (gp.gp_append_rope_q8 if q8 else gp.gp_append_rope)(kv, ps, _i32([-1, -1]), kn.to(DEV), vn.to(DEV), 1e4, tok_start=_i32([0, lens[0], T]))
+    (gp.gp_page_bounds_q8 if q8 else gp.gp_page_bounds)(kv, ps, bounds)
+    sel = torch.zeros(2, hkv, budget, dtype=torch.int32, device=DEV)
+    gp.gp_select_pages(bounds, ps, q.to(DEV), 1, 1, sel, gp.workspace(gp.GP_OP_SELECT, 2, 0, hq, hkv, d, 16, BF16))
+    outs = [torch.zeros(2, hq, d, dtype=BF16, device=DEV) for _ in range(2)]
+    (gp.gp_decode_attention_pages_q8 if q8 else gp.gp_decode_attention_pages)(
+        kv, ps, sel, q.to(DEV), 0.1, outs[0], gp.workspace(gp.GP_OP_DECODE, 2, 0, hq, hkv, d, budget, BF16))
+    (gp.gp_decode_attention_q8 if q8 else gp.gp_decode_attention)(
+        kv, ps, q.to(DEV), 0.1, outs[1], gp.workspace(gp.GP_OP_DECODE, 2, 0, hq, hkv, d, 16, BF16))
+    torch.cuda.synchronize()
+    start = 0
+    for r, m in enumerate(lens):
+        ids = table[r, :npages[r]].long().to(DEV)
+        K, V = kv.k[ids].cpu(), kv.v[ids].cpu()
+        K, V = ((_values(K, kv.k_scale[ids]), _values(V, kv.v_scale[ids])) if q8 else (K.double(), V.double()))
+        K, V = (x.transpose(0, 1).flatten(1, 2)[:, :m] for x in (K, V))
+        want, mag = _rotated(kn[start:start + m].double(), torch.arange(m), 1e4)
+        step = 2.0 ** -4 if q8 else 2.0 ** -8             # (no value of these is below e4m3's normal range by much)
+        floor = 2.0 ** -10 * float(kv.k_scale[ids].max()) if q8 else 0.0
+        assert bool(((K.transpose(0, 1) - want).abs() <= want.abs() * step + ROT * mag + floor).all())
+        start += m
+        box, n = bounds[ids].cpu(), npages[r]
+        local = torch.arange(n).view(1, n).expand(2, n)
+        want_sel = _select64(box, local, n, q, hkv, budget, 1, 1, r)
+        assert torch.equal(sel[r].cpu(), want_sel)
+        for h in range(hkv):
+            g = slice(2 * h, 2 * h + 2)
+            tok = [16 * p + i for p in want_sel[h].tolist() if p >= 0 for i in range(min(16, m - 16 * p))]
+            for out, pick in ((outs[0], tok), (outs[1], list(range(m)))):
+                want, mag, size = _attention(K[h:h + 1, pick], V[h:h + 1, pick], q[r, g].double(), 0.1)
+                assert bool(((out[r, g].cpu().double() - want).abs() <= _attention_tol(want, mag, size, d, BF16)).all()), (r, h)
+
+
+def test_two_streams_at_once():
+    """Two batches on two streams with workspaces of their own: the results of one after the other."""
+    _say("two streams at once")
+    hq, hkv, d, budget = 32, 8, 128, 20
+    gen = torch.Generator().manual_seed(77)
+    batches = []
+    for b in range(2):
+        lens = [700 + 90 * ((r + b) % 11) for r in range(24)]
+        npages = [-(-m // 16) for m in lens]
+        width = max(npages) + 200
+        kv, pool, table = _q8_cache(lens, npages, hkv, d, gen, width)
+        batches.append(dict(kv=kv, ps=_state(table, npages, lens, pool), q=torch.randn(24, hq, d, generator=gen).to(BF16).to(DEV),
+                            bounds=torch.zeros(pool, hkv, 2, d, dtype=BF16, device=DEV),
+                            sel=torch.zeros(24, hkv, budget, dtype=torch.int32, device=DEV),
+                            out=[torch.zeros(24, hq, d, dtype=BF16, device=DEV) for _ in range(2)],
+                            ws=[gp.workspace(gp.GP_OP_SELECT, 24, 0, hq, hkv, d, width, BF16),
+                                gp.workspace(gp.GP_OP_DECODE, 24, 0, hq, hkv, d, budget, BF16),
+                                gp.workspace(gp.GP_OP_DECODE, 24, 0, hq, hkv, d, width, BF16)],
+                            stream=torch.cuda.Stream()))
+
+    def go(x, stream):
+        gp.gp_page_bounds_q8(x["kv"], x["ps"], x["bounds"], stream=stream)
+        gp.gp_select_pages(x["bounds"], x["ps"], x["q"], 1, 2, x["sel"], x["ws"][0], stream=stream)
+        gp.gp_decode_attention_pages_q8(x["kv"], x["ps"], x["sel"], x["q"], 0.1, x["out"][0], x["ws"][1], stream=stream)
+        gp.gp_decode_attention_q8(x["kv"], x["ps"], x["q"], 0.1, x["out"][1], x["ws"][2], stream=stream)
+
+    torch.cuda.synchronize()
+    for x in batches:
+        go(x, None)
+    torch.cuda.synchronize()
+    alone = [[t.clone() for t in (x["bounds"], x["sel"], *x["out"])] for x in batches]
+    for x in batches:
+        for t in (x["bounds"], x["sel"], *x["out"]):
+            t.zero_()
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for x in batches:
+            go(x, x["stream"])
+    torch.cuda.synchronize()
+    for x, want in zip(batches, alone):
+        for t, w in zip((x["bounds"], x["sel"], *x["out"]), want):
+            assert torch.equal(t, w)
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "q8"])
 @pytest.mark.parametrize("captured", [False, True])
