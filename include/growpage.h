@@ -524,7 +524,7 @@ typedef struct {
  * chunks of them.
  *  - Request r brings n_r = tok_start[r + 1] - tok_start[r] tokens, rows
  *    tok_start[r] .. of k_new, v_new and q (tok_start [num_reqs + 1] int32 on
- *    the device, not decreasing, from 0 to num_tokens at most); with tok_start
+ *    the device, not decreasing, between 0 and num_tokens); with tok_start
  *    NULL every request brings one, row r (num_tokens == num_reqs, else
  *    GP_ERR_INVALID).
  *  - Row strides are in elements, so that q, k and v may lie side by side in

@@ -170,3 +170,10 @@ def test_binding_refusals():
         gp.gp_select_pages(bounds[:5], ps, q, 1, 1, i32(R, hkv, 4), codes)
     with pytest.raises(ValueError):
         gp.gp_decode_attention_pages_q8(kv8, ps, i32(R, hkv, 4).long(), q, 0.1, q, codes)
+    # what fits otherwise, but lies in host memory
+    for call in (lambda: gp.gp_append_rope_q8(kv8, ps, pos, new, new, 1e4), lambda: gp.gp_page_bounds_q8(kv8, ps, bounds),
+                 lambda: gp.gp_decode_attention_q8(kv8, ps, q, 0.1, q, codes),
+                 lambda: gp.gp_select_pages(bounds, ps, q, 1, 1, i32(R, hkv, 4), codes),
+                 lambda: gp.gp_decode_attention_pages_q8(kv8, ps, i32(R, hkv, 4), q, 0.1, q, codes)):
+        with pytest.raises(ValueError, match="device"):
+            call()

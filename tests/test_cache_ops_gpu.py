@@ -243,6 +243,33 @@ def test_append_rope_in_place(dtype):
     assert torch.equal(outs[0], outs[1])
 
 
+@pytest.mark.parametrize("cache", ["bf16", "q8"])
+def test_append_rope_starts(cache):
+    """Rows before the first request's and behind the last one's are nobody's: their queries are left as they
+    were.  Starts that decrease or leave the rows end the call without a write outside the requests' pages."""
+    _say(f"append starts {cache}")
+    reqs = [(0, 2, 9), (3, 3, 20), (0, 1, 4)]
+    s = _append_case(cache, reqs, 2, 2, 64, 17, False, 0, False)
+    fn = gp.gp_append_rope_q8 if cache == "q8" else gp.gp_append_rope
+    T = s["q"].shape[0]
+    pad = lambda t: torch.cat([t[:4], t, t[:7]]).contiguous()  # noqa: E731
+    q, k, v = pad(s["q"]), pad(s["k"]), pad(s["v"])
+    s["position_tensor"] = _i32(s["pos"])
+    q_out = torch.full_like(q, 7.0)
+    fn(s["kv"], s["ps"], s["position_tensor"], k, v, 1e4, q=q, q_out=q_out, tok_start=s["start"] + 4)
+    torch.cuda.synchronize()
+    assert bool((q_out[:4] == 7.0).all()) and bool((q_out[4 + T:] == 7.0).all())
+    _check_append(s, cache, reqs, 2, 2, 64, 1e4, q_out[4:4 + T], True)
+    owned = torch.zeros(s["pool"], dtype=torch.bool)
+    owned[s["table"][s["table"] >= 0].long()] = True
+    for starts in ([0, -5, 30, 10], [-2 ** 31, 2 ** 31 - 1, -7, 2 ** 31 - 1], [40, 3, 2, 1], [T + 100, T + 101, T + 102, T + 103]):
+        fn(s["kv"], s["ps"], s["position_tensor"], s["k"], s["v"], 1e4, q=s["q"], q_out=torch.empty_like(s["q"]),
+           tok_start=_i32(starts), advance=False)
+        torch.cuda.synchronize()
+        for t, t0 in zip(vars(s["kv"]).values(), s["before"]):
+            assert torch.equal(t.view(torch.uint8)[~owned.to(DEV)], t0.view(torch.uint8)[~owned.to(DEV)])
+
+
 def test_append_rope_bad_pages():
     """Page ids outside the pool and pages beyond the table write nothing."""
     _say("append bad pages")
