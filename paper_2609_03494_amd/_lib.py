@@ -452,6 +452,8 @@ def _append_rope(name, kv, dtype, ps, positions, k_new, v_new, rope_theta, q, q_
         q_ptr, qo_ptr, q_row = q.data_ptr(), _ptr(q_out), _row(q.stride(), T, Hq, d, name)
     if tok_start is not None and (tok_start.dtype != torch.int32 or tok_start.numel() != c_ps.num_reqs + 1):
         raise ValueError(f"{name}: tok_start [num_reqs + 1] int32")
+    if positions.dtype != torch.int32 or positions.numel() < c_ps.num_reqs:
+        raise ValueError(f"{name}: positions [num_reqs] int32")
     _on_device(name, kv.k, kv.v, ps.page_table, ps.seq_lens, positions, k_new, v_new, q, q_out, tok_start)
     st = getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(positions), _ptr(tok_start), T, q_ptr, q_row,
                                qo_ptr, k_new.data_ptr(), _row(k_new.stride(), T, shape[1], d, name), v_new.data_ptr(),
@@ -491,10 +493,17 @@ def _of(t: torch.Tensor, dtype, name: str) -> int:
     return _ptr(t)
 
 
+def _queries(name: str, q_post: torch.Tensor, out: torch.Tensor, R: int, d: int) -> None:
+    shape = q_post.shape
+    if len(shape) != 3 or shape[0] != R or shape[2] != d or out.shape != shape:
+        raise ValueError(f"{name}: q_post and out [{R}, heads, {d}]")
+
+
 def gp_decode_attention_q8(kv: KV8Layer, ps: PageState, q_post: torch.Tensor, scale: float, out: torch.Tensor,
                            ws: torch.Tensor, stream=None) -> None:
     """Decode attention over an 8-bit cache; q_post and out bfloat16."""
     c_kv, c_ps = kv.c(), ps.c()
+    _queries("gp_decode_attention_q8", q_post, out, c_ps.num_reqs, c_kv.head_dim)
     _on_device("gp_decode_attention_q8", kv.k, kv.v, kv.k_scale, kv.v_scale, ps.page_table, ps.seq_lens, q_post, out, ws)
     st = load().gp_decode_attention_q8(ctypes.byref(c_kv), ctypes.byref(c_ps), _of(q_post, torch.bfloat16, "q_post"),
                                        q_post.shape[1], scale, _of(out, torch.bfloat16, "out"), _ptr(ws), ws.numel(),
@@ -551,6 +560,7 @@ def gp_select_pages(bounds: torch.Tensor, ps: PageState, q_post: torch.Tensor, k
 def _decode_pages(name, kv, dtype, ps, selected, q_post, scale, out, ws, stream):
     c_kv, c_ps = kv.c(), ps.c()
     budget = _lists(selected, c_ps.num_reqs, c_kv.num_kv_heads)
+    _queries(name, q_post, out, c_ps.num_reqs, c_kv.head_dim)
     _on_device(name, kv.k, kv.v, ps.page_table, ps.seq_lens, selected, q_post, out, ws)
     _check(getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(selected), budget,
                                  _of(q_post, dtype, "q_post"), q_post.shape[1], scale, _of(out, dtype, "out"), _ptr(ws),

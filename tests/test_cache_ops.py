@@ -177,3 +177,27 @@ def test_binding_refusals():
                  lambda: gp.gp_decode_attention_pages_q8(kv8, ps, i32(R, hkv, 4), q, 0.1, q, codes)):
         with pytest.raises(ValueError, match="device"):
             call()
+
+
+def test_binding_refuses_short_queries_and_positions():
+    """Arguments with fewer rows than the page state has requests, which a kernel would read past."""
+    pool, hkv, d, R = 6, 2, 64, 3
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    ps = gp.PageState(i32(R, 4), i32(R), i32(R), i32(pool), i32(pool), i32(1))
+    codes, scale = torch.zeros(pool, hkv, 16, d, dtype=torch.uint8), torch.ones(pool, hkv)
+    kv8 = gp.KV8Layer(codes, codes.clone(), scale, scale.clone())
+    kv = gp.KVLayer(torch.zeros(pool, hkv, 16, d), torch.zeros(pool, hkv, 16, d))
+    new = torch.zeros(R, hkv, d, dtype=torch.bfloat16)
+    for positions in (i32(R - 1), torch.zeros(R, dtype=torch.int64)):
+        with pytest.raises(ValueError, match="positions"):
+            gp.gp_append_rope_q8(kv8, ps, positions, new, new, 1e4)
+        with pytest.raises(ValueError, match="positions"):
+            gp.gp_append_rope(kv, ps, positions, new.float(), new.float(), 1e4)
+    q, lists = torch.zeros(R, 2 * hkv, d, dtype=torch.bfloat16), i32(R, hkv, 4)
+    for x, out in ((q[:2], q), (q, q[:2]), (q[:2], q[:2]), (q[..., :32], q[..., :32]), (q, q[:, :2]), (q[0], q[0])):
+        with pytest.raises(ValueError, match="q_post and out"):
+            gp.gp_decode_attention_q8(kv8, ps, x, 0.1, out, codes)
+        with pytest.raises(ValueError, match="q_post and out"):
+            gp.gp_decode_attention_pages_q8(kv8, ps, lists, x, 0.1, out, codes)
+        with pytest.raises(ValueError, match="q_post and out"):
+            gp.gp_decode_attention_pages(kv, ps, lists, x.float(), 0.1, out.float(), codes)
