@@ -166,8 +166,9 @@ def _ptr(t: torch.Tensor | None) -> int | None:
 
 
 def _stream(stream) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    # (the current stream's handle alone: torch.cuda.current_stream() makes an object
+    # around it, 2.8 us of a call of 10-14)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
 
 
 def _dtype_code(t: torch.Tensor) -> int:
