@@ -504,7 +504,9 @@ gp_status_t gp_append_step(const gp_kv_layer_t *layers, int32_t n_layers, const 
  * mantissa bits, no infinities, 0x7f and 0xff are NaN) with one float32 scale
  * per page and KV head, so that element x of a page stands for x * scale.
  * Half the bytes of a bfloat16 cache per token and 8 more per page and head.
- * Scales are positive and finite; gp_append_rope_q8 makes powers of two.
+ * Scales are positive and at most 2^127; gp_append_rope_q8 makes powers of two
+ * from 2^-100 on.  (Values under a scale below that cost the output bits: the
+ * weights times the scale leave bfloat16's normal range.)
  * Queries, new rows and outputs of a call on such a cache are bfloat16.  Pools
  * lie at multiples of 16 bytes (GP_ERR_INVALID otherwise). */
 typedef struct {
@@ -573,8 +575,10 @@ gp_status_t gp_append_rope_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *p
 
 /* gp_decode_attention over an 8-bit cache (Sec. 3.1): the same arguments and
  * rules, q_post and out bfloat16.  The codes are used as the values they stand
- * for, without further rounding.  Takes the decode workspace of a bfloat16
- * cache of the shape. */
+ * for, without further rounding.  The scale is below 2^111 (GP_ERR_INVALID
+ * otherwise), and so is its product with a page's k_scale; either may be as
+ * small as it likes.  Takes the decode workspace of a bfloat16 cache of the
+ * shape. */
 gp_status_t gp_decode_attention_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps,
                                    const void *q_post, int32_t num_q_heads, float scale, void *out,
                                    void *ws, size_t ws_bytes, hipStream_t stream);

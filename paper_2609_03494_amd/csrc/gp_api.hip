@@ -175,7 +175,7 @@ gp_status_t decode_call(const gp_kv_layer_t *kv, const gp_page_state_t *ps, cons
     if (st != GP_OK) return st;
     if ((st = check_state(ps, kv)) != GP_OK) return st;
     if (!dims_ok(num_q_heads, kv->num_kv_heads, kv->head_dim)) return GP_ERR_UNSUPPORTED;
-    if (!(scale > 0.0f) || !isfinite(scale)) return GP_ERR_INVALID;
+    if (!(scale > 0.0f) || !isfinite(scale) || (kv8 && scale >= 0x1p111f)) return GP_ERR_INVALID;
     if (sum) {
         if (sum->num_slots <= 0) return GP_ERR_INVALID;
         if (!(sum->beta_s >= 0.0f && sum->beta_s <= 1.0f && sum->beta_l >= 0.0f && sum->beta_l <= 1.0f))
@@ -263,7 +263,7 @@ gp_status_t decode_call(const gp_kv_layer_t *kv, const gp_page_state_t *ps, cons
     a.min_run = kDecodeMinRun;
     a.slots = w.slots;
     a.pslots = w.pslots;
-    a.qscale = scale * 1.4426950408889634f;
+    a.qscale = scale * 1.4426950408889634f * (kv8 ? kQ8KeyScale : 1.0f);
     if (kv->dtype == GP_F32) {
         const double q = (double)scale * 1.4426950408889634;
         a.qscale = (float)q;

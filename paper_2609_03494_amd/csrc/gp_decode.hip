@@ -30,6 +30,7 @@
 // 2 * d * sizeof(elem) (K and V), plus the page-table entries, q and out.  A
 // copy of the kernel's loads without arithmetic (equal runs, 4 KiB head slices
 // of randomly placed pages) reads 6.5-6.9 TB/s; a plain streaming read 7.04.
+#include <float.h>
 #include <limits.h>
 
 #include "gp_internal.h"
@@ -684,16 +685,19 @@ struct Page<E4m3, D, false> {
         const int R = 8 * (kg & 1) + n / 2;
         return (kg >> 1) * HALF + (R * UPR + swizzle(R)) * 16 + (n & 1) * 8;
     }
+    // Keys are widened to 2^-16 of their codes, exactly: 448 d products of the largest
+    // queries then stay below 2^128.  The call's scale has the other factor.
+    static constexpr float kKeyUnit = 1.0f / kQ8KeyScale;
     // Q of the lane's head: operand 2 j + s is half s of key unit kg + 4 j
     static constexpr int QREGS = KK;
     __device__ static inline int qdim(int j, int n, int kg) { return 16 * (kg + 4 * (j / 2)) + 8 * (j % 2); }
-    __device__ static inline bf16x8_t widen(const u32x2_t &x) {
+    __device__ static inline bf16x8_t widen(const u32x2_t &x, float scale) {
         typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
         bf16x8_t y;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const bf16x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], 1.0f, false);
-            const bf16x2_t hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], 1.0f, true);
+            const bf16x2_t lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], scale, false);
+            const bf16x2_t hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], scale, true);
             y[4 * i] = lo[0];
             y[4 * i + 1] = lo[1];
             y[4 * i + 2] = hi[0];
@@ -715,7 +719,7 @@ struct Page<E4m3, D, false> {
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
-                    st[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(u32x2_t{x[c][j][2 * s], x[c][j][2 * s + 1]}),
+                    st[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(u32x2_t{x[c][j][2 * s], x[c][j][2 * s + 1]}, kKeyUnit),
                                                                     __builtin_bit_cast(bf16x8_t, q[2 * j + s]), st[c], 0, 0, 0);
     }
     static constexpr int VREGS = DT;
@@ -761,7 +765,7 @@ struct Page<E4m3, D, false> {
             bf16x8_t v[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                v[t] = widen(vx[t0 + t]);
+                v[t] = widen(vx[t0 + t], 1.0f);
                 ot[t0 + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[t], bhi, ot[t0 + t], 0, 0, 0);
             }
 #pragma unroll
@@ -1258,7 +1262,11 @@ decode_kernel(DecodeArgs a) {
             // online softmax of the lane's head over tokens token0 + e of both pages.  The
             // scales are positive, so the greatest product is the greatest score's; the
             // distance to the maximum is rounded once.
-            const float qs[2] = {a.qscale * __uint_as_float(ks[0]), a.qscale * __uint_as_float(ks[1])};
+            // A product that rounds to zero (a page of zero keys has the scale 2^-100) would make
+            // a NaN of a masked score, an infinite one of a score of zero: held to the positive
+            // finite numbers.  2^-149 in the place of less moves no score by more than 2^-21.
+            const float qs[2] = {__builtin_amdgcn_fmed3f(a.qscale * __uint_as_float(ks[0]), FLT_TRUE_MIN, FLT_MAX),
+                                 __builtin_amdgcn_fmed3f(a.qscale * __uint_as_float(ks[1]), FLT_TRUE_MIN, FLT_MAX)};
             if (x.n0 + x.n1 < 2 * kPage) {
                 const int t0 = Pg::token0(kg);
 #pragma unroll

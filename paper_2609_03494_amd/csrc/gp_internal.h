@@ -36,6 +36,7 @@ constexpr int kWideMerge = GP_WIDE_MERGE; // (KV head, request) pairs below whic
 constexpr int kPrefixSlotPages = 64;      // pages of one partial slot of a shared prefix, about
 constexpr int kMaxPrefixSlotPages = 128;  // and at most (LDS id table)
 constexpr int kMaxDecodePages = 8192;     // table width the decode calls accept
+constexpr float kQ8KeyScale = 65536.0f;   // codes of 8-bit keys in units of their bfloat16 operands (see Page<E4m3>)
 constexpr int kMaxRopeTokens = 1 << 27;   // tokens one gp_append_rope call takes, and
 constexpr int kMaxListedHeads = 8192;     // KV heads it, the page bounds and the selection take: grids below 2^32 threads
 constexpr size_t kScratchBytes = size_t(8) << 20;   // static scratch of gp_decode_attention_noalloc
@@ -265,7 +266,7 @@ struct DecodeArgs {
     int g_first[kMaxPrefixGroups], g_num[kMaxPrefixGroups], g_pages[kMaxPrefixGroups];
     int g_blk0[kMaxPrefixGroups + 1], g_slots[kMaxPrefixGroups];
     int R, Hkv, max_pages, pool_pages, W, W1, min_run, slots, pslots;   // W1: workgroups per KV head that fit at once
-    float qscale;      // scale * log2(e); float32 caches: rounded down, and the rest of it
+    float qscale;      // scale * log2(e); float32 caches: rounded down, and the rest of it; 8-bit: times kQ8KeyScale
     float qscale_lo;   // (> 0, so that an infinite score times it keeps its sign)
     const float *k_scale, *v_scale;   // 8-bit pools: [pool_pages][Hkv]
     const int32_t *list;              // listed pages: [R][Hkv][list_width] logical page indices (nullptr: all pages)

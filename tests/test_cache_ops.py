@@ -201,3 +201,11 @@ def test_binding_refuses_short_queries_and_positions():
             gp.gp_decode_attention_pages_q8(kv8, ps, lists, x, 0.1, out, codes)
         with pytest.raises(ValueError, match="q_post and out"):
             gp.gp_decode_attention_pages(kv, ps, lists, x.float(), 0.1, out.float(), codes)
+
+
+def test_q8_scale_limit(lib):
+    """The 8-bit calls take softmax scales below 2^111 only; the others any."""
+    for scale, want in ((2.0 ** 111, INVALID), (3.0e38, INVALID), (2.0 ** 110, WORKSPACE)):
+        assert lib.gp_decode_attention_q8(_kv8(), _ps(), FAKE, 32, scale, FAKE, FAKE, 0, None) == want
+        assert lib.gp_decode_attention_pages_q8(_kv8(), _ps(), FAKE, 8, FAKE, 32, scale, FAKE, FAKE, 0, None) == want
+        assert lib.gp_decode_attention_pages(_kv(), _ps(), FAKE, 8, FAKE, 32, scale, FAKE, FAKE, 0, None) == WORKSPACE

@@ -997,3 +997,37 @@ def test_a_run_of_them(kind, captured):
                 want, size_, size = _attention(_tokens(k64, table, r, m)[h:h + 1, tok], _tokens(v64, table, r, m)[h:h + 1, tok],
                                                q[r, g].double(), scale)
                 assert bool(((got[r, g] - want).abs() <= _attention_tol(want, size_, size, d, dt)).all()), (i, r, h)
+
+
+# ----------------------------------------------------- factors at the range's ends --
+
+@pytest.mark.parametrize("spare", [2, 130])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (3, 3, 64)])
+def test_decode_q8_scale_products(hq, hkv, d, spare):
+    """Page scales and softmax scales whose product rounds to zero or past the largest float, on pages that are
+    not full: the weights are those of the scores all the same.  The product of less than 2^-149 may stand for
+    2^-149, which moves a score of up to 2^128 by 2^-21 and its weight by as much: within the 2^-17."""
+    _say(f"decode q8 scale products heads {hq}/{hkv} d {d} spare {spare}")
+    gen = torch.Generator().manual_seed(hq + spare)
+    lens = [5, 21, 40, 16, 1]
+    npages = [-(-m // 16) for m in lens]
+    width = max(npages) + spare
+    R = len(lens)
+    kv, pool, table = _q8_cache(lens, npages, hkv, d, gen, width)
+    ps = _state(table, npages, lens, pool)
+    plain = torch.randn(R, hq, d, generator=gen).to(BF16)
+    sel = torch.arange(width, dtype=torch.int32).expand(R, hkv, width).contiguous().to(DEV)
+    ws = gp.workspace(gp.GP_OP_DECODE, R, 0, hq, hkv, d, width, BF16)
+    zero_keys = (kv.k.to(torch.int32) * 0).to(torch.uint8)
+    for keys, k_scale, scale, q in ((zero_keys, 2.0 ** -100, 1e-16, plain), (kv.k, 2.0 ** -149, 0.125, plain),
+                                    (kv.k, 2.0 ** -115, 2.0 ** -40, plain * 2.0 ** 115), (kv.k, 2.0 ** 119, 2.0 ** 20, plain * 0.0)):
+        layer = gp.KV8Layer(keys, kv.v, torch.full_like(kv.k_scale, k_scale), kv.v_scale)
+        outs = [torch.full((R, hq, d), NAN, dtype=BF16, device=DEV) for _ in range(2)]
+        gp.gp_decode_attention_q8(layer, ps, q.to(DEV), scale, outs[0], ws)
+        gp.gp_decode_attention_pages_q8(layer, ps, sel, q.to(DEV), scale, outs[1], ws)
+        torch.cuda.synchronize()
+        k64, v64 = _values(layer.k, layer.k_scale), _values(layer.v, layer.v_scale)
+        for r, m in enumerate(lens):
+            want, mag, size = _attention(_tokens(k64, table, r, m), _tokens(v64, table, r, m), q[r].double(), scale)
+            for out in outs:
+                assert bool(((out[r].cpu().double() - want).abs() <= _attention_tol(want, mag, size, d, BF16)).all()), (k_scale, scale, r)
