@@ -427,7 +427,7 @@ __global__ __launch_bounds__(NT) void select_kernel(SelectArgs a) {
         return (int)fminf(fmaxf((0.5f * s - 0.5f * least) * (2.0f * scale), 0.0f), (float)(kBins - 1));
     };
     auto key_of = [&](float s) {
-        const uint32_t u = __float_as_uint(s);
+        const uint32_t u = __float_as_uint(s + 0.0f);     // (-0, what a small negative sum rounds to, ties with 0)
         return s != s ? 0xffffffffu : u ^ ((int)u < 0 ? 0xffffffffu : 0x80000000u);
     };
     int bin[C];

@@ -1031,3 +1031,25 @@ def test_decode_q8_scale_products(hq, hkv, d, spare):
             want, mag, size = _attention(_tokens(k64, table, r, m), _tokens(v64, table, r, m), q[r].double(), scale)
             for out in outs:
                 assert bool(((out[r].cpu().double() - want).abs() <= _attention_tol(want, mag, size, d, BF16)).all()), (k_scale, scale, r)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,width,budget", [(40, 40, 12), (700, 700, 200), (3000, 3100, 900)])
+def test_select_signed_zero(dtype, n, width, budget):
+    """Sums so small that they round to -0: as good as the pages whose sum is 0, the lowest of all first."""
+    _say(f"select signed zero {dtype} {n} of {width} budget {budget}")
+    hq, hkv, d = 2, 1, 64
+    gen = torch.Generator().manual_seed(n)
+    pool, table = _paged([n] * 2, width, gen)
+    bounds = torch.zeros(pool, hkv, 2, d, dtype=dtype)
+    bounds[table[0, 1:n:3].long(), :, :, 7] = 2.0 ** -120                # times -2^-120: -2^-240
+    bounds[table[1, :n // 2].long(), :, :, 7] = 2.0 ** -120
+    bounds[table[1, 3].long()] = 1.0
+    q = torch.zeros(2, hq, d, dtype=dtype)
+    q[:, 0, 7] = -(2.0 ** -120)
+    sel = torch.empty(2, hkv, budget, dtype=torch.int32, device=DEV)
+    ws = gp.workspace(gp.GP_OP_SELECT, 2, 0, hq, hkv, d, width, dtype)
+    gp.gp_select_pages(bounds.to(DEV), _state(table, [n] * 2, [16 * n] * 2, pool), q.to(DEV), 1, 1, sel, ws)
+    torch.cuda.synchronize()
+    for r in range(2):
+        assert torch.equal(sel[r].cpu(), _select64(bounds, table, n, q, hkv, budget, 1, 1, r)), r
