@@ -557,9 +557,11 @@ typedef struct {
  * gp_append_rope_q8: rows are bfloat16, the pools 8-bit.  A page's scale of a
  * KV head is the least power of two s = 2^e, e >= -100, with |x| <= 448 s for
  * every finite value the call brings to the page, and no less than the scale
- * that the page had if it held tokens before; where it grows, the codes of the
- * older tokens are rounded again, to nearest even (exact unless one falls
- * below the format's normal range).  Codes are x / s rounded to nearest even;
+ * that the page had if it held tokens before (so that another's scale that is
+ * no power of two gives way to the next one).  Where it grows, the codes of the
+ * older tokens are rounded again, once, to nearest even (from a power of two:
+ * exact unless one falls below the format's normal range).  Codes are x / s
+ * rounded to nearest even;
  * infinities and NaN become NaN.  The keys are rounded from their float32
  * rotation. */
 gp_status_t gp_append_rope(const gp_kv_layer_t *kv, const gp_page_state_t *ps, int32_t *positions,

@@ -1053,3 +1053,50 @@ def test_select_signed_zero(dtype, n, width, budget):
     torch.cuda.synchronize()
     for r in range(2):
         assert torch.equal(sel[r].cpu(), _select64(bounds, table, n, q, hkv, budget, 1, 1, r)), r
+
+
+def _e4m3(x):
+    """float64, |x| <= 448: the nearest e4m3 value, ties to even."""
+    step = torch.exp2((torch.frexp(x)[1].double() - 4).clamp_min(-9))
+    return (x / step).round() * step
+
+
+@pytest.mark.parametrize("hkv,d", [(2, 128), (1, 64)])
+@pytest.mark.parametrize("size", [2.0 ** -6, 300.0])
+def test_append_rope_q8_other_scales(hkv, d, size):
+    """Pages that hold tokens under scales that are no powers of two, among them scales next to those that bring
+    an older code to a tie: the new scale is a power of two, the older codes are rounded once from their
+    products' exact values, the new ones from theirs."""
+    _say(f"append q8 other scales heads {hkv} d {d} size {size}")
+    gen = torch.Generator().manual_seed(d)
+    old = [1.0 / 3, 0.7, 1.5, 448.0 / 447, 0.5, 2.0 ** -100, 1.5 * 2.0 ** -120, 3e-42, 3.0 * 2.0 ** 30, 1.9 * 2.0 ** 126]
+    for x in range(9, 16):                                # x old is a tie between two codes, but for old's own rounding
+        for t in range(17, 32, 2):
+            f = torch.tensor(t / (2 * x), dtype=F32)
+            old += [float(torch.nextafter(f, f * k)) for k in (0, 1, 2) if 0.5 < f < 1]
+    R, m = len(old), 7
+    npages = [1] * R
+    pool, table = _paged(npages, 1, gen)
+    ps = _state(table, npages, [m] * R, pool)
+    codes = torch.randint(0, 256, (2, pool, hkv, 16, d), generator=gen).to(torch.uint8)
+    scale = torch.full((pool, hkv), 1.0)
+    scale[table[:, 0].long()] = torch.tensor(old, dtype=F32)[:, None].expand(-1, hkv)
+    kv = gp.KV8Layer(codes[0].to(DEV), codes[1].to(DEV), scale.to(DEV), scale.clone().to(DEV))
+    new = (torch.randn(2, R, hkv, d, generator=gen) * size).to(BF16)
+    gp.gp_append_rope_q8(kv, ps, _i32([-1] * R), new[0].to(DEV), new[1].to(DEV), 1e4)       # position 0: no turn
+    torch.cuda.synchronize()
+    ids = table[:, 0].long()
+    for which, got_codes, got_scale in ((0, kv.k, kv.k_scale), (1, kv.v, kv.v_scale)):
+        x, s0 = new[which].double(), scale.double()[ids]
+        least = (torch.frexp(x.abs().amax(-1) / 448)[1] - (torch.frexp(x.abs().amax(-1) / 448)[0] == 0.5).int()).clamp_min(-100)
+        kept = torch.frexp(s0)[1] - (torch.frexp(s0)[0] == 0.5).int()
+        s = torch.exp2(torch.maximum(least, kept).double())
+        assert torch.equal(got_scale.cpu().double()[ids], s)
+        got = got_codes.cpu().view(torch.float8_e4m3fn).double()[ids]
+        older = codes[which].view(torch.float8_e4m3fn).double()[ids][:, :, :m]
+        want = _e4m3(older * (s0 / s)[..., None, None])
+        assert torch.equal(got[:, :, :m].isnan(), older.isnan())
+        wrong = (got[:, :, :m] != want) & ~older.isnan()
+        assert not bool(wrong.any()), (int(wrong.sum()), old[int(wrong.nonzero()[0, 0])])
+        assert torch.equal(got[:, :, m], _e4m3(x / s[..., None]))
+        assert torch.equal(got_codes.cpu()[ids][:, :, m + 1:], codes[which][ids][:, :, m + 1:])
