@@ -429,10 +429,11 @@ def gp_append_step(layers: list[KVLayer], ps: PageState, positions: torch.Tensor
     _check(st, "gp_append_step")
 
 
-def _on_device(name: str, *tensors) -> None:
-    """The calls below run on the current device; their tensors lie there."""
-    dev = tensors[0].get_device()
-    for t in tensors:
+def _on_device(name: str, kv: KVLayer | KV8Layer | None, ps: PageState, *tensors) -> None:
+    """The calls below run on the current device; all tensors that their kernels read or write lie there."""
+    dev = ps.page_table.get_device()
+    layer = () if kv is None else (kv.k, kv.v, kv.k_scale, kv.v_scale) if isinstance(kv, KV8Layer) else (kv.k, kv.v)
+    for t in (ps.num_pages, ps.seq_lens, *layer, *tensors):
         if t is not None and t.get_device() != dev:
             raise ValueError(f"{name}: tensors on different devices")
     if dev < 0 or dev != torch.cuda.current_device():
@@ -455,7 +456,7 @@ def _append_rope(name, kv, dtype, ps, positions, k_new, v_new, rope_theta, q, q_
         raise ValueError(f"{name}: tok_start [num_reqs + 1] int32")
     if positions.dtype != torch.int32 or positions.numel() < c_ps.num_reqs:
         raise ValueError(f"{name}: positions [num_reqs] int32")
-    _on_device(name, kv.k, kv.v, ps.page_table, ps.seq_lens, positions, k_new, v_new, q, q_out, tok_start)
+    _on_device(name, kv, ps, positions, k_new, v_new, q, q_out, tok_start)
     st = getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(positions), _ptr(tok_start), T, q_ptr, q_row,
                                qo_ptr, k_new.data_ptr(), _row(k_new.stride(), T, shape[1], d, name), v_new.data_ptr(),
                                _row(v_new.stride(), T, shape[1], d, name), Hq, rope_theta, bool(advance), _stream(stream))
@@ -505,7 +506,7 @@ def gp_decode_attention_q8(kv: KV8Layer, ps: PageState, q_post: torch.Tensor, sc
     """Decode attention over an 8-bit cache; q_post and out bfloat16."""
     c_kv, c_ps = kv.c(), ps.c()
     _queries("gp_decode_attention_q8", q_post, out, c_ps.num_reqs, c_kv.head_dim)
-    _on_device("gp_decode_attention_q8", kv.k, kv.v, kv.k_scale, kv.v_scale, ps.page_table, ps.seq_lens, q_post, out, ws)
+    _on_device("gp_decode_attention_q8", kv, ps, q_post, out, ws)
     st = load().gp_decode_attention_q8(ctypes.byref(c_kv), ctypes.byref(c_ps), _of(q_post, torch.bfloat16, "q_post"),
                                        q_post.shape[1], scale, _of(out, torch.bfloat16, "out"), _ptr(ws), ws.numel(),
                                        _stream(stream))
@@ -518,7 +519,7 @@ def _page_bounds(name, kv, dtype, ps, bounds, from_tokens, max_update, stream):
         raise ValueError(f"{name}: bounds [pool_pages, num_kv_heads, 2, head_dim], {dtype}")
     if from_tokens is not None and (from_tokens.dtype != torch.int32 or from_tokens.numel() != c_ps.num_reqs):
         raise ValueError(f"{name}: from_tokens [num_reqs] int32")
-    _on_device(name, kv.k, ps.page_table, ps.seq_lens, bounds, from_tokens)
+    _on_device(name, kv, ps, bounds, from_tokens)
     _check(getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(from_tokens), max_update, _ptr(bounds),
                                  _stream(stream)), name)
 
@@ -551,7 +552,7 @@ def gp_select_pages(bounds: torch.Tensor, ps: PageState, q_post: torch.Tensor, k
     budget = _lists(selected, R, hkv)
     if pool != c_ps.pool_pages or R != c_ps.num_reqs or dq != d or two != 2:
         raise ValueError("gp_select_pages: bounds [pool_pages, Hkv, 2, d] and q_post [R, Hq, d] of the page state")
-    _on_device("gp_select_pages", bounds, ps.page_table, ps.seq_lens, q_post, selected, ws)
+    _on_device("gp_select_pages", None, ps, bounds, q_post, selected, ws)
     st = load().gp_select_pages(_ptr(bounds), _dtype_code(bounds), ctypes.byref(c_ps),
                                 _of(q_post, bounds.dtype, "q_post"), Hq, hkv, d, budget, keep_first, keep_last,
                                 _ptr(selected), _ptr(ws), ws.numel(), _stream(stream))
@@ -562,7 +563,7 @@ def _decode_pages(name, kv, dtype, ps, selected, q_post, scale, out, ws, stream)
     c_kv, c_ps = kv.c(), ps.c()
     budget = _lists(selected, c_ps.num_reqs, c_kv.num_kv_heads)
     _queries(name, q_post, out, c_ps.num_reqs, c_kv.head_dim)
-    _on_device(name, kv.k, kv.v, ps.page_table, ps.seq_lens, selected, q_post, out, ws)
+    _on_device(name, kv, ps, selected, q_post, out, ws)
     _check(getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(selected), budget,
                                  _of(q_post, dtype, "q_post"), q_post.shape[1], scale, _of(out, dtype, "out"), _ptr(ws),
                                  ws.numel(), _stream(stream)), name)

@@ -209,3 +209,74 @@ def test_q8_scale_limit(lib):
         assert lib.gp_decode_attention_q8(_kv8(), _ps(), FAKE, 32, scale, FAKE, FAKE, 0, None) == want
         assert lib.gp_decode_attention_pages_q8(_kv8(), _ps(), FAKE, 8, FAKE, 32, scale, FAKE, FAKE, 0, None) == want
         assert lib.gp_decode_attention_pages(_kv(), _ps(), FAKE, 8, FAKE, 32, scale, FAKE, FAKE, 0, None) == WORKSPACE
+
+
+class _NoLaunch:
+    """The library's place: counts calls, launches nothing."""
+    def __init__(self):
+        self.calls = 0
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls += 1
+            return 0
+        return call
+
+
+def _device_calls():
+    """Each call of the binding around the cache, with every tensor that its kernels reach, by name."""
+    pool, hkv, d, R = 6, 2, 64, 3
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8)  # noqa: E731
+    state = lambda: gp.PageState(i32(R, 4), i32(R), i32(R), i32(pool), i32(pool), i32(1))  # noqa: E731
+    layers = {"": lambda: gp.KVLayer(bf(pool, hkv, 16, d), bf(pool, hkv, 16, d)),
+              "_q8": lambda: gp.KV8Layer(u8(pool, hkv, 16, d), u8(pool, hkv, 16, d), torch.ones(pool, hkv), torch.ones(pool, hkv))}
+    of_state = lambda ps: dict(page_table=ps.page_table, num_pages=ps.num_pages, seq_lens=ps.seq_lens)  # noqa: E731
+    for q8, layer in layers.items():
+        kv, ps, t = layer(), state(), dict(positions=i32(R), k_new=bf(R, hkv, d), v_new=bf(R, hkv, d), q=bf(R, hkv, d),
+                                           q_out=bf(R, hkv, d), tok_start=i32(R + 1))
+        yield f"gp_append_rope{q8}", {**vars(kv), **of_state(ps), **t}, lambda fn, kv=kv, ps=ps, t=t: fn(
+            kv, ps, t["positions"], t["k_new"], t["v_new"], 1e4, q=t["q"], q_out=t["q_out"], tok_start=t["tok_start"])
+        kv, ps, t = layer(), state(), dict(bounds=bf(pool, hkv, 2, d), from_tokens=i32(R))
+        yield f"gp_page_bounds{q8}", {**vars(kv), **of_state(ps), **t}, lambda fn, kv=kv, ps=ps, t=t: fn(
+            kv, ps, t["bounds"], from_tokens=t["from_tokens"])
+        kv, ps, t = layer(), state(), dict(selected=i32(R, hkv, 4), q=bf(R, hkv, d), out=bf(R, hkv, d), ws=u8(64))
+        yield f"gp_decode_attention_pages{q8}", {**vars(kv), **of_state(ps), **t}, lambda fn, kv=kv, ps=ps, t=t: fn(
+            kv, ps, t["selected"], t["q"], 0.1, t["out"], t["ws"])
+    kv, ps, t = layers["_q8"](), state(), dict(q=bf(R, hkv, d), out=bf(R, hkv, d), ws=u8(64))
+    yield "gp_decode_attention_q8", {**vars(kv), **of_state(ps), **t}, lambda fn, kv=kv, ps=ps, t=t: fn(
+        kv, ps, t["q"], 0.1, t["out"], t["ws"])
+    ps, t = state(), dict(bounds=bf(pool, hkv, 2, d), q=bf(R, hkv, d), selected=i32(R, hkv, 4), ws=u8(64))
+    yield "gp_select_pages", {**of_state(ps), **t}, lambda fn, ps=ps, t=t: fn(
+        t["bounds"], ps, t["q"], 1, 1, t["selected"], t["ws"])
+
+
+def test_binding_checks_the_device_of_every_tensor(monkeypatch):
+    """Host tensors that say they lie on device 0: the call goes through.  One of them at a time on the host or on
+    another device, whichever it is: the call is refused and the library not reached."""
+    lib = _NoLaunch()
+    monkeypatch.setattr(_lib, "load", lambda: lib)
+    monkeypatch.setattr(_lib, "_stream", lambda stream: 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    seen = 0
+    for name, tensors, call in _device_calls():
+        fn = getattr(gp, name)
+        for t in tensors.values():
+            t.get_device = lambda: 0
+        lib.calls = 0
+        call(fn)
+        assert lib.calls == 1, name
+        for what, t in tensors.items():
+            for dev in (-1, 1):
+                t.get_device = lambda dev=dev: dev
+                with pytest.raises(ValueError, match="device"):
+                    call(fn)
+                assert lib.calls == 1, (name, what)
+                seen += 1
+            t.get_device = lambda: 0
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)      # all on a device that is not the current one
+        with pytest.raises(ValueError, match="current device"):
+            call(fn)
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    assert seen == 2 * 77                                 # tensors of the eight calls
