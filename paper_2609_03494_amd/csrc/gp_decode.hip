@@ -2039,17 +2039,26 @@ hipError_t launch_g(int G, const DecodeArgs &a, int stages, hipStream_t s) {
 // Attention over an 8-bit pool, over listed pages, or both: no token, no prefix.
 template <typename T, int D, int MODE>
 hipError_t launch_read(int G, const DecodeArgs &a, hipStream_t s) {
+    static_assert(sizeof(T) == 1 || MODE == 3, "whole caches of other types have launch_g");
     using E = typename Elem<T>::type;
     const dim3 grid(a.Hkv, a.W), mgrid(a.Hkv, a.R);
     constexpr int NW = waves_of<T, D>(), NT = 64 * NW;
     constexpr int NN = page_bytes_of<T, D>() <= 2048 ? 4 : NW;
-    // the rules were measured on requests of half to all of the table's width; lists are as
-    // long as they are wide, so equal runs and their merge cost a third more there, a
-    // workgroup per request the same (16 lists of 200 pages, 8 KV heads, 8 bits, d 64: 23.5 us
-    // and 20.0)
-    const int pages = MODE == 3 ? cdiv(3 * a.list_width, 4) : a.max_pages, columns = sizeof(T) == 1 ? cdiv(pages, 2) : pages;
-    const bool own = sizeof(T) == 1 ? decode_own_pairs(cdiv(columns, NW), a.R, a.Hkv)
-                                    : decode_own(columns, a.R, a.Hkv, page_bytes_of<T, D>(), NW, quad_heads<T>(G));
+    // A workgroup per request and head, or equal runs and their merge.  8-bit: the rule was
+    // measured on requests of half to all of the table's width, lists are as long as they are
+    // wide, so their width counts three quarters (us a call, own workgroups and equal runs: 16
+    // lists of 200 pages, 8 KV heads, d 64: 19.0 and 20.1, d 128 24.9 and 27.1; of 250 29.4 and
+    // 30.2; 24 of 250 34.7 and 41.4; 8 of 125 16.4 and 15.1).  Of 888 batches (1-128 lists of
+    // 16-400 pages, full or of any length, 4 and 8 KV heads) the call is 0.6 % above the faster
+    // of both on average, bfloat16 1.8 %, with its rule on the whole width.  float32: see
+    // decode_own_f32_lists.
+    bool own;
+    if constexpr (sizeof(T) == 1)
+        own = decode_own_pairs(cdiv(cdiv(MODE == 3 ? cdiv(3 * a.list_width, 4) : a.max_pages, 2), NW), a.R, a.Hkv);
+    else if constexpr (sizeof(T) == 2)
+        own = decode_own(a.list_width, a.R, a.Hkv, page_bytes_of<T, D>(), NW, quad_heads<T>(G));
+    else
+        own = decode_own_f32_lists(cdiv(a.list_width, NW), a.R, a.Hkv);
     const bool narrow = own && decode_own_narrow(a.R, a.Hkv), wide = (int64_t)a.Hkv * a.R < kWideMerge;
     switch (G) {
 #define GP_CASE(GG)                                                                \

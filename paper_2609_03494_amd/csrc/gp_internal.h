@@ -98,6 +98,16 @@ __host__ __device__ inline bool decode_own_pairs(int per, int R, int Hkv) {
     return per <= (pairs >= 448 ? 16 : pairs >= 128 ? 12 : 7);
 }
 
+// ... for lists of float32 pages (per: pages per wave), whose products take a wave longer:
+// up to six in any batch, up to ten with pairs for three quarters of the CUs (us a call, own
+// workgroups and equal runs: one list of 48 pages, 64/8 heads, d 128, twelve per wave: 34.5
+// and 15.8, of 24 19.6 and 22.7; one of 56, 32/8, d 64, seven: 12.1 and 11.5, of 48 11.0 and
+// 14.0; 24 of 80, 23.2 and 28.0).  Of 888 batches 1.2 % above the faster of both on average;
+// with the rule for whole caches 2.3 %, on three quarters of the width 4.8 %.
+__host__ __device__ inline bool decode_own_f32_lists(int per, int R, int Hkv) {
+    return per <= ((int64_t)R * Hkv >= 192 ? 10 : 6);
+}
+
 struct DecodeWs {
     size_t partial, lens, prefix, total;
     size_t plain;                 // bytes a call without a shared prefix touches
