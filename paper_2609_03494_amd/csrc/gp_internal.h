@@ -413,4 +413,13 @@ __device__ inline uint16_t f32_to_bf16(float f) {
     return (uint16_t)(u >> 16);
 }
 
+// x f (x an 8-bit code) with its last bit set where it is not exact: rounded to fewer bits
+// then, it goes where the exact product would, also next to a tie.
+__device__ inline float odd_product(float x, float f) {
+    const float v = x * f, rest = fmaf(x, f, -v);
+    if (rest == 0.0f || v == 0.0f) return v;
+    const uint32_t u = __float_as_uint(v);
+    return __uint_as_float(((rest < 0.0f) != (v < 0.0f) ? u - 1 : u) | 1);
+}
+
 }  // namespace gp

@@ -136,14 +136,6 @@ __device__ inline float power_from(float old) {
     const uint32_t u = __float_as_uint(old);
     return __uint_as_float(u & 0x7fffff ? min((u & 0x7f800000u) + 0x800000u, 0x7f000000u) : u);
 }
-// x f with its last bit set where it is not exact: rounded to fewer bits then, it goes where
-// the exact product would, also next to a tie.  (Below 2^-12 the code is zero.)
-__device__ inline float times(float x, float f) {
-    const float v = x * f, rest = fmaf(x, f, -v);
-    if (rest == 0.0f || !(fabsf(v) >= 0x1p-12f)) return v;
-    const uint32_t u = __float_as_uint(v);
-    return __uint_as_float(((rest < 0.0f) != (v < 0.0f) ? u - 1 : u) | 1);
-}
 __device__ inline uint32_t codes(float a, float b, float c, float d) {
     int u = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);              // round to nearest even
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, u, true);
@@ -288,7 +280,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                             uint32_t *w = reinterpret_cast<uint32_t *>(page + half * H + c);
                             const uint32_t u = *w;
                             const auto x0 = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), x1 = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
-                            *w = codes(times(x0[0], f), times(x0[1], f), times(x1[0], f), times(x1[1], f));
+                            *w = codes(odd_product(x0[0], f), odd_product(x0[1], f), odd_product(x1[0], f), odd_product(x1[1], f));
                         }
                 }
             }

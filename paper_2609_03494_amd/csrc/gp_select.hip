@@ -99,10 +99,10 @@ __global__ __launch_bounds__(64 * kBoundWaves) void bounds_kernel(BoundsArgs a) 
         if (pid < 0 || pid >= a.pool_pages) continue;
         const int ntok = min(kPage, m - p * kPage);
         const size_t slice = (size_t)pid * a.Hkv + h;
-        float x[RPL][EU];
+        float x[RPL][EU], scale = 1.0f;               // (8 bits: codes; the scale is positive and meets the bounds)
         if constexpr (CACHE == 1) {
             const uint8_t *src = reinterpret_cast<const uint8_t *>(a.k) + slice * kPage * D + u * EU;
-            const float scale = a.k_scale[slice];
+            scale = a.k_scale[slice];
             u32x2_t w[RPL];
 #pragma unroll
             for (int i = 0; i < RPL; ++i) w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t *>(src + (i * RG + g) * D));
@@ -111,10 +111,10 @@ __global__ __launch_bounds__(64 * kBoundWaves) void bounds_kernel(BoundsArgs a) 
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const auto y0 = __builtin_amdgcn_cvt_pk_f32_fp8(w[i][c], false), y1 = __builtin_amdgcn_cvt_pk_f32_fp8(w[i][c], true);
-                    x[i][4 * c] = y0[0] * scale;
-                    x[i][4 * c + 1] = y0[1] * scale;
-                    x[i][4 * c + 2] = y1[0] * scale;
-                    x[i][4 * c + 3] = y1[1] * scale;
+                    x[i][4 * c] = y0[0];
+                    x[i][4 * c + 1] = y0[1];
+                    x[i][4 * c + 2] = y1[0];
+                    x[i][4 * c + 3] = y1[1];
                 }
         } else {
             const E *src = reinterpret_cast<const E *>(a.k) + slice * kPage * D + u * EU;
@@ -148,6 +148,10 @@ __global__ __launch_bounds__(64 * kBoundWaves) void bounds_kernel(BoundsArgs a) 
                 lo[e] = fold8(lo[e], least);
                 hi[e] = fold8(hi[e], greatest);
             }
+        }
+        if constexpr (CACHE == 1) {                   // (the lanes that write them: g = 0 the least, 1 the greatest)
+#pragma unroll
+            for (int e = 0; e < EU; ++e) lo[e] = hi[e] = odd_product(g == 1 ? hi[e] : lo[e], scale);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {

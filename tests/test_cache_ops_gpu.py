@@ -1100,3 +1100,37 @@ def test_append_rope_q8_other_scales(hkv, d, size):
         assert not bool(wrong.any()), (int(wrong.sum()), old[int(wrong.nonzero()[0, 0])])
         assert torch.equal(got[:, :, m], _e4m3(x / s[..., None]))
         assert torch.equal(got_codes.cpu()[ids][:, :, m + 1:], codes[which][ids][:, :, m + 1:])
+
+
+def _bf16(x):
+    """float64 to the nearest bfloat16 value, ties to even, in one rounding."""
+    step = torch.exp2(torch.frexp(x)[1].double() - 8)
+    return (x / step).round() * step
+
+
+@pytest.mark.parametrize("hkv,d", [(2, 128), (1, 64)])
+def test_page_bounds_q8_other_scales(hkv, d):
+    """Scales that are no powers of two, among them those next to the ones that bring a code to a tie: the bounds
+    are the codes' values rounded once."""
+    _say(f"bounds q8 other scales heads {hkv} d {d}")
+    gen = torch.Generator().manual_seed(d)
+    scales = [1.0 / 3, 0.7, 2.0 ** -100, 1.9 * 2.0 ** -100, 1.3 * 2.0 ** 90]
+    for x in range(9, 16, 2):                             # x scale is a tie between two bfloat16 values, but for the scale's own rounding
+        for t in range(257, 512, 10):
+            f = torch.tensor(t / x, dtype=F32)
+            scales += [float(torch.nextafter(f, f * k)) for k in (0, 1, 2)]
+    R = len(scales)
+    lens = [1 + 5 * r % 16 for r in range(R)]
+    pool, table = _paged([1] * R, 1, gen)
+    codes = torch.randint(0, 254, (pool, hkv, 16, d), generator=gen)
+    codes = torch.where(codes >= 127, codes + 1, codes).to(torch.uint8)        # every finite code
+    scale = torch.ones(pool, hkv)
+    scale[table[:, 0].long()] = torch.tensor(scales, dtype=F32)[:, None].expand(-1, hkv)
+    kv = gp.KV8Layer(codes.to(DEV), codes.to(DEV), scale.to(DEV), scale.to(DEV))
+    bounds = torch.zeros(pool, hkv, 2, d, dtype=BF16, device=DEV)
+    gp.gp_page_bounds_q8(kv, _state(table, [1] * R, lens, pool), bounds)
+    torch.cuda.synchronize()
+    got, v64 = bounds.cpu().double(), _values(kv.k, kv.k_scale)
+    for r, m in enumerate(lens):
+        want = _bf16(_bounds64(v64, table, lens, r, 0))
+        assert torch.equal(got[int(table[r, 0])], want), (r, m, scales[r])
