@@ -39,9 +39,9 @@
  *    zero on completion, so it can be reused without clearing.  Two calls
  *    that run concurrently must not share a workspace.
  *  - Pools (k, v) and workspaces lie at multiples of 16 bytes, other buffers at
- *    any multiple of their element's size.  gp_append_step takes pools, and the
- *    decode calls float32 pools and workspaces, at any multiple of the element
- *    as well.
+ *    any multiple of their element's size.  gp_append_step, gp_append_rope and
+ *    gp_page_bounds take pools, and the decode calls float32 pools and
+ *    workspaces, at any multiple of the element as well.
  *  - Page size b is 16 tokens; head_dim is 64 or 128; num_q_heads is 1, 2, 4
  *    or 8 times num_kv_heads.  Decode attention takes page tables up to 8192
  *    pages wide (131072 tokens per request), the boundary calls up to 4096
@@ -543,7 +543,8 @@ typedef struct {
  *  - q_out [num_tokens][num_q_heads][head_dim] takes the rotated queries of
  *    all requests that are not held, with or without room (q NULL: no
  *    queries; num_q_heads is then not looked at).  q_out may be q itself
- *    where q_stride == num_q_heads * head_dim; any other overlap is refused.
+ *    where q_stride == num_q_heads * head_dim; any other overlap of q_out with
+ *    q, k_new or v_new is refused.  Rows and q_out lie outside the pools.
  *  - advance != 0: seq_lens[r] and positions[r] of the requests that took
  *    their tokens then grow by n_r (pass 0 for every layer of a model but the
  *    last, as in gp_decode_step).
@@ -630,7 +631,8 @@ gp_status_t gp_select_pages(const void *bounds, gp_dtype_t dtype, const gp_page_
  * page (-1, or n and above) adds nothing; a page listed twice counts twice.  A
  * head whose list has no token gets a zero output.  Lists as gp_select_pages
  * writes them (from any step: they name table columns, not physical pages).
- * Takes the decode workspace of a table `budget` pages wide. */
+ * bfloat16 pools off 16 bytes are refused (GP_ERR_INVALID).  Takes the decode
+ * workspace of a table `budget` pages wide. */
 gp_status_t gp_decode_attention_pages(const gp_kv_layer_t *kv, const gp_page_state_t *ps,
                                       const int32_t *selected, int32_t budget, const void *q_post,
                                       int32_t num_q_heads, float scale, void *out, void *ws,

@@ -182,6 +182,8 @@ gp_status_t decode_call(const gp_kv_layer_t *kv, const gp_page_state_t *ps, cons
             return GP_ERR_INVALID;
     }
     if (listed && (budget < 1 || budget > kMaxDecodePages)) return GP_ERR_INVALID;
+    // (pages go to LDS in pieces of 16 bytes; float32 ones have another way)
+    if (listed && kv->dtype == GP_BF16 && !aligned16(kv->k, kv->v)) return GP_ERR_INVALID;
     if (ps->num_reqs == 0) return GP_OK;
     if (!q_post || !out || (!ws && !noalloc) || (listed && !selected)) return GP_ERR_INVALID;
     if (sum && (!sum->q_pre || !sum->slot_ids || !sum->init || !sum->qstate)) return GP_ERR_INVALID;

@@ -280,3 +280,10 @@ def test_binding_checks_the_device_of_every_tensor(monkeypatch):
             call(fn)
         monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     assert seen == 2 * 77                                 # tensors of the eight calls
+
+
+def test_decode_pages_refuses_pools_off_16_bytes(lib):
+    """bfloat16 pools; float32 ones may lie at any multiple of 4."""
+    call = lambda kv: lib.gp_decode_attention_pages(kv, _ps(), FAKE, 8, FAKE, 32, 0.1, FAKE, FAKE, 0, None)  # noqa: E731
+    assert call(_kv(k=FAKE + 2)) == call(_kv(v=FAKE + 8)) == INVALID
+    assert call(_kv()) == call(_kv(k=FAKE + 4, v=FAKE + 8, dtype=0)) == WORKSPACE
