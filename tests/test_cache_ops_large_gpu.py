@@ -287,3 +287,176 @@ def test_bounds_after_a_compaction():
             g = slice(h * G, (h + 1) * G)
             want, mag, size = _attention(_tokens(k64, table, r, m)[h:h + 1, tok], _tokens(v64, table, r, m)[h:h + 1, tok], q[r, g].double(), 0.09)
             assert bool(((got[r, g] - want).abs() <= _attention_tol(want, mag, size, d, BF16)).all()), (r, h)
+
+
+# ------------------------------------------------------------- the ends of the ranges --
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "q8"])
+def test_small_buffers_off_16_bytes(kind):
+    """Queries, outputs, bounds, lists and scales at any multiple of their element, float32 pools too: the bytes
+    of the aligned calls."""
+    _say(f"buffers off 16 bytes {kind}")
+    hq, hkv, d, budget = 8, 2, 128, 5
+    dt, q8 = F32 if kind == "f32" else BF16, kind == "q8"
+    gen = torch.Generator().manual_seed(31)
+    lens = [300, 17, 1, 0, 160]
+    npages = [-(-m // 16) for m in lens]
+    R, width, pool = len(lens), 24, sum(npages)
+    table = torch.full((R, width), -1, dtype=torch.int32)
+    perm, at = torch.randperm(pool, generator=gen).int(), 0
+    for r, P in enumerate(npages):
+        table[r, :P] = perm[at:at + P]
+        at += P
+    if q8:
+        pools = [torch.randint(0, 120, (pool, hkv, 16, d), generator=gen).to(torch.uint8).to(DEV) for _ in range(2)]
+        scales = [torch.rand(pool, hkv, generator=gen).add(0.5).to(DEV) for _ in range(2)]
+    else:
+        pools = [torch.randn(pool, hkv, 16, d, generator=gen).to(dt).to(DEV) for _ in range(2)]
+    q = torch.randn(R, hq, d, generator=gen).to(dt).to(DEV)
+    results = []
+    for off in (0, 1, 3):
+        if q8:
+            kv = gp.KV8Layer(*pools, *(_offset(s, off) for s in scales))
+        else:
+            kv = gp.KVLayer(*(_offset(p, off) if kind == "f32" else p for p in pools))
+        to = lambda t: _offset(t, off)  # noqa: E731
+        ps = gp.PageState(to(table.to(DEV)), to(_i32(npages)), to(_i32(lens)), _i32([1] * pool), _i32([0] * pool), _i32([0]))
+        bounds, out = to(torch.zeros(pool, hkv, 2, d, dtype=dt, device=DEV)), [to(torch.full_like(q, NAN)) for _ in range(2)]
+        sel, mine = to(torch.zeros(R, hkv, budget, dtype=torch.int32, device=DEV)), to(q)
+        (gp.gp_page_bounds_q8 if q8 else gp.gp_page_bounds)(kv, ps, bounds)
+        gp.gp_select_pages(bounds, ps, mine, 1, 1, sel, gp.workspace(gp.GP_OP_SELECT, R, 0, hq, hkv, d, width, dt))
+        (gp.gp_decode_attention_pages_q8 if q8 else gp.gp_decode_attention_pages)(
+            kv, ps, sel, mine, 0.1, out[0], gp.workspace(gp.GP_OP_DECODE, R, 0, hq, hkv, d, budget, dt))
+        (gp.gp_decode_attention_q8 if q8 else gp.gp_decode_attention)(
+            kv, ps, mine, 0.1, out[1], gp.workspace(gp.GP_OP_DECODE, R, 0, hq, hkv, d, width, dt))
+        torch.cuda.synchronize()
+        results.append([t.clone() for t in (bounds, sel, *out)])
+        assert bool(out[0].isfinite().all()) and bool(out[1].isfinite().all())
+    for other in results[1:]:
+        for a, b in zip(results[0], other):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "q8"])
+def test_most_requests(kind):
+    """65535 requests of up to three pages, one KV head: prompts and a token each, bounds, selection, attention."""
+    R, hq, hkv, d, width, budget = 65535, 1, 1, 64, 3, 2
+    _say(f"most requests {kind}")
+    q8 = kind == "q8"
+    gen = torch.Generator().manual_seed(65)
+    new = torch.randint(0, 46, (R,), generator=gen)
+    new[:4] = torch.tensor([0, 45, 1, 16])
+    lens = (new + 1).tolist()
+    table = torch.randperm(width * R, generator=gen).int().view(R, width)
+    pool = width * R
+    if q8:
+        kv = gp.KV8Layer(*(torch.full((pool, hkv, 16, d), 0x7f, dtype=torch.uint8, device=DEV) for _ in range(2)),
+                         *(torch.full((pool, hkv), NAN, device=DEV) for _ in range(2)))
+    else:
+        kv = gp.KVLayer(*(torch.full((pool, hkv, 16, d), NAN, dtype=BF16, device=DEV) for _ in range(2)))
+    append, bound, attend, whole = ((gp.gp_append_rope_q8, gp.gp_page_bounds_q8, gp.gp_decode_attention_pages_q8, gp.gp_decode_attention_q8)
+                                    if q8 else (gp.gp_append_rope, gp.gp_page_bounds, gp.gp_decode_attention_pages, gp.gp_decode_attention))
+    ps, pos = _state(table, [width] * R, [0] * R, pool), _i32([-1] * R)
+    starts = torch.cat([torch.zeros(1, dtype=torch.int64), new.cumsum(0)])
+    T = int(starts[-1])
+    k, v = (torch.randn(T, hkv, d, generator=gen).to(BF16) for _ in range(2))
+    k1, v1, q = (torch.randn(R, hkv, d, generator=gen).to(BF16) for _ in range(3))
+    append(kv, ps, pos, k.to(DEV), v.to(DEV), 1e4, tok_start=_i32(starts))
+    q_out = torch.zeros(R, hq, d, dtype=BF16, device=DEV)
+    append(kv, ps, pos, k1.to(DEV), v1.to(DEV), 1e4, q=q.to(DEV), q_out=q_out)
+    bounds = torch.zeros(pool, hkv, 2, d, dtype=BF16, device=DEV)
+    bound(kv, ps, bounds)
+    sel = torch.zeros(R, hkv, budget, dtype=torch.int32, device=DEV)
+    gp.gp_select_pages(bounds, ps, q_out, 0, 1, sel, gp.workspace(gp.GP_OP_SELECT, R, 0, hq, hkv, d, width, BF16))
+    out = [torch.full((R, hq, d), NAN, dtype=BF16, device=DEV) for _ in range(2)]
+    attend(kv, ps, sel, q_out, 0.125, out[0], gp.workspace(gp.GP_OP_DECODE, R, 0, hq, hkv, d, budget, BF16))
+    whole(kv, ps, q_out, 0.125, out[1], gp.workspace(gp.GP_OP_DECODE, R, 0, hq, hkv, d, width, BF16))
+    torch.cuda.synchronize()
+    assert ps.seq_lens.cpu().tolist() == lens and pos.cpu().tolist() == [m - 1 for m in lens]
+    assert all(bool(o.isfinite().all()) for o in out)
+    k64, v64 = (_values(kv.k, kv.k_scale), _values(kv.v, kv.v_scale)) if q8 else (kv.k.cpu().double(), kv.v.cpu().double())
+    box, chosen, qr, got = bounds.cpu(), sel.cpu(), q_out.cpu(), [o.cpu().double() for o in out]
+    for r in [0, 1, 2, 3, R - 1] + torch.randint(0, R, (200,), generator=gen).tolist():
+        m, n = lens[r], -(-lens[r] // 16)
+        rows = torch.cat([k[starts[r]:starts[r + 1]], k1[r:r + 1]]).double()
+        want, mag = _rotated(rows, torch.arange(m), 1e4)
+        K, V = _tokens(k64, table, r, m), _tokens(v64, table, r, m)
+        floor = 2.0 ** -10 * float(kv.k_scale[table[r, :n].long().to(DEV)].max()) if q8 else 0.0
+        # (the last page's older codes may have been rounded again under the token's scale: half its lowest step)
+        assert bool(((K.transpose(0, 1) - want).abs() <= want.abs() * (2.0 ** -4 if q8 else 2.0 ** -8) + ROT * mag + 2 * floor).all()), r
+        for p in range(n):
+            assert torch.equal(box[int(table[r, p])].double(), _bounds64(k64, table, lens, r, p)), (r, p)
+        want_sel = _select64(box, table, n, qr, hkv, budget, 0, 1, r)
+        assert torch.equal(chosen[r], want_sel), r
+        tok = [16 * p + j for p in want_sel[0].tolist() if p >= 0 for j in range(min(16, m - 16 * p))]
+        for o, pick in ((got[0], tok), (got[1], list(range(m)))):
+            want, mag, size = _attention(K[:, pick], V[:, pick], qr[r].double(), 0.125)
+            assert bool(((o[r] - want).abs() <= _attention_tol(want, mag, size, d, BF16)).all()), r
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "q8"])
+def test_widest_tables(kind):
+    """Tables and lists of 8192 pages: every page listed, in an order of its own, against the whole cache."""
+    R, hq, hkv, d, width = 2, 4, 1, 64, 8192
+    _say(f"widest tables {kind}")
+    dt, q8 = F32 if kind == "f32" else BF16, kind == "q8"
+    gen = torch.Generator().manual_seed(8192)
+    lens, npages, pool = [16 * width, 16 * width - 9], [width, width], 2 * width
+    table = torch.randperm(pool, generator=gen).int().view(R, width)
+    if q8:
+        kv = gp.KV8Layer(*(torch.randint(0, 100, (pool, hkv, 16, d), generator=gen).to(torch.uint8).to(DEV) for _ in range(2)),
+                         *(torch.rand(pool, hkv, generator=gen).add(0.5).mul(2.0 ** -5).to(DEV) for _ in range(2)))
+        k64, v64 = _values(kv.k, kv.k_scale), _values(kv.v, kv.v_scale)
+    else:
+        kv = gp.KVLayer(*(torch.randn(pool, hkv, 16, d, generator=gen).to(dt).to(DEV) for _ in range(2)))
+        k64, v64 = kv.k.cpu().double(), kv.v.cpu().double()
+    sel = torch.stack([torch.randperm(width, generator=gen) for _ in range(R)]).int().view(R, hkv, width).to(DEV)
+    q = torch.randn(R, hq, d, generator=gen).to(dt)
+    ps, out = _state(table, npages, lens, pool), [torch.full((R, hq, d), NAN, dtype=dt, device=DEV) for _ in range(2)]
+    ws = gp.workspace(gp.GP_OP_DECODE, R, 0, hq, hkv, d, width, dt)
+    (gp.gp_decode_attention_pages_q8 if q8 else gp.gp_decode_attention_pages)(kv, ps, sel, q.to(DEV), 0.125, out[0], ws)
+    (gp.gp_decode_attention_q8 if q8 else gp.gp_decode_attention)(kv, ps, q.to(DEV), 0.125, out[1], ws)
+    torch.cuda.synchronize()
+    for r, m in enumerate(lens):
+        want, mag, size = _attention(_tokens(k64, table, r, m), _tokens(v64, table, r, m), q[r].double(), 0.125)
+        for o in out:
+            assert bool(((o[r].cpu().double() - want).abs() <= _attention_tol(want, mag, size, d, dt)).all()), r
+
+
+def test_rows_past_32_bits():
+    """2^26 + 13 new tokens, whose rows and pages lie past 2^32 bytes: the last of them where they belong."""
+    T, R, hkv, d = 2 ** 26 + 13, 600, 1, 64
+    _say(f"rows past 32 bits, {T} tokens")
+    per = -(-T // R)
+    new = [per] * (R - 1) + [T - per * (R - 1)]
+    npages = [-(-n // 16) for n in new]
+    pool, width = sum(npages), max(npages)
+    assert width <= 8192 and T * d * 2 > 2 ** 32
+    first = torch.tensor([0] + npages[:-1]).cumsum(0)
+    table = (first[:, None] + torch.arange(width)).int()
+    for r, P in enumerate(npages):
+        table[r, P:] = -1
+    table = torch.where(table >= 0, pool - 1 - table, table)              # the last request's pages first
+    table = torch.cat([table[R // 2:], table[:R // 2]])                   # (and halfway round)
+    counts = npages[R // 2:] + npages[:R // 2]
+    sizes = new[R // 2:] + new[:R // 2]
+    gen = torch.Generator(device=DEV).manual_seed(26)
+    k = torch.randn(T, hkv, d, generator=gen, device=DEV, dtype=BF16)
+    v = torch.randn(T, hkv, d, generator=gen, device=DEV, dtype=BF16)
+    kv = gp.KVLayer(*(torch.zeros(pool, hkv, 16, d, dtype=BF16, device=DEV) for _ in range(2)))
+    ps, pos = _state(table, counts, [0] * R, pool), _i32([-1] * R)
+    starts = [0]
+    for n in sizes:
+        starts.append(starts[-1] + n)
+    gp.gp_append_rope(kv, ps, pos, k, v, 1e6, tok_start=_i32(starts))
+    torch.cuda.synchronize()
+    assert ps.seq_lens.cpu().tolist() == sizes
+    for r in (0, 1, R // 2 - 1, R // 2, R - 2, R - 1):
+        n = sizes[r]
+        ids = table[r, :counts[r]].long().to(DEV)
+        got = kv.v[ids].transpose(1, 2).reshape(-1, hkv, d)
+        assert torch.equal(got[:n], v[starts[r]:starts[r + 1]]) and bool((got[n:] == 0).all()), r
+        at = torch.tensor([0, 1, n // 2, n - 2, n - 1])
+        want, mag = _rotated(k[starts[r] + at.to(DEV)].cpu().double(), at, 1e6)
+        turned = kv.k[ids].transpose(1, 2).reshape(-1, hkv, d)[at.to(DEV)].cpu().double()
+        assert bool(((turned - want).abs() <= want.abs() * HALF[BF16] + ROT * mag).all()), r
