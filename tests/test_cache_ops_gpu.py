@@ -1134,3 +1134,33 @@ def test_page_bounds_q8_other_scales(hkv, d):
     for r, m in enumerate(lens):
         want = _bf16(_bounds64(v64, table, lens, r, 0))
         assert torch.equal(got[int(table[r, 0])], want), (r, m, scales[r])
+
+
+@pytest.mark.parametrize("k_scale,q_size", [(2.0 ** -6, 1.0), (2.0 ** -100, 2.0 ** 94), (2.0 ** 100, 2.0 ** -106)])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (2, 2, 64)])
+def test_decode_q8_every_key_code(hq, hkv, d, k_scale, q_size):
+    """Each finite code as a key, met by a query of one dim: the weights are those of the values it stands for."""
+    _say(f"decode q8 every key code heads {hq}/{hkv} d {d} scale {k_scale}")
+    gen = torch.Generator().manual_seed(d)
+    finite = torch.tensor([c for c in range(256) if c & 0x7f != 0x7f], dtype=torch.uint8)
+    R, lens = 16, [16] * 16
+    pool, table = _paged([1] * R, 4, gen)
+    codes = torch.zeros(pool, hkv, 16, d, dtype=torch.uint8)
+    for r in range(R):                                    # dim 5 + h: 16 codes side by side, other ones in each head
+        for h in range(hkv):
+            codes[int(table[r, 0]), h, :, 5 + h] = finite[(16 * r + 37 * h + torch.arange(16)) % 254]
+    values = torch.randn(pool, hkv, 16, d, generator=gen).to(torch.float8_e4m3fn).view(torch.uint8)
+    scale = torch.full((pool, hkv), k_scale)
+    kv = gp.KV8Layer(codes.to(DEV), values.to(DEV), scale.to(DEV), torch.ones(pool, hkv, device=DEV))
+    q = torch.zeros(R, hq, d)
+    for h in range(hkv):
+        q[:, h * (hq // hkv):(h + 1) * (hq // hkv), 5 + h] = q_size
+    q = q.to(BF16)
+    out = torch.full((R, hq, d), NAN, dtype=BF16, device=DEV)
+    gp.gp_decode_attention_q8(kv, _state(table, [1] * R, lens, pool), q.to(DEV), 0.5, out,
+                              gp.workspace(gp.GP_OP_DECODE, R, 0, hq, hkv, d, 4, BF16))
+    torch.cuda.synchronize()
+    k64, v64 = _values(kv.k, kv.k_scale), _values(kv.v, kv.v_scale)
+    for r in range(R):
+        want, mag, size = _attention(_tokens(k64, table, r, 16), _tokens(v64, table, r, 16), q[r].double(), 0.5)
+        assert bool(((out[r].cpu().double() - want).abs() <= _attention_tol(want, mag, size, d, BF16)).all()), r
