@@ -646,8 +646,8 @@ struct Page<float, D, true> : QuadOut<D> {
 // each.  One page at a time (the sixteen tokens twice, with both terms in one
 // product) every value was widened in two lanes and a page cost 190 vector
 // instructions; now 106, and the softmax is formed once per pair.  64 requests of
-// 1024-8192 tokens, 32/8 heads, d 128: 97 us for the pass, 6.1 TB/s (119 us and 5.0
-// before), 256 requests 241 us, 6.2 TB/s, of the 6.9 that a stream of reads reaches.
+// 1024-8192 tokens, 32/8 heads, d 128: 99.6 us for the pass (119 before), 6.1 TB/s of
+// traffic, 256 requests 247 us and 6.3, of the 6.9 that a stream of reads reaches.
 // The vector ALU is busy a third of that time (212 instructions of 4 cycles a pair), the
 // matrix unit a sixth (384 cycles).  More or fewer workgroups (512 to 2048), or one of
 // sixteen waves per request: the same within 2 %.

@@ -19,9 +19,10 @@
 // items.
 //
 // Bound: HBM for prompts (every row read once and written once): 42 k tokens of 64/8
-// heads, d 128, bfloat16 take 338 us for 1.73 GB, 5.1 TB/s (a device copy of 2 GiB
-// reaches 4.9); 8-bit chunks 134 us for 0.70 GB, 5.2 TB/s.  Latency for the tokens of a
-// step: 3.6 us, 8 bits 6.1 (load, the page's maximum, old codes, store).
+// heads, d 128, bfloat16 take 339 us for 1.73 GB, 5.1 TB/s (a device copy of 2 GiB
+// reaches 4.9); 42 k of 32/8 in float32 365 us for 1.81 GB, 5.0 TB/s; 8-bit chunks 135 us
+// for 0.70 GB, 5.2 TB/s.  Latency for the tokens of a step: 3.6 us, 8 bits 6.2 (load, the
+// page's maximum, old codes, store); advancing the lengths is a launch of its own, 1.4 us.
 #include <algorithm>
 #include <type_traits>
 

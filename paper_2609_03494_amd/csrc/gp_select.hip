@@ -10,9 +10,10 @@
 // order of a sum; it is rounded once to float32 and the ties go to the lower page.
 //
 // Bound: HBM.  The bounds of a page and head are 2 d elements, a sixteenth of the
-// page's keys and values.  Scores: 226 MB of boxes in 40.5 us, 5.6 TB/s, of the 6.9 that
-// a stream of reads reaches; bounds: 337 MB in 63.5 us, 5.3 TB/s.  The choice itself
-// reads a few numbers a page and waits on its own barriers: 6.3 us, 7.8 for 384 lists
+// page's keys and values.  Scores: 226 MB of boxes in 40.8 us, 5.5 TB/s, of the 6.9 that
+// a stream of reads reaches; bounds: 337 MB (float32, d 64) in 63.7 us, 5.3 TB/s, 304 MB
+// (bfloat16, d 128) in 64.5, 4.7, 156 MB (8 bits, d 128) in 48.8, 3.2.  The choice itself
+// reads a few numbers a page and waits on its own barriers: 6.4 us, 7.8 for 384 lists
 // out of up to 2048 pages.
 #include <algorithm>
 #include <type_traits>
