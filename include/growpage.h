@@ -9,10 +9,14 @@
  *   gp_update_summaries  every step: the two EMA query summaries (Sec. 3.2)
  *   gp_decode_attention  every step: paged GQA decode attention (Sec. 3.1)
  *   gp_append_rope       prompts and new tokens into the cache, rotated on the way
- *                        (bfloat16, float32, or 8-bit values with scales)
+ *                        (bfloat16, float32, or 8-bit values with scales);
+ *                        gp_append_rotary: pairs side by side, a part of the head,
+ *                        frequencies for longer contexts
  *   gp_decode_attention_q8     decode attention over the 8-bit cache
  *   gp_select_pages, gp_decode_attention_pages   attention over the pages that
  *                        a bound on their logits selects
+ *   gp_pages_reserve, gp_pages_fork, gp_pages_release   pages to requests, shared
+ *                        with those that continue them, and back to the free stack
  *   gp_boundary_score    at boundaries: calibrated, rotated summaries scored
  *                        against the cached keys, top-p working sets (Sec. 3.2,
  *                        App. E.1) and token importance (Sec. 3.3)
@@ -576,6 +580,59 @@ gp_status_t gp_append_rope_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *p
                               const void *v_new, int64_t v_stride, int32_t num_q_heads, float rope_theta,
                               int32_t advance, hipStream_t stream);
 
+/* Rotary positions in other forms than gp_append_rope's (half-split pairs of the whole
+ * head at theta^(-2 i / d)).  A rotation turns the first rotary_dim dims of a head, the
+ * others pass as they are: pair i < rotary_dim / 2 is (x_i, x_{i + rotary_dim / 2}) with
+ * GP_ROPE_HALF and (x_{2 i}, x_{2 i + 1}) with GP_ROPE_INTERLEAVED.  At the
+ * logical index t it turns by t * freq[i] radians (the product in 64 bits) and grows
+ * by `magnitude`: cosine and sine times the magnitude are rounded to float32 once.
+ * rotary_dim: a multiple of 16 (GP_ERR_UNSUPPORTED otherwise) up to head_dim;
+ * frequencies finite, the magnitude positive and finite (GP_ERR_INVALID).
+ * HOST memory, read during the call. */
+enum { GP_ROPE_HALF = 0, GP_ROPE_INTERLEAVED = 1 };
+typedef struct {
+    int32_t layout;          /* GP_ROPE_*                                       */
+    int32_t rotary_dim;
+    float magnitude;         /* 1: rotation only                                */
+    double freq[64];         /* [rotary_dim / 2]                                */
+} gp_rope_t;
+
+/* Frequencies for a rotation (HOST memory, nothing is launched): f_i =
+ * theta^(-2 i / rotary_dim), scaled for contexts longer than those of training.
+ *  - high_turns == 0: all divided by `factor` (1: none; the positions shrink).
+ *  - otherwise by how often a pair turns over the first `context` tokens, u_i =
+ *    context f_i / 2 pi: pairs of more than high_turns turns keep f_i, those of
+ *    less than low_turns get f_i / factor, and in between f_i (w + (1 - w) /
+ *    factor) with w = (u_i - low_turns) / (high_turns - low_turns).
+ * factor >= 1, 0 <= low_turns < high_turns, theta, context > 0, all finite; rotary_dim
+ * even, 2 to 128 (GP_ERR_INVALID). */
+gp_status_t gp_rope_frequencies(double *freq, int32_t rotary_dim, double theta, double factor,
+                                double low_turns, double high_turns, double context);
+
+/* gp_append_rope and gp_append_rope_q8 with a rotation of the caller's: all else as
+ * there. */
+gp_status_t gp_append_rotary(const gp_kv_layer_t *kv, const gp_page_state_t *ps, int32_t *positions,
+                             const gp_rope_t *rope, const int32_t *tok_start, int32_t num_tokens,
+                             const void *q, int64_t q_stride, void *q_out, const void *k_new,
+                             int64_t k_stride, const void *v_new, int64_t v_stride, int32_t num_q_heads,
+                             int32_t advance, hipStream_t stream);
+gp_status_t gp_append_rotary_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps, int32_t *positions,
+                                const gp_rope_t *rope, const int32_t *tok_start, int32_t num_tokens,
+                                const void *q, int64_t q_stride, void *q_out, const void *k_new,
+                                int64_t k_stride, const void *v_new, int64_t v_stride,
+                                int32_t num_q_heads, int32_t advance, hipStream_t stream);
+
+/* gp_boundary_score_stages over a cache written with such a rotation: the calibrated
+ * summaries turn as `rope` says, magnitude included, in 64 bits throughout
+ * (params->rope_theta is not looked at). */
+gp_status_t gp_boundary_score_rotary(const gp_kv_layer_t *kv, const gp_page_state_t *ps,
+                                     const void *q_pre, const float *qstate, int32_t num_slots,
+                                     const int32_t *slot_ids, const int32_t *positions,
+                                     const int32_t *bnd, int32_t num_bnd, int32_t num_q_heads,
+                                     const gp_params_t *params, const gp_rope_t *rope, int32_t *k_counts,
+                                     float *scores, int32_t max_cand, void *ws, size_t ws_bytes,
+                                     hipStream_t stream, int32_t stages);
+
 /* gp_decode_attention over an 8-bit cache (Sec. 3.1): the same arguments and
  * rules, q_post and out bfloat16.  The codes are used as the values they stand
  * for, without further rounding.  The scale is below 2^111 (GP_ERR_INVALID
@@ -641,6 +698,58 @@ gp_status_t gp_decode_attention_pages_q8(const gp_kv8_layer_t *kv, const gp_page
                                          const int32_t *selected, int32_t budget, const void *q_post,
                                          int32_t num_q_heads, float scale, void *out, void *ws,
                                          size_t ws_bytes, hipStream_t stream);
+
+/* Pages to requests, from the free stack (Sec. 4.2, App. E.2): what a request
+ * needs before tokens go in (gp_append_rope takes them only where they fit).
+ * gp_pages_reserve: every request r that is not held gets the pages that
+ * tokens[r] more tokens need beyond the P_r that it has, ceil((m_r + tokens[r]) /
+ * page_size) - P_r, off the top of the stack, with a reference count of one, appended to
+ * its table row.  Requests are served in order: from the first whose pages would
+ * leave fewer than keep_free on the stack, none that needs any gets them (no
+ * request overtakes one that waits).  One whose pages do not fit its table row
+ * gets none and holds up nobody.  granted[r] = 1 where r has the room for its
+ * tokens after the call, else 0 (and no page).  tokens [num_reqs] int32, negative
+ * as 0; granted [num_reqs] int32, both on the device. */
+gp_status_t gp_pages_reserve(const gp_page_state_t *ps, const int32_t *tokens, int32_t keep_free,
+                             int32_t *granted, hipStream_t stream);
+
+/* A request that goes on from another's tokens (several replies to one prompt, a
+ * prompt that begins like another; App. E.2, reference-counted blocks).  Fork i
+ * makes row children[i], which must hold nothing (no pages, no tokens), continue
+ * row parents[i]: it takes the first L = min(m_p, lengths[i]) tokens (lengths NULL:
+ * all), the whole pages among them by reference (their counts grow by one), the
+ * L % page_size rows of the next as a copy in a page off the stack, in each of the
+ * n_layers layers (8-bit: with the page's scales), so that both can go on writing.
+ * Its num_pages and seq_lens are set, and with positions not NULL its
+ * positions[c] = positions[p] - (m_p - L).  Rows of the copy past L stay as they were.
+ *  - forked[i] = 1, or 0 with nothing done: an index out of range, a held parent, a
+ *    child that holds something or that an earlier fork of the call lists too, or no
+ *    page left on the stack for the copy.  Fresh pages go to the forks in order.
+ *  - All is judged on the state as the call starts; one parent may have any number
+ *    of children.  A row that is to become a child has no tokens, so as a parent in the
+ *    same call it gives none.
+ *  - Page bounds (gp_page_bounds) of the copied page and summaries are the caller's
+ *    to make or copy.
+ * parents, children, lengths and forked [num_forks] int32 on the device.  Pools at
+ * multiples of 16 bytes (GP_ERR_INVALID otherwise); layers of one shape; at most 2048
+ * forks, 256 layers and 8192 KV heads (GP_ERR_UNSUPPORTED). */
+gp_status_t gp_pages_fork(const gp_kv_layer_t *layers, int32_t n_layers, const gp_page_state_t *ps,
+                          const int32_t *parents, const int32_t *children, const int32_t *lengths,
+                          int32_t num_forks, int32_t *positions, int32_t *forked, hipStream_t stream);
+gp_status_t gp_pages_fork_q8(const gp_kv8_layer_t *layers, int32_t n_layers, const gp_page_state_t *ps,
+                             const int32_t *parents, const int32_t *children, const int32_t *lengths,
+                             int32_t num_forks, int32_t *positions, int32_t *forked, hipStream_t stream);
+
+/* Requests that end: each of the `num` rows listed gives up its pages (every
+ * one loses one reference; those without any go onto the free stack, lowest page id
+ * first, as in gp_boundary_apply) and is left with num_pages = seq_lens = 0.  A row listed
+ * twice counts once; one out of range or held is left as it is.  The table row and
+ * positions keep their old values.  reqs [num] int32 on the device, num at most
+ * 65535.
+ * These three calls change the free stack and the reference counts and must be
+ * ordered with the others that do (see gp_boundary_compact).  Tables up to 8192
+ * pages wide, 65535 requests (GP_ERR_UNSUPPORTED). */
+gp_status_t gp_pages_release(const gp_page_state_t *ps, const int32_t *reqs, int32_t num, hipStream_t stream);
 
 /* Bytes of workspace an operation needs (op = GP_OP_DECODE / SCORE / APPLY / SELECT). */
 size_t gp_workspace_bytes(int32_t op, int32_t num_reqs, int32_t num_bnd, int32_t num_q_heads,

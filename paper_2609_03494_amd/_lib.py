@@ -26,6 +26,7 @@ GP_METRIC_TOP_P, GP_METRIC_ENTROPY = 0, 1
 GP_DECODE_CHUNKS, GP_DECODE_MERGE, GP_DECODE_PREFIX = 1, 2, 4
 GP_LAYOUT_SHIFT, GP_LAYOUT_FILL = 0, 1
 GP_SCORE_WEIGHTS, GP_SCORE_COUNTS = 1, 2
+GP_ROPE_HALF, GP_ROPE_INTERLEAVED = 0, 1
 PAGE_SIZE = 16
 GP_ERR_SCRATCH = 5
 
@@ -34,7 +35,9 @@ EXPORTS = ("gp_update_summaries", "gp_decode_attention", "gp_decode_attention_no
            "gp_boundary_apply", "gp_boundary_select", "gp_boundary_decide", "gp_boundary_compact",
            "gp_release_held", "gp_append_step", "gp_append_rope", "gp_append_rope_q8", "gp_decode_attention_q8",
            "gp_page_bounds", "gp_page_bounds_q8", "gp_select_pages", "gp_decode_attention_pages",
-           "gp_decode_attention_pages_q8", "gp_workspace_bytes", "gp_status_string", "gp_stream_read")
+           "gp_decode_attention_pages_q8", "gp_pages_reserve", "gp_pages_fork", "gp_pages_fork_q8", "gp_pages_release",
+           "gp_append_rotary", "gp_append_rotary_q8", "gp_rope_frequencies", "gp_boundary_score_rotary",
+           "gp_workspace_bytes", "gp_status_string", "gp_stream_read")
 
 
 class GrowPageError(RuntimeError):
@@ -61,6 +64,11 @@ class _PageState(ctypes.Structure):
                 ("free_list", ctypes.c_void_p), ("free_count", ctypes.c_void_p),
                 ("num_reqs", ctypes.c_int32), ("max_pages", ctypes.c_int32),
                 ("pool_pages", ctypes.c_int32)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("freq", ctypes.c_double * 64)]
 
 
 class _PrefixGroup(ctypes.Structure):
@@ -134,7 +142,9 @@ def load() -> ctypes.CDLL:
     i64, ps_p, kv_p, kv8_p = ctypes.c_int64, ctypes.POINTER(_PageState), ctypes.POINTER(_KVLayer), ctypes.POINTER(_KV8Layer)
     rope_args = [ps_p, vp, vp, i32, vp, i64, vp, vp, i64, vp, i64, i32, f32, i32, vp]
     pages_args = [ps_p, vp, i32, vp, i32, f32, vp, vp, sz, vp]
+    rotary_args = [ps_p, vp, ctypes.POINTER(_Rope), vp, i32, vp, i64, vp, vp, i64, vp, i64, i32, i32, vp]
     for name, layer, rest in (("gp_append_rope", kv_p, rope_args), ("gp_append_rope_q8", kv8_p, rope_args),
+                              ("gp_append_rotary", kv_p, rotary_args), ("gp_append_rotary_q8", kv8_p, rotary_args),
                               ("gp_decode_attention_q8", kv8_p, [ps_p, vp, i32, f32, vp, vp, sz, vp]),
                               ("gp_page_bounds", kv_p, [ps_p, vp, i32, vp, vp]),
                               ("gp_page_bounds_q8", kv8_p, [ps_p, vp, i32, vp, vp]),
@@ -144,6 +154,17 @@ def load() -> ctypes.CDLL:
         getattr(lib, name).argtypes = [layer] + rest
     lib.gp_select_pages.restype = ctypes.c_int
     lib.gp_select_pages.argtypes = [vp, ctypes.c_int, ps_p, vp, i32, i32, i32, i32, i32, i32, vp, vp, sz, vp]
+    lib.gp_rope_frequencies.restype = ctypes.c_int
+    lib.gp_rope_frequencies.argtypes = [vp, i32] + [ctypes.c_double] * 5
+    lib.gp_boundary_score_rotary.restype = ctypes.c_int
+    lib.gp_boundary_score_rotary.argtypes = lib.gp_boundary_score.argtypes[:11] + [ctypes.POINTER(_Rope)] + \
+        lib.gp_boundary_score.argtypes[11:] + [i32]
+    lib.gp_pages_reserve.restype = lib.gp_pages_release.restype = ctypes.c_int
+    lib.gp_pages_reserve.argtypes = [ps_p, vp, i32, vp, vp]
+    lib.gp_pages_release.argtypes = [ps_p, vp, i32, vp]
+    for name, layer in (("gp_pages_fork", kv_p), ("gp_pages_fork_q8", kv8_p)):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = [layer, i32, ps_p, vp, vp, vp, i32, vp, vp, vp]
     _lib = lib
     return lib
 
@@ -211,6 +232,24 @@ class KV8Layer:
         if ks.dtype != torch.float32 or vs.dtype != torch.float32 or ks.shape != (pool, hkv) or vs.shape != (pool, hkv):
             raise ValueError("scales of an 8-bit cache: float32 [pool_pages, num_kv_heads]")
         return _KV8Layer(_ptr(k), _ptr(v), _ptr(ks), _ptr(vs), pool, hkv, b, d)
+
+
+class Layers:
+    """The layers of one cache (KVLayer or KV8Layer, all of one kind) as the calls over several take
+    them, made once: a program keeps it beside the pools, whose tensors it holds."""
+
+    def __init__(self, layers):
+        self.layers = list(layers)
+        kinds = {type(layer) for layer in self.layers}
+        if len(kinds) != 1 or not kinds <= {KVLayer, KV8Layer}:
+            raise ValueError("Layers: one or more KVLayer, or KV8Layer")
+        self.q8 = kinds == {KV8Layer}
+        self._c = ((_KV8Layer if self.q8 else _KVLayer) * len(self.layers))(*[layer.c() for layer in self.layers])
+        devices = {t.get_device() for layer in self.layers for t in vars(layer).values()}
+        self._device = devices.pop() if len(devices) == 1 else -1
+
+    def __len__(self) -> int:
+        return len(self.layers)
 
 
 @dataclass
@@ -440,7 +479,8 @@ def _on_device(name: str, kv: KVLayer | KV8Layer | None, ps: PageState, *tensors
         raise ValueError(f"{name}: tensors that are not on the current device")
 
 
-def _append_rope(name, kv, dtype, ps, positions, k_new, v_new, rope_theta, q, q_out, tok_start, advance, stream):
+def _append_rope(name, kv, dtype, ps, positions, k_new, v_new, rope_theta, q, q_out, tok_start, advance, stream,
+                 rope=None):
     c_kv, c_ps = kv.c(), ps.c()
     d, shape = c_kv.head_dim, k_new.shape
     T = shape[0]
@@ -457,9 +497,10 @@ def _append_rope(name, kv, dtype, ps, positions, k_new, v_new, rope_theta, q, q_
     if positions.dtype != torch.int32 or positions.numel() < c_ps.num_reqs:
         raise ValueError(f"{name}: positions [num_reqs] int32")
     _on_device(name, kv, ps, positions, k_new, v_new, q, q_out, tok_start)
-    st = getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(positions), _ptr(tok_start), T, q_ptr, q_row,
-                               qo_ptr, k_new.data_ptr(), _row(k_new.stride(), T, shape[1], d, name), v_new.data_ptr(),
-                               _row(v_new.stride(), T, shape[1], d, name), Hq, rope_theta, bool(advance), _stream(stream))
+    form, theta = ((), (rope_theta,)) if rope is None else ((ctypes.byref(rope._c),), ())
+    st = getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(positions), *form, _ptr(tok_start), T, q_ptr,
+                               q_row, qo_ptr, k_new.data_ptr(), _row(k_new.stride(), T, shape[1], d, name), v_new.data_ptr(),
+                               _row(v_new.stride(), T, shape[1], d, name), Hq, *theta, bool(advance), _stream(stream))
     _check(st, name)
 
 
@@ -487,6 +528,58 @@ def gp_append_rope_q8(kv: KV8Layer, ps: PageState, positions: torch.Tensor, k_ne
     """gp_append_rope into an 8-bit cache (rows bfloat16)."""
     _append_rope("gp_append_rope_q8", kv, torch.bfloat16, ps, positions, k_new, v_new, rope_theta, q, q_out,
                  tok_start, advance, stream)
+
+
+def gp_rope_frequencies(rotary_dim: int, theta: float, factor: float = 1.0, low_turns: float = 0.0,
+                        high_turns: float = 0.0, context: float = 0.0) -> list[float]:
+    """Radians per position of each of rotary_dim / 2 pairs: theta^(-2 i / rotary_dim), over `factor`
+    for all of them, or (high_turns not 0) for those that turn seldom over the first `context` tokens."""
+    if not 2 <= rotary_dim <= 128:
+        raise ValueError("gp_rope_frequencies: rotary_dim 2 to 128")
+    freq = (ctypes.c_double * 64)()
+    _check(load().gp_rope_frequencies(freq, rotary_dim, theta, factor, low_turns, high_turns, context),
+           "gp_rope_frequencies")
+    return list(freq)[:rotary_dim // 2]
+
+
+class Rope:
+    """A rotation: GP_ROPE_HALF or GP_ROPE_INTERLEAVED pairs over the first 2 len(freq) dims of a head,
+    radians per position of each pair, and a factor on cosine and sine.  Not to be changed afterwards."""
+
+    def __init__(self, layout: int, freq, magnitude: float = 1.0):
+        self.layout, self.freq, self.magnitude = layout, tuple(float(f) for f in freq), float(magnitude)
+        if not 1 <= len(self.freq) <= 64:
+            raise ValueError("Rope: 1 to 64 frequencies, one for each pair")
+        self._c = _Rope(layout, 2 * len(self.freq), magnitude, (ctypes.c_double * 64)(*self.freq))
+
+
+def gp_append_rotary(kv: KVLayer, ps: PageState, positions: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                     rope: Rope, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+                     tok_start: torch.Tensor | None = None, advance: bool = True, stream=None) -> None:
+    """gp_append_rope with a rotation of the caller's."""
+    _append_rope("gp_append_rotary", kv, kv.k.dtype, ps, positions, k_new, v_new, 0.0, q, q_out, tok_start, advance,
+                 stream, rope)
+
+
+def gp_append_rotary_q8(kv: KV8Layer, ps: PageState, positions: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                        rope: Rope, q: torch.Tensor | None = None, q_out: torch.Tensor | None = None,
+                        tok_start: torch.Tensor | None = None, advance: bool = True, stream=None) -> None:
+    """gp_append_rotary into an 8-bit cache (rows bfloat16)."""
+    _append_rope("gp_append_rotary_q8", kv, torch.bfloat16, ps, positions, k_new, v_new, 0.0, q, q_out, tok_start,
+                 advance, stream, rope)
+
+
+def gp_boundary_score_rotary(kv: KVLayer, ps: PageState, q_pre: torch.Tensor, qstate: torch.Tensor, slot_ids: torch.Tensor,
+                             positions: torch.Tensor, bnd: torch.Tensor, params: Params, rope: Rope, k_counts: torch.Tensor,
+                             scores: torch.Tensor, ws: torch.Tensor, stream=None,
+                             stages: int = GP_SCORE_WEIGHTS | GP_SCORE_COUNTS) -> None:
+    """gp_boundary_score of a cache written by gp_append_rotary with the same rope."""
+    c_kv, c_ps, c_p = kv.c(), ps.c(), params.c()
+    _on_device("gp_boundary_score_rotary", kv, ps, q_pre, qstate, slot_ids, positions, bnd, k_counts, scores, ws)
+    _check(load().gp_boundary_score_rotary(
+        ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(q_pre), _ptr(qstate), qstate.shape[0], _ptr(slot_ids), _ptr(positions),
+        _ptr(bnd), bnd.shape[0], q_pre.shape[1], ctypes.byref(c_p), ctypes.byref(rope._c), _ptr(k_counts), _ptr(scores),
+        scores.shape[-1], _ptr(ws), ws.numel(), _stream(stream), stages), "gp_boundary_score_rotary")
 
 
 def _of(t: torch.Tensor, dtype, name: str) -> int:
@@ -579,3 +672,61 @@ def gp_decode_attention_pages_q8(kv: KV8Layer, ps: PageState, selected: torch.Te
                                  scale: float, out: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
     """gp_decode_attention_pages over an 8-bit cache; q_post and out bfloat16."""
     _decode_pages("gp_decode_attention_pages_q8", kv, torch.bfloat16, ps, selected, q_post, scale, out, ws, stream)
+
+
+def _pages(name: str, ps: PageState, **tensors) -> _PageState:
+    c_ps = ps.c()
+    for key, t in tensors.items():
+        if t is not None and t.dtype != torch.int32:
+            raise ValueError(f"{name}: {key} int32")
+    _on_device(name, None, ps, ps.refcount, ps.free_list, ps.free_count, *tensors.values())
+    if ps.free_list.shape[0] < c_ps.pool_pages:
+        raise ValueError(f"{name}: free_list [pool_pages]")
+    return c_ps
+
+
+def gp_pages_reserve(ps: PageState, tokens: torch.Tensor, granted: torch.Tensor, keep_free: int = 0, stream=None) -> None:
+    """Pages for tokens[r] more tokens of each request, off the free stack in the order of the
+    requests; granted[r] 1 or 0 (both int32 [R])."""
+    c_ps = _pages("gp_pages_reserve", ps, tokens=tokens, granted=granted)
+    if tokens.numel() != c_ps.num_reqs or granted.numel() != c_ps.num_reqs:
+        raise ValueError("gp_pages_reserve: tokens and granted [num_reqs]")
+    _check(load().gp_pages_reserve(ctypes.byref(c_ps), _ptr(tokens), keep_free, _ptr(granted), _stream(stream)),
+           "gp_pages_reserve")
+
+
+def _pages_fork(name, q8, layers, ps, parents, children, forked, lengths, positions, stream):
+    if not isinstance(layers, Layers):
+        layers = Layers(layers)
+    c_ps = _pages(name, ps, parents=parents, children=children, forked=forked, lengths=lengths, positions=positions)
+    n = parents.numel()
+    if layers.q8 != q8:
+        raise ValueError(f"{name}: layers of {'8-bit' if q8 else 'bfloat16 or float32'} pools")
+    if children.numel() != n or forked.numel() != n or (lengths is not None and lengths.numel() != n):
+        raise ValueError(f"{name}: parents, children, lengths and forked of one size")
+    if positions is not None and positions.numel() < c_ps.num_reqs:
+        raise ValueError(f"{name}: positions [num_reqs]")
+    if layers._device != ps.page_table.get_device():
+        raise ValueError(f"{name}: tensors on different devices")
+    _check(getattr(load(), name)(layers._c, len(layers), ctypes.byref(c_ps), _ptr(parents), _ptr(children), _ptr(lengths), n,
+                                 _ptr(positions), _ptr(forked), _stream(stream)), name)
+
+
+def gp_pages_fork(layers, ps: PageState, parents: torch.Tensor, children: torch.Tensor, forked: torch.Tensor,
+                  lengths: torch.Tensor | None = None, positions: torch.Tensor | None = None, stream=None) -> None:
+    """Rows children[i] continue rows parents[i] (lengths[i] of their tokens, or all): whole pages
+    shared, the rows of the last one copied on every layer; forked[i] 1 or 0.  layers: a Layers,
+    or a list of KVLayer."""
+    _pages_fork("gp_pages_fork", False, layers, ps, parents, children, forked, lengths, positions, stream)
+
+
+def gp_pages_fork_q8(layers, ps: PageState, parents: torch.Tensor, children: torch.Tensor, forked: torch.Tensor,
+                     lengths: torch.Tensor | None = None, positions: torch.Tensor | None = None, stream=None) -> None:
+    """gp_pages_fork of an 8-bit cache (a Layers, or a list of KV8Layer)."""
+    _pages_fork("gp_pages_fork_q8", True, layers, ps, parents, children, forked, lengths, positions, stream)
+
+
+def gp_pages_release(ps: PageState, reqs: torch.Tensor, stream=None) -> None:
+    """The rows listed give up their pages, which go back to the free stack when nobody else holds them."""
+    c_ps = _pages("gp_pages_release", ps, reqs=reqs)
+    _check(load().gp_pages_release(ctypes.byref(c_ps), _ptr(reqs), reqs.numel(), _stream(stream)), "gp_pages_release")

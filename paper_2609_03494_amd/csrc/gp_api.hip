@@ -84,6 +84,59 @@ gp_status_t from_hip(hipError_t e) { return e == hipSuccess ? GP_OK : GP_ERR_HIP
 
 int elem_bytes(gp_dtype_t dt) { return dt == GP_F32 ? 4 : 2; }
 
+// What the three calls on pages have in common.
+gp_status_t pages_args(const gp_page_state_t *ps, PagesArgs *a) {
+    const gp_status_t st = check_state(ps, nullptr);
+    if (st != GP_OK) return st;
+    if (!ps->refcount || !ps->free_list || !ps->free_count || ps->pool_pages <= 0) return GP_ERR_INVALID;
+    if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages) return GP_ERR_UNSUPPORTED;
+    *a = {};
+    a->page_table = ps->page_table;
+    a->num_pages = ps->num_pages;
+    a->seq_lens = ps->seq_lens;
+    a->refcount = ps->refcount;
+    a->free_list = ps->free_list;
+    a->free_count = ps->free_count;
+    a->R = ps->num_reqs;
+    a->max_pages = ps->max_pages;
+    a->pool_pages = ps->pool_pages;
+    return GP_OK;
+}
+
+// `layer(l, &as)`: layer l as the checks take layers, after its own checks.
+template <typename Check, typename Put>
+gp_status_t fork_call(int32_t n_layers, const gp_page_state_t *ps, const int32_t *parents, const int32_t *children,
+                      const int32_t *lengths, int32_t num_forks, int32_t *positions, int32_t *forked, int elem,
+                      hipStream_t stream, Check layer, Put put) {
+    if (n_layers <= 0 || num_forks < 0) return GP_ERR_INVALID;
+    if (n_layers > kMaxForkLayers) return GP_ERR_UNSUPPORTED;
+    PagesArgs a;
+    gp_status_t st;
+    gp_kv_layer_t first, as;
+    if ((st = layer(0, &first)) != GP_OK || (st = check_state(ps, &first)) != GP_OK) return st;
+    for (int l = 0; l < n_layers; ++l) {
+        if ((st = layer(l, &as)) != GP_OK) return st;
+        if (!aligned16(as.k, as.v) || as.pool_pages != first.pool_pages || as.num_kv_heads != first.num_kv_heads ||
+            as.head_dim != first.head_dim || as.dtype != first.dtype)
+            return GP_ERR_INVALID;
+    }
+    if ((st = pages_args(ps, &a)) != GP_OK) return st;
+    if (num_forks == 0 || ps->num_reqs == 0) return GP_OK;
+    if (!parents || !children || !forked) return GP_ERR_INVALID;
+    if (num_forks > kMaxForks || first.num_kv_heads > kMaxListedHeads) return GP_ERR_UNSUPPORTED;
+    a.reqs = parents;
+    a.children = children;
+    a.lengths = lengths;
+    a.n = num_forks;
+    a.positions = positions;
+    a.flags = forked;
+    a.Hkv = first.num_kv_heads;
+    a.row_bytes = first.head_dim * (elem ? elem : elem_bytes(first.dtype));
+    PageLayers p[kMaxForkLayers / kMaxLayers] = {};
+    for (int l = 0; l < n_layers; ++l) put(l, p[l / kMaxLayers], l % kMaxLayers);
+    return from_hip(launch_fork(a, p, n_layers, stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -368,8 +421,20 @@ bool overlap(const void *p, int64_t n, const void *q, int64_t m, int e) {
     return a < b + (uintptr_t)m * e && b < a + (uintptr_t)n * e;
 }
 
+// What a rotation has to be (d: head_dim).
+gp_status_t check_rope(const gp_rope_t *rope, int d) {
+    if (!rope || (rope->layout != GP_ROPE_HALF && rope->layout != GP_ROPE_INTERLEAVED)) return GP_ERR_INVALID;
+    if (rope->rotary_dim < 2 || rope->rotary_dim > d) return GP_ERR_INVALID;
+    if (rope->rotary_dim % 16) return GP_ERR_UNSUPPORTED;
+    if (!(rope->magnitude > 0.0f) || !isfinite(rope->magnitude)) return GP_ERR_INVALID;
+    for (int i = 0; i < rope->rotary_dim / 2; ++i)
+        if (!isfinite(rope->freq[i])) return GP_ERR_INVALID;
+    return GP_OK;
+}
+
+// rope: the rotation (nullptr: half-split pairs of the whole head at rope_theta).
 gp_status_t rope_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, const gp_page_state_t *ps,
-                      int32_t *positions, const int32_t *tok_start, int32_t num_tokens, const void *q,
+                      const gp_rope_t *rope, int32_t *positions, const int32_t *tok_start, int32_t num_tokens, const void *q,
                       int64_t q_stride, void *q_out, const void *k_new, int64_t k_stride, const void *v_new,
                       int64_t v_stride, int32_t num_q_heads, float rope_theta, int32_t advance,
                       hipStream_t stream) {
@@ -377,6 +442,7 @@ gp_status_t rope_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, const 
     if (st != GP_OK) return st;
     if ((st = check_state(ps, kv)) != GP_OK) return st;
     if (!(rope_theta > 0.0f) || !isfinite(rope_theta) || num_tokens < 0) return GP_ERR_INVALID;
+    if (rope && (st = check_rope(rope, kv->head_dim)) != GP_OK) return st;
     if (!tok_start && num_tokens != ps->num_reqs) return GP_ERR_INVALID;
     if (q && !dims_ok(num_q_heads, kv->num_kv_heads, kv->head_dim)) return GP_ERR_UNSUPPORTED;
     const int64_t row = (int64_t)kv->num_kv_heads * kv->head_dim, qrow = (int64_t)num_q_heads * kv->head_dim;
@@ -419,10 +485,19 @@ gp_status_t rope_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, const 
     a.Hkv = kv->num_kv_heads;
     a.max_pages = ps->max_pages;
     a.pool_pages = kv->pool_pages;
+    constexpr long double kTurn = 0.159154943091895335768883763372514362L;    // 1 / (2 pi)
+    a.layout = -1;
+    if (rope) {
+        a.layout = rope->layout;
+        a.half = rope->rotary_dim / 2;
+        a.magnitude = rope->magnitude;
+        for (int i = 0; i < a.half; ++i) a.turns[i] = (double)(kTurn * rope->freq[i]);
+        return from_hip(launch_rope(kv8 ? 1 : e, kv->head_dim, a, advance != 0, stream));
+    }
     // one power, the others by products in extended precision: 64 powers took the
     // host longer than the launch
     const long double step = powl((long double)rope_theta, -2.0L / kv->head_dim);
-    long double f = 0.159154943091895335768883763372514362L;              // 1 / (2 pi)
+    long double f = kTurn;
     for (int i = 0; i < kv->head_dim / 2; ++i, f *= step) a.turns[i] = (double)f;
     return from_hip(launch_rope(kv8 ? 1 : e, kv->head_dim, a, advance != 0, stream));
 }
@@ -460,7 +535,7 @@ gp_status_t gp_append_rope(const gp_kv_layer_t *kv, const gp_page_state_t *ps, i
                            void *q_out, const void *k_new, int64_t k_stride, const void *v_new,
                            int64_t v_stride, int32_t num_q_heads, float rope_theta, int32_t advance,
                            hipStream_t stream) {
-    return rope_call(kv, nullptr, ps, positions, tok_start, num_tokens, q, q_stride, q_out, k_new, k_stride, v_new,
+    return rope_call(kv, nullptr, ps, nullptr, positions, tok_start, num_tokens, q, q_stride, q_out, k_new, k_stride, v_new,
                      v_stride, num_q_heads, rope_theta, advance, stream);
 }
 
@@ -472,8 +547,51 @@ gp_status_t gp_append_rope_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *p
     gp_kv_layer_t as;
     const gp_status_t st = check_layer8(kv, &as);
     if (st != GP_OK) return st;
-    return rope_call(&as, kv, ps, positions, tok_start, num_tokens, q, q_stride, q_out, k_new, k_stride, v_new,
+    return rope_call(&as, kv, ps, nullptr, positions, tok_start, num_tokens, q, q_stride, q_out, k_new, k_stride, v_new,
                      v_stride, num_q_heads, rope_theta, advance, stream);
+}
+
+gp_status_t gp_rope_frequencies(double *freq, int32_t rotary_dim, double theta, double factor, double low_turns,
+                                double high_turns, double context) {
+    if (!freq || rotary_dim < 2 || rotary_dim > 128 || rotary_dim % 2) return GP_ERR_INVALID;
+    if (!(theta > 0.0) || !isfinite(theta) || !(factor >= 1.0) || !isfinite(factor)) return GP_ERR_INVALID;
+    const bool by_turns = high_turns != 0.0;
+    if (by_turns && (!(low_turns >= 0.0) || !(high_turns > low_turns) || !isfinite(high_turns) || !(context > 0.0) ||
+                     !isfinite(context)))
+        return GP_ERR_INVALID;
+    const long double two_pi = 6.283185307179586476925286766559005768L;
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        const long double f = powl((long double)theta, -2.0L * i / rotary_dim);
+        long double keep = 0.0L;
+        if (by_turns) {
+            keep = (context * f / two_pi - low_turns) / ((long double)high_turns - low_turns);
+            keep = std::min(1.0L, std::max(0.0L, keep));
+        }
+        freq[i] = (double)(f * (keep + (1.0L - keep) / factor));
+    }
+    return GP_OK;
+}
+
+gp_status_t gp_append_rotary(const gp_kv_layer_t *kv, const gp_page_state_t *ps, int32_t *positions,
+                             const gp_rope_t *rope, const int32_t *tok_start, int32_t num_tokens, const void *q,
+                             int64_t q_stride, void *q_out, const void *k_new, int64_t k_stride, const void *v_new,
+                             int64_t v_stride, int32_t num_q_heads, int32_t advance, hipStream_t stream) {
+    if (!rope) return GP_ERR_INVALID;
+    return rope_call(kv, nullptr, ps, rope, positions, tok_start, num_tokens, q, q_stride, q_out, k_new, k_stride,
+                     v_new, v_stride, num_q_heads, 1.0f, advance, stream);
+}
+
+gp_status_t gp_append_rotary_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps, int32_t *positions,
+                                const gp_rope_t *rope, const int32_t *tok_start, int32_t num_tokens, const void *q,
+                                int64_t q_stride, void *q_out, const void *k_new, int64_t k_stride,
+                                const void *v_new, int64_t v_stride, int32_t num_q_heads, int32_t advance,
+                                hipStream_t stream) {
+    gp_kv_layer_t as;
+    const gp_status_t st = check_layer8(kv, &as);
+    if (st != GP_OK) return st;
+    if (!rope) return GP_ERR_INVALID;
+    return rope_call(&as, kv, ps, rope, positions, tok_start, num_tokens, q, q_stride, q_out, k_new, k_stride,
+                     v_new, v_stride, num_q_heads, 1.0f, advance, stream);
 }
 
 gp_status_t gp_page_bounds(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const int32_t *from_tokens,
@@ -522,24 +640,27 @@ gp_status_t gp_select_pages(const void *bounds, gp_dtype_t dtype, const gp_page_
     return from_hip(launch_select(dtype, head_dim, num_q_heads / num_kv_heads, a, stream));
 }
 
-gp_status_t gp_boundary_score_stages(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const void *q_pre,
-                                     const float *qstate, int32_t num_slots, const int32_t *slot_ids,
-                                     const int32_t *positions, const int32_t *bnd, int32_t num_bnd,
-                                     int32_t num_q_heads, const gp_params_t *params, int32_t *k_counts,
-                                     float *scores, int32_t max_cand, void *ws, size_t ws_bytes,
-                                     hipStream_t stream, int32_t stages) {
+namespace {
+
+// rope: the rotation (nullptr: half-split pairs at params->rope_theta).
+gp_status_t score_call(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const void *q_pre, const float *qstate,
+                       int32_t num_slots, const int32_t *slot_ids, const int32_t *positions, const int32_t *bnd,
+                       int32_t num_bnd, int32_t num_q_heads, const gp_params_t *params, const gp_rope_t *rope,
+                       int32_t *k_counts, float *scores, int32_t max_cand, void *ws, size_t ws_bytes,
+                       hipStream_t stream, int32_t stages) {
     if (stages <= 0 || (stages & ~(GP_SCORE_WEIGHTS | GP_SCORE_COUNTS)) != 0) return GP_ERR_INVALID;
     gp_status_t st = check_layer(kv);
     if (st != GP_OK) return st;
     if ((st = check_state(ps, kv)) != GP_OK) return st;
     if (!dims_ok(num_q_heads, kv->num_kv_heads, kv->head_dim)) return GP_ERR_UNSUPPORTED;
     if (!params || num_bnd < 0 || num_slots <= 0) return GP_ERR_INVALID;
+    if (rope && (st = check_rope(rope, kv->head_dim)) != GP_OK) return st;
     if (num_bnd == 0) return GP_OK;
     if (!q_pre || !qstate || !slot_ids || !positions || !bnd || !k_counts || !scores || !ws)
         return GP_ERR_INVALID;
     if (max_cand < (ps->max_pages - 1) * kPage) return GP_ERR_INVALID;
     if (!(params->p > 0.0f && params->p <= 1.0f) || !(params->scale > 0.0f) ||
-        !(params->rope_theta > 0.0f))
+        (!rope && !(params->rope_theta > 0.0f)))
         return GP_ERR_INVALID;
     if (params->metric != GP_METRIC_TOP_P && params->metric != GP_METRIC_ENTROPY) return GP_ERR_INVALID;
     if (num_bnd > 65535 || ps->max_pages > kMaxBoundaryPages) return GP_ERR_UNSUPPORTED;
@@ -576,7 +697,30 @@ gp_status_t gp_boundary_score_stages(const gp_kv_layer_t *kv, const gp_page_stat
     a.theta = params->rope_theta;
     a.p = params->p;
     a.metric = params->metric;
-    return from_hip(launch_score(kv->dtype, kv->head_dim, num_q_heads / kv->num_kv_heads, a, stages, stream));
+    return from_hip(launch_score(kv->dtype, kv->head_dim, num_q_heads / kv->num_kv_heads, a, rope, stages, stream));
+}
+
+}  // namespace
+
+gp_status_t gp_boundary_score_stages(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const void *q_pre,
+                                     const float *qstate, int32_t num_slots, const int32_t *slot_ids,
+                                     const int32_t *positions, const int32_t *bnd, int32_t num_bnd,
+                                     int32_t num_q_heads, const gp_params_t *params, int32_t *k_counts,
+                                     float *scores, int32_t max_cand, void *ws, size_t ws_bytes,
+                                     hipStream_t stream, int32_t stages) {
+    return score_call(kv, ps, q_pre, qstate, num_slots, slot_ids, positions, bnd, num_bnd, num_q_heads, params, nullptr,
+                      k_counts, scores, max_cand, ws, ws_bytes, stream, stages);
+}
+
+gp_status_t gp_boundary_score_rotary(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const void *q_pre,
+                                     const float *qstate, int32_t num_slots, const int32_t *slot_ids,
+                                     const int32_t *positions, const int32_t *bnd, int32_t num_bnd,
+                                     int32_t num_q_heads, const gp_params_t *params, const gp_rope_t *rope,
+                                     int32_t *k_counts, float *scores, int32_t max_cand, void *ws, size_t ws_bytes,
+                                     hipStream_t stream, int32_t stages) {
+    if (!rope) return GP_ERR_INVALID;
+    return score_call(kv, ps, q_pre, qstate, num_slots, slot_ids, positions, bnd, num_bnd, num_q_heads, params, rope,
+                      k_counts, scores, max_cand, ws, ws_bytes, stream, stages);
 }
 
 gp_status_t gp_boundary_score(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const void *q_pre,
@@ -749,6 +893,65 @@ gp_status_t gp_release_held(const gp_page_state_t *ps, hipStream_t stream) {
     if (!ps || !ps->seq_lens || ps->num_reqs < 0) return GP_ERR_INVALID;
     if (ps->num_reqs == 0) return GP_OK;
     return from_hip(launch_release(ps->seq_lens, ps->num_reqs, stream));
+}
+
+gp_status_t gp_pages_reserve(const gp_page_state_t *ps, const int32_t *tokens, int32_t keep_free, int32_t *granted,
+                             hipStream_t stream) {
+    PagesArgs a;
+    const gp_status_t st = pages_args(ps, &a);
+    if (st != GP_OK) return st;
+    if (keep_free < 0) return GP_ERR_INVALID;
+    if (ps->num_reqs == 0) return GP_OK;
+    if (!tokens || !granted) return GP_ERR_INVALID;
+    a.tokens = tokens;
+    a.flags = granted;
+    a.keep_free = keep_free;
+    return from_hip(launch_reserve(a, stream));
+}
+
+gp_status_t gp_pages_release(const gp_page_state_t *ps, const int32_t *reqs, int32_t num, hipStream_t stream) {
+    PagesArgs a;
+    const gp_status_t st = pages_args(ps, &a);
+    if (st != GP_OK) return st;
+    if (num < 0) return GP_ERR_INVALID;
+    if (num == 0 || ps->num_reqs == 0) return GP_OK;
+    if (!reqs) return GP_ERR_INVALID;
+    // (more than each request once is no use; it keeps the sums of pages within 32 bits)
+    if (num > 65535) return GP_ERR_UNSUPPORTED;
+    a.reqs = reqs;
+    a.n = num;
+    return from_hip(launch_pages_release(a, stream));
+}
+
+gp_status_t gp_pages_fork(const gp_kv_layer_t *layers, int32_t n_layers, const gp_page_state_t *ps,
+                          const int32_t *parents, const int32_t *children, const int32_t *lengths, int32_t num_forks,
+                          int32_t *positions, int32_t *forked, hipStream_t stream) {
+    if (!layers) return GP_ERR_INVALID;
+    return fork_call(
+        n_layers, ps, parents, children, lengths, num_forks, positions, forked, 0, stream,
+        [&](int l, gp_kv_layer_t *as) {
+            *as = layers[l];
+            return check_layer(as);
+        },
+        [&](int l, PageLayers &p, int at) {
+            p.k[at] = layers[l].k;
+            p.v[at] = layers[l].v;
+        });
+}
+
+gp_status_t gp_pages_fork_q8(const gp_kv8_layer_t *layers, int32_t n_layers, const gp_page_state_t *ps,
+                             const int32_t *parents, const int32_t *children, const int32_t *lengths,
+                             int32_t num_forks, int32_t *positions, int32_t *forked, hipStream_t stream) {
+    if (!layers) return GP_ERR_INVALID;
+    return fork_call(
+        n_layers, ps, parents, children, lengths, num_forks, positions, forked, 1, stream,
+        [&](int l, gp_kv_layer_t *as) { return check_layer8(&layers[l], as); },
+        [&](int l, PageLayers &p, int at) {
+            p.k[at] = layers[l].k;
+            p.v[at] = layers[l].v;
+            p.k_scale[at] = layers[l].k_scale;
+            p.v_scale[at] = layers[l].v_scale;
+        });
 }
 
 }  // extern "C"

@@ -46,6 +46,8 @@ constexpr int kStatBlock = 64;            // candidate tokens per softmax-statis
 constexpr int kProbChunk = 1024;          // tokens per weight/score work item
 constexpr int kCompactChunk = 256;        // slots per compaction work item
 constexpr int kMaxLayers = 64;            // layers one gp_boundary_apply call can take
+constexpr int kMaxForks = 2048;           // forks one gp_pages_fork call takes,
+constexpr int kMaxForkLayers = 4 * kMaxLayers;   // over at most so many layers
 constexpr size_t kAlign = 256;
 
 __host__ __device__ inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
@@ -316,6 +318,9 @@ struct RopeArgs {
     int64_t q_stride, k_stride, v_stride;   // elements from token to token
     int R, T, Hq, Hkv, max_pages, pool_pages;
     double turns[64];                 // theta^(-2 i / d) / (2 pi): turns per position of rotary pair i
+    // gp_append_rotary: pairing (-1: half-split over the whole head), rotary pairs, factor on cosine and sine
+    int layout, half;
+    double magnitude;
 };
 
 struct BoundsArgs {
@@ -379,6 +384,21 @@ struct LayerPtrs {
     void *k, *v;
 };
 
+// gp_pages_reserve, gp_pages_fork and gp_pages_release.
+struct PagesArgs {
+    int32_t *page_table, *num_pages, *seq_lens, *refcount, *free_list, *free_count;
+    int32_t *positions;               // fork: may be nullptr
+    const int32_t *tokens;            // reserve: [R]
+    const int32_t *reqs, *children;   // release: requests; fork: parents and children, [n]
+    const int32_t *lengths;           // fork: tokens to take, [n] (nullptr: all)
+    int32_t *flags;                   // reserve: granted [R]; fork: forked [n]
+    int R, n, max_pages, pool_pages, keep_free, n_layers, Hkv, row_bytes;
+};
+struct PageLayers {
+    void *k[kMaxLayers], *v[kMaxLayers];
+    float *k_scale[kMaxLayers], *v_scale[kMaxLayers];   // 8-bit pools
+};
+
 // ---------------------------------------------------------------- launchers --
 
 hipError_t launch_summaries(gp_dtype_t dt, const SummaryArgs &a, hipStream_t s);
@@ -390,13 +410,18 @@ hipError_t launch_decode_pages(gp_dtype_t dt, int D, int G, const DecodeArgs &a,
 hipError_t launch_rope(int cache, int D, const RopeArgs &a, bool advance, hipStream_t s);
 hipError_t launch_bounds(int cache, int D, const BoundsArgs &a, hipStream_t s);
 hipError_t launch_select(gp_dtype_t dt, int D, int G, const SelectArgs &a, hipStream_t s);
-hipError_t launch_score(gp_dtype_t dt, int D, int G, const ScoreArgs &a, int stages, hipStream_t s);
+// rope: nullptr: half-split pairs at a.theta
+hipError_t launch_score(gp_dtype_t dt, int D, int G, const ScoreArgs &a, const gp_rope_t *rope, int stages, hipStream_t s);
 // Stages of the boundary apply (selection, decision, compaction).
 constexpr int kStageSelect = 1, kStageDecide = 2, kStageCompact = 4;
 
 hipError_t launch_apply(gp_dtype_t dt, int D, const ApplyArgs &a, const LayerPtrs *layers, int stages,
                         hipStream_t s);
 hipError_t launch_release(int32_t *seq_lens, int R, hipStream_t s);
+hipError_t launch_reserve(const PagesArgs &a, hipStream_t s);
+hipError_t launch_pages_release(const PagesArgs &a, hipStream_t s);
+// layers: kMaxLayers of them in each PageLayers but the last
+hipError_t launch_fork(const PagesArgs &a, const PageLayers *layers, int n_layers, hipStream_t s);
 hipError_t launch_stream_read(const void *src, size_t bytes, uint32_t *out, hipStream_t s);
 
 // ---------------------------------------------------------- device helpers --

@@ -78,6 +78,11 @@ __device__ inline u32x4_t narrow(const float (&x)[4]) {
     return u;
 }
 
+// Where the pairs of a row lie: over the whole head, half a head apart (as
+// gp_append_rope has them), or as a gp_rope_t says: in the first 2 `half` dims, half of
+// them apart or side by side.
+enum { kWhole = 0, kPart = 1, kBeside = 2 };
+
 // one rotary pair, products and sums rounded one at a time
 __device__ inline void rotate(float &a, float &b, const float2 &cs) {
 #pragma clang fp contract(off)
@@ -146,8 +151,8 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kBatch = 4;                             // row pieces in flight per thread
 
 // CACHE: bytes of a pool element.  STREAM: the call moves more than the last-level
-// cache holds (see launch_cd).
-template <int CACHE, int D, bool STREAM>
+// cache holds (see launch_form).  FORM: kWhole, kPart, kBeside.
+template <int CACHE, int D, bool STREAM, int FORM>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     using E = typename std::conditional<CACHE == 4, float, uint16_t>::type;
     constexpr int EPU = 16 / (int)sizeof(E);          // elements per 16 bytes
@@ -174,21 +179,31 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
         if (pid < 0 || pid >= a.pool_pages) pid = -1;
     }
     const double pos = (double)a.positions[r] + 1.0 + first;
-    for (int i = tid; i < rows * H; i += kThreads) {
-        const double t = (pos + i / H) * a.turns[i % H];
+    const int half = FORM == kWhole ? H : a.half;     // rotary pairs
+    for (int i = tid; i < rows * half; i += kThreads) {
+        const int k = i / half, pair = i - k * half;
+        const double t = (pos + k) * a.turns[pair];
         double s, c;
         sincospi(2.0 * (t - rint(t)), &s, &c);
-        s_cs[i / H][i % H] = make_float2((float)c, (float)s);
+        if (FORM != kWhole) {
+            s *= a.magnitude;
+            c *= a.magnitude;
+        }
+        s_cs[k][pair] = make_float2((float)c, (float)s);
     }
     __syncthreads();
 
     // rows that go out in their own type, in pieces of two 16-byte units that
-    // rotate into each other: the queries, and the keys and values of such a pool
+    // rotate into each other (side by side: each in itself): the queries, and the keys and
+    // values of such a pool.  Behind the rotated part units go out as they came, by twos.
     {
         const int kv = CACHE == 1 || pid < 0 ? 0 : a.Hkv;
         const int heads = a.Hq + 2 * kv, total = rows * heads;
         constexpr int GROUPS = kThreads / UPH;        // threads of one row and head
-        const int u = tid % UPH;
+        const int u = tid % UPH, hu = half / EPU;
+        const bool inside = FORM == kWhole || u < hu;     // (side by side: units 2 u and 2 u + 1, of 2 hu rotated ones)
+        const int at0 = (FORM == kWhole || (FORM == kPart && inside) ? u : 2 * u) * EPU;
+        const int at1 = FORM == kWhole ? at0 + H : FORM == kPart && inside ? at0 + half : at0 + EPU;
         for (int x0 = tid / UPH + GROUPS * kBatch * (int)blockIdx.y; x0 < total; x0 += GROUPS * kBatch * (int)gridDim.y) {
             u32x4_t p[kBatch], q[kBatch];
             E *to[kBatch];
@@ -201,7 +216,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                 const int hh = x - row[k] * heads;
                 const int64_t t = tok + row[k];
                 const E *src;
-                turn[k] = true;
+                turn[k] = inside;
                 if (hh < a.Hq) {
                     src = reinterpret_cast<const E *>(a.q) + t * a.q_stride + (int64_t)hh * D;
                     to[k] = reinterpret_cast<E *>(a.q_out) + (t * a.Hq + hh) * D;
@@ -210,10 +225,10 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                     const int h = hh - a.Hq - (isv ? kv : 0);
                     src = reinterpret_cast<const E *>(isv ? a.v_new : a.k_new) + t * (isv ? a.v_stride : a.k_stride) + (int64_t)h * D;
                     to[k] = reinterpret_cast<E *>(isv ? a.v : a.k) + (((size_t)pid * a.Hkv + h) * kPage + lo + row[k]) * D;
-                    turn[k] = !isv;
+                    turn[k] = inside && !isv;
                 }
-                p[k] = load16<STREAM>(src + u * EPU);
-                q[k] = load16<STREAM>(src + H + u * EPU);
+                p[k] = load16<STREAM>(src + at0);
+                q[k] = load16<STREAM>(src + at1);
             }
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
@@ -222,13 +237,21 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                     float xa[EPU], xb[EPU];
                     widen(p[k], xa);
                     widen(q[k], xb);
+                    if constexpr (FORM == kBeside) {
 #pragma unroll
-                    for (int e = 0; e < EPU; ++e) rotate(xa[e], xb[e], s_cs[row[k]][u * EPU + e]);
+                        for (int e = 0; e < EPU; e += 2) {
+                            rotate(xa[e], xa[e + 1], s_cs[row[k]][u * EPU + e / 2]);
+                            rotate(xb[e], xb[e + 1], s_cs[row[k]][u * EPU + (EPU + e) / 2]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < EPU; ++e) rotate(xa[e], xb[e], s_cs[row[k]][u * EPU + e]);
+                    }
                     p[k] = narrow(xa);
                     q[k] = narrow(xb);
                 }
-                store16<STREAM>(to[k] + u * EPU, p[k]);
-                store16<STREAM>(to[k] + H + u * EPU, q[k]);
+                store16<STREAM>(to[k] + at0, p[k]);
+                store16<STREAM>(to[k] + at1, q[k]);
             }
         }
     }
@@ -253,8 +276,35 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                 for (int c = 0; c < EH; c += 8)
                     widen(load16<STREAM>(src + half * H + c), reinterpret_cast<float(&)[8]>(x[half][c]));
             if (!isv) {
+                if constexpr (FORM == kWhole) {
 #pragma unroll
-                for (int e = 0; e < EH; ++e) rotate(x[0][e], x[1][e], s_cs[rr][sub * EH + e]);
+                    for (int e = 0; e < EH; ++e) rotate(x[0][e], x[1][e], s_cs[rr][sub * EH + e]);
+                } else {
+#pragma unroll
+                    for (int part = 0; part < 2; ++part)
+#pragma unroll
+                        for (int c = 0; c < EH; c += 8) {
+                            const int at = part * H + sub * EH + c;       // the dims of these eight
+                            if (at >= 2 * half) continue;
+                            float *y = x[part] + c;
+                            if constexpr (FORM == kBeside) {
+#pragma unroll
+                                for (int e = 0; e < 8; e += 2) rotate(y[e], y[e + 1], s_cs[rr][(at + e) / 2]);
+                            } else {
+                                // their partners, which another lane may hold, once more from memory
+                                const bool low = at < half;
+                                float z[8];
+                                widen(load16<STREAM>(src - sub * EH + (low ? at + half : at - half)), z);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    const float2 cs = s_cs[rr][(low ? at : at - half) + e];
+                                    float lo_ = low ? y[e] : z[e], hi_ = low ? z[e] : y[e];
+                                    rotate(lo_, hi_, cs);
+                                    y[e] = low ? lo_ : hi_;
+                                }
+                            }
+                        }
+                }
             }
             float *sp = (isv ? a.v_scale : a.k_scale) + (size_t)pid * a.Hkv + h;
             float old = lo > 0 ? *sp : 0.0f;          // the page held tokens before (wave-uniform; requested with the rows)
@@ -315,8 +365,8 @@ __global__ __launch_bounds__(256) void rope_advance_kernel(RopeArgs a) {
     a.positions[r] += b.n;
 }
 
-template <int CACHE, int D>
-void launch_cd(const RopeArgs &a, hipStream_t s) {
+template <int CACHE, int D, int FORM>
+void launch_form(const RopeArgs &a, hipStream_t s) {
     const int items = a.start ? a.T / kPage + 2 * a.R : a.R;
     // heads split so that about 1024 workgroups are there, as long as each has a batch of
     // pieces per thread or, in 8 bits, one job per wave
@@ -328,8 +378,15 @@ void launch_cd(const RopeArgs &a, hipStream_t s) {
     // 146 -> 135.  Smaller calls leave the queries there for the attention that follows.
     const int64_t row = (int64_t)D * (CACHE == 4 ? 4 : 2), bytes = a.T * row * (2 * a.Hq + 3 * a.Hkv);
     const dim3 grid(items, split);
-    if (bytes > (int64_t)256 << 20) rope_kernel<CACHE, D, true><<<grid, kThreads, 0, s>>>(a);
-    else rope_kernel<CACHE, D, false><<<grid, kThreads, 0, s>>>(a);
+    if (bytes > (int64_t)256 << 20) rope_kernel<CACHE, D, true, FORM><<<grid, kThreads, 0, s>>>(a);
+    else rope_kernel<CACHE, D, false, FORM><<<grid, kThreads, 0, s>>>(a);
+}
+
+template <int CACHE, int D>
+void launch_cd(const RopeArgs &a, hipStream_t s) {
+    if (a.layout < 0) launch_form<CACHE, D, kWhole>(a, s);
+    else if (a.layout == GP_ROPE_HALF) launch_form<CACHE, D, kPart>(a, s);
+    else launch_form<CACHE, D, kBeside>(a, s);
 }
 
 }  // namespace

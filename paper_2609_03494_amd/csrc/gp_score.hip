@@ -23,6 +23,9 @@
 // Bound: the key read (|C| * d * sizeof(elem) per KV head) plus 2G float32
 // exponentials written and read back; kernel 0 does 2G fp64 FMAs per key
 // element.
+#include <algorithm>
+#include <type_traits>
+
 #include "gp_internal.h"
 
 namespace gp {
@@ -163,8 +166,24 @@ constexpr int kLogitsWaves = GP_LOGITS_WAVES;   // waves per workgroup, sharing 
 #define GP_LOGITS_TARGET_WAVES 16384
 #endif
 
-template <typename T, int D, int G>
-__global__ __launch_bounds__(64 * kLogitsWaves) void logits_kernel(ScoreArgs a) {
+// How the summaries turn: half-split pairs at theta^(-2k/D), or as a gp_rope_t says
+// (pairs behind the rotated part: an angle of zero).
+struct ThetaForm {
+    template <int D>
+    __device__ static int dim(int k, int second) { return k + second * (D / 2); }
+};
+struct TableForm {
+    double freq[64], magnitude;
+    int half, interleaved;            // rotary pairs; pairing
+    template <int D>
+    __device__ int dim(int k, int second) const {
+        if (!interleaved && k < half) return k + second * half;
+        return 2 * k + second;        // (half-split: 2 half + 2 (k - half), side by side as well)
+    }
+};
+
+template <typename T, int D, int G, typename Form>
+__global__ __launch_bounds__(64 * kLogitsWaves) void logits_kernel(ScoreArgs a, Form form) {
     __builtin_amdgcn_s_setprio(3);   // issue ahead of co-resident decode waves
     constexpr int V = 2 * G;
     constexpr int VH = (V + 3) / 4;                  // view quarters (MFMAs per key operand)
@@ -225,8 +244,8 @@ __global__ __launch_bounds__(64 * kLogitsWaves) void logits_kernel(ScoreArgs a) 
 #pragma unroll
     for (int j = 0; j < PP; ++j) {
         const int kk = min(lr + TPR * j, H - 1);
-        q1[j] = ld<T>(qrow + kk);
-        q2[j] = ld<T>(qrow + kk + H);
+        q1[j] = ld<T>(qrow + form.template dim<D>(kk, 0));
+        q2[j] = ld<T>(qrow + form.template dim<D>(kk, 1));
     }
     const double pos = (double)a.positions[rc];
     const bool ok = (r >= 0) & (r < a.R) & (slot >= 0) & (slot < a.M) & (P >= 2) & (P <= a.max_pages) &
@@ -242,9 +261,15 @@ __global__ __launch_bounds__(64 * kLogitsWaves) void logits_kernel(ScoreArgs a) 
         if (e < 4 * nit) s_pg[e] = pg < P - 1 && pev[j] >= 0 && pev[j] < a.pool_pages ? pev[j] : -1;
     }
     if ((int)threadIdx.x < H) {
-        const double ang = pos * pow(a.theta, (-2.0 * (int)threadIdx.x) / D);
-        s_cs[0][threadIdx.x] = cos(ang);
-        s_cs[1][threadIdx.x] = sin(ang);
+        if constexpr (std::is_same<Form, ThetaForm>::value) {
+            const double ang = pos * pow(a.theta, (-2.0 * (int)threadIdx.x) / D);
+            s_cs[0][threadIdx.x] = cos(ang);
+            s_cs[1][threadIdx.x] = sin(ang);
+        } else {
+            const double ang = pos * form.freq[threadIdx.x], mag = (int)threadIdx.x < form.half ? form.magnitude : 1.0;
+            s_cs[0][threadIdx.x] = mag * cos(ang);
+            s_cs[1][threadIdx.x] = mag * sin(ang);
+        }
     }
     double qq = 0.0;
 #pragma unroll
@@ -301,8 +326,8 @@ __global__ __launch_bounds__(64 * kLogitsWaves) void logits_kernel(ScoreArgs a) 
 #pragma unroll
     for (int j = 0; j < PP; ++j) {
         const int kk = min(lr + TPR * j, H - 1);
-        s1[j] = (double)srow[kk];
-        s2[j] = (double)srow[kk + H];
+        s1[j] = (double)srow[form.template dim<D>(kk, 0)];
+        s2[j] = (double)srow[form.template dim<D>(kk, 1)];
     }
     double ss = 0.0;
 #pragma unroll
@@ -336,8 +361,8 @@ __global__ __launch_bounds__(64 * kLogitsWaves) void logits_kernel(ScoreArgs a) 
         if (kk < H) {
             const double x1 = gam * s1[j], x2 = gam * s2[j];
             const double c = s_cs[0][kk], sn = s_cs[1][kk];
-            put(kk, x1 * c - x2 * sn);
-            put(kk + H, x2 * c + x1 * sn);
+            put(form.template dim<D>(kk, 0), x1 * c - x2 * sn);
+            put(form.template dim<D>(kk, 1), x2 * c + x1 * sn);
         }
     }
     __syncthreads();
@@ -710,8 +735,8 @@ __global__ __launch_bounds__(256) void entropy_kernel(ScoreArgs a) {
     }
 }
 
-template <typename T, int D>
-hipError_t launch_gd(int G, const ScoreArgs &a, int stages, hipStream_t s) {
+template <typename T, int D, typename Form>
+hipError_t launch_gd(int G, const ScoreArgs &a, const Form &form, int stages, hipStream_t s) {
     // the KV head is the fastest grid index everywhere: workgroups are handed to
     // the XCDs round-robin, so head h's workgroups all run on one XCD and read
     // back what the previous kernel left in that XCD's L2
@@ -732,7 +757,7 @@ hipError_t launch_gd(int G, const ScoreArgs &a, int stages, hipStream_t s) {
     switch (G) {
 #define GP_CASE(GG)                                                   \
     case GG:                                                          \
-        logits_kernel<T, D, GG><<<g1, 64 * kLogitsWaves, 0, s>>>(b);  \
+        logits_kernel<T, D, GG><<<g1, 64 * kLogitsWaves, 0, s>>>(b, form);  \
         weights_kernel<GG><<<g2, 256, 0, s>>>(a);                     \
         break;
         GP_CASE(1) GP_CASE(2) GP_CASE(4) GP_CASE(8)
@@ -751,11 +776,22 @@ hipError_t launch_gd(int G, const ScoreArgs &a, int stages, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_score(gp_dtype_t dt, int D, int G, const ScoreArgs &a, int stages, hipStream_t s) {
+template <typename Form>
+static hipError_t launch_form(gp_dtype_t dt, int D, int G, const ScoreArgs &a, const Form &form, int stages, hipStream_t s) {
     if (a.Rb == 0) return hipSuccess;
     if (dt == GP_BF16)
-        return D == 128 ? launch_gd<uint16_t, 128>(G, a, stages, s) : launch_gd<uint16_t, 64>(G, a, stages, s);
-    return D == 128 ? launch_gd<float, 128>(G, a, stages, s) : launch_gd<float, 64>(G, a, stages, s);
+        return D == 128 ? launch_gd<uint16_t, 128>(G, a, form, stages, s) : launch_gd<uint16_t, 64>(G, a, form, stages, s);
+    return D == 128 ? launch_gd<float, 128>(G, a, form, stages, s) : launch_gd<float, 64>(G, a, form, stages, s);
+}
+
+hipError_t launch_score(gp_dtype_t dt, int D, int G, const ScoreArgs &a, const gp_rope_t *rope, int stages, hipStream_t s) {
+    if (!rope) return launch_form(dt, D, G, a, ThetaForm{}, stages, s);
+    TableForm form = {};
+    form.half = rope->rotary_dim / 2;
+    form.interleaved = rope->layout == GP_ROPE_INTERLEAVED;
+    form.magnitude = rope->magnitude;
+    std::copy(rope->freq, rope->freq + form.half, form.freq);
+    return launch_form(dt, D, G, a, form, stages, s);
 }
 
 }  // namespace gp

@@ -1,0 +1,161 @@
+"""The operators on a prompt's way into the decode step refuse what they do not take,
+before any launch; rotary frequencies, which are made on the host."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2609_03494_amd as gp
+from paper_2609_03494_amd import _lib
+from test_cache_ops import FAKE, INVALID, ROPE, UNSUPPORTED, WORKSPACE, _kv, _kv8, _ps, lib  # noqa: F401
+
+
+def _rope(layout=0, n=128, mag=1.0, freq=None):
+    r = _lib._Rope(layout, n, mag)
+    for i in range(64):
+        r.freq[i] = 1.0 / (i + 1)
+    if freq is not None:
+        r.freq[freq[0]] = freq[1]
+    return ctypes.byref(r)
+
+
+def _rotary(fn, kv, ps, rope, **kw):
+    a = dict(ROPE, **kw)
+    return fn(kv, ps, a["positions"], rope, a["start"], a["tokens"], a["q"], a["q_stride"], a["q_out"], a["k"], a["k_stride"],
+              a["v"], a["v_stride"], a["hq"], a["advance"], None)
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_append_rotary_refusals(lib, q8):  # noqa: F811
+    fn, kv = (lib.gp_append_rotary_q8, _kv8) if q8 else (lib.gp_append_rotary, _kv)
+    nan, inf = float("nan"), float("inf")
+    for bad in (None, _rope(layout=2), _rope(layout=-1), _rope(n=0), _rope(n=-16), _rope(n=144), _rope(mag=0.0), _rope(mag=-1.0),
+                _rope(mag=nan), _rope(mag=inf), _rope(freq=(0, inf)), _rope(freq=(63, nan))):
+        assert _rotary(fn, kv(), _ps(), bad) == INVALID
+    assert _rotary(fn, kv(d=64), _ps(), _rope(n=128), k_stride=512, v_stride=512, q_stride=2048) == INVALID
+    for n in (2, 8, 24, 120):
+        assert _rotary(fn, kv(), _ps(), _rope(n=n)) == UNSUPPORTED
+    good = _rope(n=64)
+    for bad in (dict(tokens=3), dict(k_stride=1023), dict(q_stride=4095), dict(positions=None), dict(k=None), dict(q_out=None),
+                dict(q_out=0x100000 + 256), dict(q_out=0x300000 - 4)):
+        assert _rotary(fn, kv(), _ps(), good, **bad) == INVALID, bad
+    assert _rotary(fn, None, _ps(), good) == _rotary(fn, kv(), None, good) == INVALID
+    assert _rotary(fn, kv(d=96), _ps(), good) == _rotary(fn, kv(), _ps(), good, hq=24) == UNSUPPORTED
+    assert _rotary(fn, kv(), _ps(), _rope(n=64, freq=(32, nan)), tokens=0, start=FAKE) == 0     # (behind the pairs: not looked at)
+
+
+def test_boundary_score_rotary_refusals(lib):  # noqa: F811
+    p = _lib._Params(0.9, 0.999, 0.99, 0.0, 0.088, 0.0, 4, 0)          # rope_theta is not looked at
+
+    def call(rope, stages=3, n=1 << 40, params=p, cand=144):
+        return lib.gp_boundary_score_rotary(_kv(), _ps(), FAKE, FAKE, 512, FAKE, FAKE, FAKE, 2, 32, ctypes.byref(params), rope,
+                                            FAKE, FAKE, cand, FAKE, n, None, stages)
+    assert call(None) == call(_rope(layout=5)) == call(_rope(mag=0.0)) == call(_rope(), stages=0) == call(_rope(), stages=4) == INVALID
+    assert call(_rope(), cand=16) == INVALID
+    assert call(_rope(n=40)) == UNSUPPORTED
+    assert call(_rope(), n=16) == WORKSPACE
+
+
+def test_rope_frequencies(lib):  # noqa: F811
+    for n in (2, 16, 96, 128):
+        f = gp.gp_rope_frequencies(n, 1.0e6)
+        assert len(f) == n // 2 and f[0] == 1.0
+        for i, x in enumerate(f):
+            assert abs(x - 1.0e6 ** (-2.0 * i / n)) <= 1e-15 * x
+        for i, (x, y) in enumerate(zip(f, gp.gp_rope_frequencies(n, 1.0e6, 4.0))):
+            assert y == x / 4
+        g = gp.gp_rope_frequencies(n, 1.0e6, 8.0, 1.0, 4.0, 8192)
+        for i, (x, y) in enumerate(zip(f, g)):
+            u = 8192 * x / (2 * math.pi)
+            keep = min(1.0, max(0.0, (u - 1.0) / 3.0))
+            assert abs(y - x * (keep + (1 - keep) / 8)) <= 1e-14 * x
+    freq = (ctypes.c_double * 64)()
+    call = lambda n=64, theta=1e6, factor=2.0, low=1.0, high=4.0, ctx=8192.0, to=freq: lib.gp_rope_frequencies(  # noqa: E731
+        to, n, theta, factor, low, high, ctx)
+    nan, inf = float("nan"), float("inf")
+    assert call() == 0
+    for bad in (dict(to=None), dict(n=0), dict(n=63), dict(n=130), dict(theta=0.0), dict(theta=nan), dict(theta=inf),
+                dict(factor=0.5), dict(factor=nan), dict(factor=inf), dict(low=-1.0), dict(low=nan), dict(low=4.0),
+                dict(high=0.5), dict(high=-1.0), dict(high=nan), dict(high=inf), dict(ctx=0.0), dict(ctx=nan), dict(ctx=inf)):
+        assert call(**bad) == INVALID, bad
+    with pytest.raises(gp.GrowPageError):
+        gp.gp_rope_frequencies(64, -1.0)
+    with pytest.raises(ValueError):
+        gp.gp_rope_frequencies(256, 1.0e6)
+    with pytest.raises(ValueError):
+        gp.Rope(0, [])
+
+
+def _state(R=4, width=10, pool=100, **none):
+    a = dict(table=FAKE, pages=FAKE, lens=FAKE, refs=FAKE, stack=FAKE, height=FAKE)
+    a.update(none)
+    return ctypes.byref(_lib._PageState(a["table"], a["pages"], a["lens"], a["refs"], a["stack"], a["height"], R, width, pool))
+
+
+BAD_STATES = [dict(table=None), dict(pages=None), dict(lens=None), dict(refs=None), dict(stack=None), dict(height=None),
+              dict(pool=0), dict(R=-1), dict(width=0)]
+
+
+def test_pages_refusals(lib):  # noqa: F811
+    reserve = lambda ps=None, tokens=FAKE, keep=0, granted=FAKE: lib.gp_pages_reserve(ps or _state(), tokens, keep, granted, None)  # noqa: E731
+    release = lambda ps=None, reqs=FAKE, n=3: lib.gp_pages_release(ps or _state(), reqs, n, None)  # noqa: E731
+    for bad in BAD_STATES:
+        assert reserve(_state(**bad)) == release(_state(**bad)) == INVALID, bad
+    assert lib.gp_pages_reserve(None, FAKE, 0, FAKE, None) == lib.gp_pages_release(None, FAKE, 1, None) == INVALID
+    assert reserve(tokens=None) == reserve(granted=None) == reserve(keep=-1) == release(reqs=None) == release(n=-1) == INVALID
+    for call in (reserve, release):
+        assert call(_state(R=65536)) == call(_state(width=8193)) == UNSUPPORTED
+        assert call(_state(R=0)) == 0
+    assert release(n=65536) == UNSUPPORTED
+    assert release(n=0, reqs=None) == 0
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_fork_refusals(lib, q8):  # noqa: F811
+    fn = lib.gp_pages_fork_q8 if q8 else lib.gp_pages_fork
+
+    def layers(*kw):
+        kind = _lib._KV8Layer if q8 else _lib._KVLayer
+        made = []
+        for k in kw:
+            a = dict(k=FAKE, v=FAKE, pool=100, hkv=8, page=16, d=128)
+            a.update(k)
+            made.append(kind(a["k"], a["v"], *((FAKE, FAKE) if q8 else ()), a["pool"], a["hkv"], a["page"], a["d"],
+                             *(() if q8 else (a.get("dtype", 1),))))
+        return (kind * len(made))(*made)
+
+    def call(ls=None, n=None, ps=None, parents=FAKE, children=FAKE, forks=2, forked=FAKE):
+        ls = layers({}, {}) if ls is None else ls
+        return fn(ls, len(ls) if n is None else n, ps or _state(), parents, children, None, forks, None, forked, None)
+    assert fn(None, 1, _state(), FAKE, FAKE, None, 2, None, FAKE, None) == call(n=0) == call(n=-3) == INVALID
+    assert call(parents=None) == call(children=None) == call(forked=None) == call(forks=-1) == INVALID
+    for bad in (dict(k=None), dict(v=None), dict(pool=99), dict(hkv=4), dict(d=64), dict(k=FAKE + 8), dict(v=FAKE + 4), dict(hkv=0)):
+        assert call(layers({}, bad)) == INVALID, bad
+    assert call(layers(dict(pool=99), dict(pool=99))) == INVALID                  # another pool than the state's
+    if not q8:
+        assert call(layers({}, dict(dtype=0))) == call(layers({}, dict(dtype=7))) == INVALID
+    for bad in BAD_STATES:
+        assert call(ps=_state(**bad)) == INVALID, bad
+    assert call(layers(dict(d=96))) == call(layers(dict(page=32))) == call(forks=2049) == UNSUPPORTED
+    assert call(layers(*([{}] * 257))) == call(layers(dict(hkv=8193))) == call(ps=_state(R=65536)) == UNSUPPORTED
+    assert call(forks=0, parents=None) == call(ps=_state(R=0)) == 0
+
+
+def test_binding_refusals():
+    """What the Python calls check themselves, on tensors that no GPU has to hold."""
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    ps = gp.PageState(i32(4, 10), i32(4), i32(4), i32(100), i32(100), i32(1))
+    k = torch.zeros(100, 2, 16, 64, dtype=torch.bfloat16)
+    layer = gp.KVLayer(k, k)
+    with pytest.raises(ValueError):
+        gp.gp_pages_release(ps, torch.zeros(3, dtype=torch.int64))
+    with pytest.raises(ValueError):
+        gp.gp_pages_reserve(ps, i32(4), torch.zeros(4))
+    with pytest.raises(ValueError):                                     # not on a GPU
+        gp.gp_pages_reserve(ps, i32(4), i32(4))
+    with pytest.raises(ValueError):
+        gp.Layers([])
+    with pytest.raises(ValueError):
+        gp.Layers([layer, gp.KV8Layer(k.view(torch.uint8)[..., :64].contiguous(), k.view(torch.uint8)[..., :64].contiguous(),
+                                      torch.zeros(100, 2), torch.zeros(100, 2))])
