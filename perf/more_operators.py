@@ -315,8 +315,8 @@ def _handles(s):
     s["state"] = gp.PageState(**vars(s["ps"]))
     if case["kind"] == "fork":
         pool, scales = s["pool"], s["scales"]
-        s["layers"] = [gp.KV8Layer(pool[i, 0], pool[i, 1], scales[i, 0], scales[i, 1]) if scales is not None else
-                       gp.KVLayer(pool[i, 0], pool[i, 1]) for i in range(case["layers"])]
+        s["layers"] = gp.Layers(gp.KV8Layer(pool[i, 0], pool[i, 1], scales[i, 0], scales[i, 1]) if scales is not None else
+                                gp.KVLayer(pool[i, 0], pool[i, 1]) for i in range(case["layers"]))
     if case["kind"] in ("prompt", "rotary"):
         s["layer"] = (gp.KV8Layer if case["cache"] == "q8" else gp.KVLayer)(**vars(s["kv"]))
     if case["kind"] == "prompt":
