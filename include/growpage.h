@@ -12,6 +12,7 @@
  *                        (bfloat16, float32, or 8-bit values with scales);
  *                        gp_append_rotary: pairs side by side, a part of the head,
  *                        frequencies for longer contexts
+ *   gp_prompt_attention  attention of prompts, chunks and drafted tokens over the cache
  *   gp_decode_attention_q8     decode attention over the 8-bit cache
  *   gp_select_pages, gp_decode_attention_pages   attention over the pages that
  *                        a bound on their logits selects
@@ -143,7 +144,7 @@ enum {
 };
 
 /* Which workspace gp_workspace_bytes() sizes. */
-enum { GP_OP_DECODE = 0, GP_OP_SCORE = 1, GP_OP_APPLY = 2, GP_OP_SELECT = 3 };
+enum { GP_OP_DECODE = 0, GP_OP_SCORE = 1, GP_OP_APPLY = 2, GP_OP_SELECT = 3, GP_OP_PROMPT = 4 };
 
 typedef struct {
     void *k;                 /* [pool_pages][num_kv_heads][page_size][head_dim] */
@@ -643,6 +644,43 @@ gp_status_t gp_decode_attention_q8(const gp_kv8_layer_t *kv, const gp_page_state
                                    const void *q_post, int32_t num_q_heads, float scale, void *out,
                                    void *ws, size_t ws_bytes, hipStream_t stream);
 
+/* Attention of new tokens over the paged cache (Sec. 3.1, attention-output equation,
+ * with a causal limit): whole prompts, chunks of them, drafted tokens to check, single
+ * tokens, in any mix.
+ *  - Request r brings n_r tokens, rows tok_start[r] .. of q and out (tok_start as in
+ *    gp_append_rope; NULL: one each), whose keys and values are in the cache
+ *    already.  With c_r tokens before them, token j attends over the first c_r + j +
+ *    1 tokens of the request, itself the last:
+ *      out[j][g] = sum_{i <= c_r + j} softmax_i(scale * q[j][g] . k_i) v_i.
+ *  - advanced == 0: seq_lens do not count the new tokens yet, c_r = m_r (every
+ *    layer of a model but the last, between gp_append_rope with advance 0 and the
+ *    next layer); a request without room for its n_r tokens (which the append
+ *    then left out) gets zero outputs.  advanced != 0: they do, c_r = m_r - n_r (a
+ *    token for which c_r + j + 1 <= 0 gets a zero output).
+ *  - A held request is left out: its rows of out are not written, nor are rows that
+ *    belong to no request.  A row whose weights have no positive sum gets zeros, as in
+ *    gp_decode_attention.  Tokens that a row does not see are never used, whatever
+ *    they hold, infinities and NaN included.
+ *  - float32 sums and statistics; of a bfloat16 or 8-bit cache the weights are
+ *    rounded to bfloat16 for their product with the values, and a weight below 2^-126
+ *    of the row's largest counts as zero.  8-bit: q and out bfloat16, the scale as in
+ *    gp_decode_attention_q8.
+ * q: rows of q_stride elements, [num_q_heads][head_dim] contiguous; out [num_tokens]
+ * [num_q_heads][head_dim], which may not overlap q (GP_ERR_INVALID).  Pools at multiples
+ * of 16 bytes (GP_ERR_INVALID otherwise).  The work is split by the lengths of the whole
+ * batch, so that a row's float32 sums depend on them to rounding (as in
+ * gp_decode_attention).  Tables up to 8192 pages, 65535 requests, 8192 KV heads; (num_tokens
+ * * G / 128 + num_reqs) * num_kv_heads below 2^24 (GP_ERR_UNSUPPORTED).  Takes the
+ * GP_OP_PROMPT workspace of num_tokens or more. */
+gp_status_t gp_prompt_attention(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const int32_t *tok_start,
+                                int32_t num_tokens, int32_t advanced, const void *q, int64_t q_stride,
+                                int32_t num_q_heads, float scale, void *out, void *ws, size_t ws_bytes,
+                                hipStream_t stream);
+gp_status_t gp_prompt_attention_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps,
+                                   const int32_t *tok_start, int32_t num_tokens, int32_t advanced,
+                                   const void *q, int64_t q_stride, int32_t num_q_heads, float scale,
+                                   void *out, void *ws, size_t ws_bytes, hipStream_t stream);
+
 /* Bounds of the cached keys, for gp_select_pages: of every page and KV head
  * the least (bounds[page][head][0]) and the greatest (.. [1]) value that each
  * head dim takes over the page's resident tokens.  bounds [pool_pages]
@@ -751,7 +789,8 @@ gp_status_t gp_pages_fork_q8(const gp_kv8_layer_t *layers, int32_t n_layers, con
  * pages wide, 65535 requests (GP_ERR_UNSUPPORTED). */
 gp_status_t gp_pages_release(const gp_page_state_t *ps, const int32_t *reqs, int32_t num, hipStream_t stream);
 
-/* Bytes of workspace an operation needs (op = GP_OP_DECODE / SCORE / APPLY / SELECT). */
+/* Bytes of workspace an operation needs (op = GP_OP_DECODE / SCORE / APPLY / SELECT /
+ * PROMPT; for GP_OP_PROMPT num_bnd is the most tokens that a call brings). */
 size_t gp_workspace_bytes(int32_t op, int32_t num_reqs, int32_t num_bnd, int32_t num_q_heads,
                           int32_t num_kv_heads, int32_t head_dim, int32_t max_pages,
                           int32_t page_size, gp_dtype_t dtype, int32_t n_layers);

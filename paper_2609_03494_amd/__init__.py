@@ -17,5 +17,6 @@ from ._lib import (  # noqa: F401
     gp_decode_attention_q8, gp_page_bounds, gp_page_bounds_q8, gp_select_pages, gp_decode_attention_shared, gp_decode_attention_stages, gp_decode_step, gp_stream_read, gp_update_summaries, gp_workspace_bytes, load, status_string,
     workspace,
     GP_ROPE_HALF, GP_ROPE_INTERLEAVED, Rope, gp_append_rotary, gp_append_rotary_q8, gp_boundary_score_rotary, gp_rope_frequencies,
+    GP_OP_PROMPT, gp_prompt_attention, gp_prompt_attention_q8,
     Layers, gp_pages_fork, gp_pages_fork_q8, gp_pages_release, gp_pages_reserve,
 )

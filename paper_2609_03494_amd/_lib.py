@@ -18,7 +18,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libgrowpage.so")
 
 GP_F32, GP_BF16 = 0, 1
-GP_OP_DECODE, GP_OP_SCORE, GP_OP_APPLY, GP_OP_SELECT = 0, 1, 2, 3
+GP_OP_DECODE, GP_OP_SCORE, GP_OP_APPLY, GP_OP_SELECT, GP_OP_PROMPT = 0, 1, 2, 3, 4
 GP_COMPRESS, GP_GROW, GP_FALLBACK, GP_PREEMPT, GP_NOT_BOUNDARY = 0, 1, 2, 3, 4
 GP_SHRINK = 5
 GP_POLICY_GROWPAGE, GP_POLICY_FIXED, GP_POLICY_RANDOM, GP_POLICY_INVERSE, GP_POLICY_SHRINK = 0, 1, 2, 3, 4
@@ -37,6 +37,7 @@ EXPORTS = ("gp_update_summaries", "gp_decode_attention", "gp_decode_attention_no
            "gp_page_bounds", "gp_page_bounds_q8", "gp_select_pages", "gp_decode_attention_pages",
            "gp_decode_attention_pages_q8", "gp_pages_reserve", "gp_pages_fork", "gp_pages_fork_q8", "gp_pages_release",
            "gp_append_rotary", "gp_append_rotary_q8", "gp_rope_frequencies", "gp_boundary_score_rotary",
+           "gp_prompt_attention", "gp_prompt_attention_q8",
            "gp_workspace_bytes", "gp_status_string", "gp_stream_read")
 
 
@@ -143,7 +144,9 @@ def load() -> ctypes.CDLL:
     rope_args = [ps_p, vp, vp, i32, vp, i64, vp, vp, i64, vp, i64, i32, f32, i32, vp]
     pages_args = [ps_p, vp, i32, vp, i32, f32, vp, vp, sz, vp]
     rotary_args = [ps_p, vp, ctypes.POINTER(_Rope), vp, i32, vp, i64, vp, vp, i64, vp, i64, i32, i32, vp]
-    for name, layer, rest in (("gp_append_rope", kv_p, rope_args), ("gp_append_rope_q8", kv8_p, rope_args),
+    prompt_args = [ps_p, vp, i32, i32, vp, i64, i32, f32, vp, vp, sz, vp]
+    for name, layer, rest in (("gp_prompt_attention", kv_p, prompt_args), ("gp_prompt_attention_q8", kv8_p, prompt_args),
+                              ("gp_append_rope", kv_p, rope_args), ("gp_append_rope_q8", kv8_p, rope_args),
                               ("gp_append_rotary", kv_p, rotary_args), ("gp_append_rotary_q8", kv8_p, rotary_args),
                               ("gp_decode_attention_q8", kv8_p, [ps_p, vp, i32, f32, vp, vp, sz, vp]),
                               ("gp_page_bounds", kv_p, [ps_p, vp, i32, vp, vp]),
@@ -730,3 +733,31 @@ def gp_pages_release(ps: PageState, reqs: torch.Tensor, stream=None) -> None:
     """The rows listed give up their pages, which go back to the free stack when nobody else holds them."""
     c_ps = _pages("gp_pages_release", ps, reqs=reqs)
     _check(load().gp_pages_release(ctypes.byref(c_ps), _ptr(reqs), reqs.numel(), _stream(stream)), "gp_pages_release")
+
+
+def _prompt(name, kv, dtype, ps, q, scale, out, ws, tok_start, advanced, stream):
+    c_kv, c_ps = kv.c(), ps.c()
+    shape, d = q.shape, c_kv.head_dim
+    if len(shape) != 3 or shape[2] != d or q.dtype != dtype or out.dtype != dtype or out.shape != shape:
+        raise ValueError(f"{name}: q and out [tokens, heads, {d}], {dtype}")
+    T, Hq = shape[0], shape[1]
+    if tok_start is not None and (tok_start.dtype != torch.int32 or tok_start.numel() != c_ps.num_reqs + 1):
+        raise ValueError(f"{name}: tok_start [num_reqs + 1] int32")
+    _on_device(name, kv, ps, q, out, ws, tok_start)
+    _check(getattr(load(), name)(ctypes.byref(c_kv), ctypes.byref(c_ps), _ptr(tok_start), T, bool(advanced), q.data_ptr(),
+                                 _row(q.stride(), T, Hq, d, name), Hq, scale, _ptr(out), _ptr(ws), ws.numel(),
+                                 _stream(stream)), name)
+
+
+def gp_prompt_attention(kv: KVLayer, ps: PageState, q: torch.Tensor, scale: float, out: torch.Tensor, ws: torch.Tensor,
+                        tok_start: torch.Tensor | None = None, advanced: bool = False, stream=None) -> None:
+    """New tokens attend over the cache that already holds them: q [T, Hq, d] with any stride from
+    token to token, out [T, Hq, d]; tok_start [R + 1] int32, or None for one token per request;
+    advanced: seq_lens count the new tokens."""
+    _prompt("gp_prompt_attention", kv, kv.k.dtype, ps, q, scale, out, ws, tok_start, advanced, stream)
+
+
+def gp_prompt_attention_q8(kv: KV8Layer, ps: PageState, q: torch.Tensor, scale: float, out: torch.Tensor, ws: torch.Tensor,
+                           tok_start: torch.Tensor | None = None, advanced: bool = False, stream=None) -> None:
+    """gp_prompt_attention over an 8-bit cache; q and out bfloat16."""
+    _prompt("gp_prompt_attention_q8", kv, torch.bfloat16, ps, q, scale, out, ws, tok_start, advanced, stream)

@@ -171,6 +171,7 @@ size_t gp_workspace_bytes(int32_t op, int32_t num_reqs, int32_t num_bnd, int32_t
             return decode_ws(num_reqs, num_q_heads, num_kv_heads, head_dim, max_pages, decode_waves(elem_bytes(dtype), head_dim)).total;
         case GP_OP_SCORE: return score_ws(num_bnd, num_q_heads, num_kv_heads, max_pages).total;
         case GP_OP_SELECT: return select_ws(num_reqs, num_kv_heads, max_pages);
+        case GP_OP_PROMPT: return prompt_ws();
         case GP_OP_APPLY:
             return apply_ws(num_bnd, num_kv_heads, head_dim, elem_bytes(dtype), max_pages, n_layers).total;
     }
@@ -502,6 +503,52 @@ gp_status_t rope_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, const 
     return from_hip(launch_rope(kv8 ? 1 : e, kv->head_dim, a, advance != 0, stream));
 }
 
+gp_status_t prompt_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, const gp_page_state_t *ps,
+                        const int32_t *tok_start, int32_t num_tokens, int32_t advanced, const void *q,
+                        int64_t q_stride, int32_t num_q_heads, float scale, void *out, void *ws, size_t ws_bytes,
+                        hipStream_t stream) {
+    gp_status_t st = check_layer(kv);
+    if (st != GP_OK) return st;
+    if ((st = check_state(ps, kv)) != GP_OK) return st;
+    if (!dims_ok(num_q_heads, kv->num_kv_heads, kv->head_dim)) return GP_ERR_UNSUPPORTED;
+    if (!(scale > 0.0f) || !isfinite(scale) || (kv8 && scale >= 0x1p111f) || num_tokens < 0) return GP_ERR_INVALID;
+    if (!tok_start && num_tokens != ps->num_reqs) return GP_ERR_INVALID;
+    const int64_t row = (int64_t)num_q_heads * kv->head_dim;
+    if (q_stride < row || q_stride > int64_t(1) << 30 || !aligned16(kv->k, kv->v)) return GP_ERR_INVALID;
+    if (ps->num_reqs == 0 || num_tokens == 0) return GP_OK;
+    if (!q || !out || !ws) return GP_ERR_INVALID;
+    if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages || kv->num_kv_heads > kMaxListedHeads) return GP_ERR_UNSUPPORTED;
+    const int e = elem_bytes(kv->dtype);
+    if (overlap(out, num_tokens * row, q, (num_tokens - 1) * q_stride + row, e)) return GP_ERR_INVALID;
+    PromptArgs a = {};
+    a.G = num_q_heads / kv->num_kv_heads;
+    while (1 << a.lg < a.G) ++a.lg;
+    a.tokens = kPromptRows / a.G;
+    const int64_t places = tok_start ? (int64_t)num_tokens / a.tokens + ps->num_reqs : ps->num_reqs;
+    if (places * kv->num_kv_heads >= int64_t(1) << 24) return GP_ERR_UNSUPPORTED;      // a grid of 2^32 threads
+    a.places = (int)places;
+    if (ws_bytes < prompt_ws()) return GP_ERR_WORKSPACE;
+    a.k = kv->k;
+    a.v = kv->v;
+    a.q = q;
+    a.out = out;
+    a.k_scale = kv8 ? kv8->k_scale : nullptr;
+    a.v_scale = kv8 ? kv8->v_scale : nullptr;
+    a.page_table = ps->page_table;
+    a.num_pages = ps->num_pages;
+    a.seq_lens = ps->seq_lens;
+    a.start = tok_start;
+    a.q_stride = q_stride;
+    a.R = ps->num_reqs;
+    a.T = num_tokens;
+    a.Hkv = kv->num_kv_heads;
+    a.max_pages = ps->max_pages;
+    a.pool_pages = kv->pool_pages;
+    a.advanced = advanced != 0;
+    a.qscale = scale * 1.4426950408889634f * (kv8 ? kQ8KeyScale : 1.0f);
+    return from_hip(launch_prompt(kv8 ? 1 : e, kv->head_dim, a, stream));
+}
+
 gp_status_t bounds_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, const gp_page_state_t *ps,
                         const int32_t *from_tokens, int32_t max_update, void *bounds, hipStream_t stream) {
     gp_status_t st = check_layer(kv);
@@ -592,6 +639,25 @@ gp_status_t gp_append_rotary_q8(const gp_kv8_layer_t *kv, const gp_page_state_t 
     if (!rope) return GP_ERR_INVALID;
     return rope_call(&as, kv, ps, rope, positions, tok_start, num_tokens, q, q_stride, q_out, k_new, k_stride,
                      v_new, v_stride, num_q_heads, 1.0f, advance, stream);
+}
+
+gp_status_t gp_prompt_attention(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const int32_t *tok_start,
+                                int32_t num_tokens, int32_t advanced, const void *q, int64_t q_stride,
+                                int32_t num_q_heads, float scale, void *out, void *ws, size_t ws_bytes,
+                                hipStream_t stream) {
+    return prompt_call(kv, nullptr, ps, tok_start, num_tokens, advanced, q, q_stride, num_q_heads, scale, out, ws,
+                       ws_bytes, stream);
+}
+
+gp_status_t gp_prompt_attention_q8(const gp_kv8_layer_t *kv, const gp_page_state_t *ps, const int32_t *tok_start,
+                                   int32_t num_tokens, int32_t advanced, const void *q, int64_t q_stride,
+                                   int32_t num_q_heads, float scale, void *out, void *ws, size_t ws_bytes,
+                                   hipStream_t stream) {
+    gp_kv_layer_t as;
+    const gp_status_t st = check_layer8(kv, &as);
+    if (st != GP_OK) return st;
+    return prompt_call(&as, kv, ps, tok_start, num_tokens, advanced, q, q_stride, num_q_heads, scale, out, ws, ws_bytes,
+                       stream);
 }
 
 gp_status_t gp_page_bounds(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const int32_t *from_tokens,

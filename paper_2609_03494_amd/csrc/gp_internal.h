@@ -37,6 +37,7 @@ constexpr int kPrefixSlotPages = 64;      // pages of one partial slot of a shar
 constexpr int kMaxPrefixSlotPages = 128;  // and at most (LDS id table)
 constexpr int kMaxDecodePages = 8192;     // table width the decode calls accept
 constexpr float kQ8KeyScale = 65536.0f;   // codes of 8-bit keys in units of their bfloat16 operands (see Page<E4m3>)
+constexpr int kPromptRows = 128;          // (token, query head) rows of a prompt attention item
 constexpr int kMaxRopeTokens = 1 << 27;   // tokens one gp_append_rope call takes, and
 constexpr int kMaxListedHeads = 8192;     // KV heads it, the page bounds and the selection take: grids below 2^32 threads
 constexpr size_t kScratchBytes = size_t(8) << 20;   // static scratch of gp_decode_attention_noalloc
@@ -174,6 +175,8 @@ __host__ __device__ inline DecodeWs decode_ws(int R, int Hq, int Hkv, int D, int
 __host__ __device__ inline size_t select_ws(int R, int Hkv, int max_pages) {
     return align_up((size_t)R * Hkv * max_pages * sizeof(float) + 64);
 }
+
+__host__ __device__ inline size_t prompt_ws() { return kAlign; }
 
 struct ScoreWs {
     size_t cand, expz, part, weights, total;
@@ -323,6 +326,19 @@ struct RopeArgs {
     double magnitude;
 };
 
+// gp_prompt_attention: n_r new tokens per request attend over its pages.
+struct PromptArgs {
+    const void *k, *v, *q;
+    void *out;
+    const float *k_scale, *v_scale;   // 8-bit pools
+    const int32_t *page_table, *num_pages, *seq_lens;
+    const int32_t *start;             // [R + 1] first token of each request; nullptr: one token each
+    int64_t q_stride;                 // elements from token to token
+    int R, T, Hkv, G, lg, max_pages, pool_pages, advanced;   // lg: log2 G
+    int tokens, places;               // new tokens of an item, items of one KV head at most
+    float qscale;                     // scale * log2(e); 8-bit: times kQ8KeyScale
+};
+
 struct BoundsArgs {
     const void *k;
     const float *k_scale;             // 8-bit pools
@@ -408,6 +424,7 @@ hipError_t launch_decode_q8(int D, int G, const DecodeArgs &a, hipStream_t s);
 hipError_t launch_decode_pages(gp_dtype_t dt, int D, int G, const DecodeArgs &a, hipStream_t s);
 // cache: element bytes of the pool (1: e4m3 codes, 2, 4)
 hipError_t launch_rope(int cache, int D, const RopeArgs &a, bool advance, hipStream_t s);
+hipError_t launch_prompt(int cache, int D, const PromptArgs &a, hipStream_t s);
 hipError_t launch_bounds(int cache, int D, const BoundsArgs &a, hipStream_t s);
 hipError_t launch_select(gp_dtype_t dt, int D, int G, const SelectArgs &a, hipStream_t s);
 // rope: nullptr: half-split pairs at a.theta
