@@ -61,10 +61,27 @@ __device__ inline float sum_halves(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// x where at < 0, else -inf (in vector registers alone: 32 compares would take 64 scalar ones)
+__device__ inline float masked(float x, int at) {
+    const uint32_t keep = (uint32_t)(at >> 31);
+    return __uint_as_float((__float_as_uint(x) & keep) | (0xff800000u & ~keep));
+}
 __device__ inline uint32_t pack_bf16(float a, float b) {             // to nearest even
     const bf16x2_t x = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, x);
 }
+
+// 16 bytes a lane from base + off to LDS, `to` + 16 lane, past the registers.  Written as
+// assembly since the compiler makes every LDS read wait for all such loads in flight,
+// those into the other stage included; here the wave waits for them (kWaitVm0) before
+// the barrier that hands the stage over.  No register is written.
+__device__ inline void load_lds(const void *base, uint32_t off, uint32_t to) {
+    __asm__ volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(to) : "memory");
+}
+__device__ inline uint32_t lds_addr(const void *p) {
+    return (uint32_t)(size_t)(__attribute__((address_space(3))) const char *)p;
+}
+constexpr int kWaitVm0 = 0x0F70;                                     // s_waitcnt vmcnt(0)
 
 // CACHE: bytes of a pool element (1: e4m3 codes, as bfloat16 in LDS).
 template <int CACHE, int D>
@@ -161,27 +178,43 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
         for (int s = 0; s < QS; ++s) q[s] = load16(src + s * (32 / (int)sizeof(E)));
     }
 
-    // a tile's way from the pools to LDS
+    // a tile's way from the pools to LDS: a wave takes LOADS pieces of 1024 bytes each of
+    // the keys and the values, 8-bit ones through registers, where they are widened
     const int32_t *table = a.page_table + (size_t)r * a.max_pages;
-    u32x4_t kr[LOADS], vr[LOADS];
+    const size_t slice = (size_t)h * kPage * D * CACHE, page_bytes = (size_t)a.Hkv * kPage * D * CACHE;
+    u32x4_t kr[CACHE == 1 ? LOADS : 1], vr[CACHE == 1 ? LOADS : 1];
     float ks[2][TL::PAGES], vs[2][TL::PAGES];                        // 8-bit: scales, of the tile in work and the next
-    auto page_of = [&](int tile, int pg) {
-        const int id = scalar_load(table, min(tile * TL::PAGES + pg, last_page));
-        return min(max(id, 0), a.pool_pages - 1);
+    int ids[LOADS], pids[TL::PAGES];                                 // pages of the next pieces; 8-bit: of the next tile
+    auto page_of = [&](int tile, int pg) { return scalar_load(table, min(tile * TL::PAGES + pg, last_page)); };
+    auto inside = [&](int id) { return min(max(id, 0), a.pool_pages - 1); };
+    auto request = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) ids[i] = page_of(tile, (i * kThreads + wave * 64) / TL::PU);
+        if constexpr (CACHE == 1)
+#pragma unroll
+            for (int p = 0; p < TL::PAGES; ++p) pids[p] = page_of(tile, p);
     };
-    auto load = [&](int tile) {
+    auto load = [&](int buf) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int first_unit = i * kThreads + wave * 64, pg = first_unit / TL::PU;
-            const size_t slice = ((size_t)page_of(tile, pg) * a.Hkv + h) * kPage * D * CACHE;
-            const size_t off = slice + (size_t)(first_unit % TL::PU + lane) * 16;
-            kr[i] = *reinterpret_cast<const u32x4_t *>(static_cast<const char *>(a.k) + off);
-            vr[i] = *reinterpret_cast<const u32x4_t *>(static_cast<const char *>(a.v) + off);
+            const int piece = i * kWaves + wave;
+            const size_t from = inside(ids[i]) * page_bytes + slice + (size_t)(piece * 64 % TL::PU) * 16;
+            const char *kp = static_cast<const char *>(a.k) + from, *vp = static_cast<const char *>(a.v) + from;
+            if constexpr (CACHE == 1) {
+                kr[i] = reinterpret_cast<const u32x4_t *>(kp)[lane];
+                vr[i] = reinterpret_cast<const u32x4_t *>(vp)[lane];
+            } else {
+                // the unit that belongs at the lane's place in LDS
+                const int t = (piece * 64 + lane) / TL::UPR, c = lane % TL::UPR;
+                const int ku = (lane & ~(TL::UPR - 1)) + (c ^ TL::key_swizzle(t)), vu = (lane & ~(TL::UPR - 1)) + (c ^ TL::value_swizzle(t));
+                load_lds(kp, ku * 16, lds_addr(s_k[buf] + piece * 1024));
+                load_lds(vp, vu * 16, lds_addr(s_v[buf] + piece * 1024));
+            }
         }
         if constexpr (CACHE == 1) {
 #pragma unroll
             for (int p = 0; p < TL::PAGES; ++p) {
-                const int64_t sc = (int64_t)page_of(tile, p) * a.Hkv + h;
+                const int64_t sc = (int64_t)inside(pids[p]) * a.Hkv + h;
                 ks[1][p] = scalar_load(a.k_scale, sc);
                 vs[1][p] = scalar_load(a.v_scale, sc);
             }
@@ -201,16 +234,18 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
         }
         return is;
     };
-    // border: some row does not see all of the tile's tokens
-    auto store = [&](int tile, int buf, bool border) {
+    // the loaded tile stands in LDS after this and a barrier.  border: some row does not see
+    // all of its tokens: values behind the request's tokens become zero (whatever lies there),
+    // and a tile is marked that has infinite values or NaN among the others
+    auto settle = [&](int tile, int buf, bool border) {
         bool found = false;
+        if constexpr (CACHE == 1) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int u = i * kThreads + tid, t = u / TL::PUR, c = u % TL::PUR;
-            u32x4_t *kt = reinterpret_cast<u32x4_t *>(s_k[buf] + t * TL::ROWB), *vt = reinterpret_cast<u32x4_t *>(s_v[buf] + t * TL::ROWB);
-            const int sk = TL::key_swizzle(t), sv = TL::value_swizzle(t);
-            if (border && tile * TOK + t >= last) vr[i] = u32x4_t{};   // (whatever lies behind the request's tokens)
-            if constexpr (CACHE == 1) {
+            for (int i = 0; i < LOADS; ++i) {
+                const int u = i * kThreads + tid, t = u / TL::PUR, c = u % TL::PUR;
+                u32x4_t *kt = reinterpret_cast<u32x4_t *>(s_k[buf] + t * TL::ROWB), *vt = reinterpret_cast<u32x4_t *>(s_v[buf] + t * TL::ROWB);
+                const int sk = TL::key_swizzle(t), sv = TL::value_swizzle(t);
+                if (border && tile * TOK + t >= last) vr[i] = u32x4_t{};
                 constexpr float unit = 1.0f / kQ8KeyScale;           // (see Page<E4m3>::kKeyUnit of the decode kernel)
                 const u32x4_t v0 = widen(vr[i][0], vr[i][1], 1.0f), v1 = widen(vr[i][2], vr[i][3], 1.0f);
                 kt[(2 * c) ^ sk] = widen(kr[i][0], kr[i][1], unit);
@@ -218,10 +253,18 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
                 vt[(2 * c) ^ sv] = v0;
                 vt[(2 * c + 1) ^ sv] = v1;
                 if (border) found |= odd(v0) || odd(v1);
-            } else {
-                kt[c ^ sk] = kr[i];
-                vt[c ^ sv] = vr[i];
-                if (border) found |= odd(vr[i]);
+            }
+        } else {
+            __builtin_amdgcn_s_waitcnt(kWaitVm0);
+            if (border) {
+                __asm__ volatile("" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < LOADS; ++i) {
+                    const int u = (i * kWaves + wave) * 64 + lane;
+                    u32x4_t *at = reinterpret_cast<u32x4_t *>(s_v[buf]) + u;
+                    if (tile * TOK + u / TL::UPR >= last) *at = u32x4_t{};
+                    else found |= odd(*at);
+                }
             }
         }
         if (border && __any(found) && lane == 0) s_odd[buf] = tile;
@@ -233,9 +276,13 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
     for (int d = 0; d < DB; ++d) o[d] = f32x16_t{};
     float m = kNegInf, l = 0.0f;                                     // the row's maximum (both halves the same), this half's sum
     if (tid < 2) s_odd[tid] = -1;
-    if (tiles > 0) load(0);
+    if (tiles > 0) {
+        request(0);
+        load(0);
+        request(1);
+    }
     __syncthreads();
-    if (tiles > 0) store(0, 0, on_border(0));
+    if (tiles > 0) settle(0, 0, on_border(0));
     __syncthreads();
     for (int tile = 0; tile < tiles; ++tile) {
         const int buf = tile & 1;
@@ -246,7 +293,10 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
                 vs[0][p] = vs[1][p];
             }
         }
-        if (tile + 1 < tiles) load(tile + 1);
+        if (tile + 1 < tiles) {
+            load(buf ^ 1);
+            request(tile + 2);
+        }
         if (tile * TOK < wave_last) {
             // S^T
             f32x16_t st[TB];
@@ -267,21 +317,21 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
                     }
                 }
             }
-            // in units of log2, 8-bit: with the page's scale
+            // (8-bit: in units of log2, with the page's scale; the others' scale comes with the difference)
+            if constexpr (CACHE == 1) {
 #pragma unroll
-            for (int tb = 0; tb < TB; ++tb)
+                for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float f = CACHE == 1 ? __builtin_amdgcn_fmed3f(a.qscale * ks[0][2 * tb + i / 8], FLT_TRUE_MIN, FLT_MAX) : a.qscale;
-                    st[tb][i] *= f;
-                }
+                    for (int i = 0; i < 16; ++i) st[tb][i] *= __builtin_amdgcn_fmed3f(a.qscale * ks[0][2 * tb + i / 8], FLT_TRUE_MIN, FLT_MAX);
+            }
+            const float unit = CACHE == 1 ? 1.0f : a.qscale;
             if ((tile + 1) * TOK > wave_first) {
                 const int left = sees - tile * TOK - 4 * half;       // tokens of the tile that the row sees, from this half's first on
 #pragma unroll
                 for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (tb * 32 + 8 * (i / 4) + i % 4 >= left) st[tb][i] = kNegInf;
+                        st[tb][i] = masked(st[tb][i], tb * 32 + 8 * (i / 4) + i % 4 - left);
             }
             float top = st[0][0];
 #pragma unroll
@@ -289,8 +339,9 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, st[tb][i]);
             top = max_halves(top);
-            if (__any(top > m)) {
-                const float up = fmaxf(m, top), f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - up);
+            // (a maximum may lag by 8 in log2: weights up to 2^8, relative errors as they are)
+            if (__any(top * unit > m * unit + 8.0f)) {
+                const float up = fmaxf(m, top), f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f((m - up) * unit);
                 l *= f;
 #pragma unroll
                 for (int d = 0; d < DB; ++d)
@@ -298,12 +349,12 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
                     for (int i = 0; i < 16; ++i) o[d][i] *= f;
                 m = up;
             }
-            const float from = m == kNegInf ? 0.0f : m;              // (a row that sees nothing yet)
+            const float from = m == kNegInf ? 0.0f : m * unit;       // (a row that sees nothing yet)
 #pragma unroll
             for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    st[tb][i] = __builtin_amdgcn_exp2f(st[tb][i] - from);
+                    st[tb][i] = __builtin_amdgcn_exp2f(fmaf(st[tb][i], unit, -from));
                     l += st[tb][i];
                 }
             if constexpr (CACHE == 1) {
@@ -318,23 +369,31 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
             if constexpr (CACHE == 4) {
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
-                    f32x16_t plus = {}, minus = {};
+                    auto value = [&](int tb, int i) {
+                        const int t = tb * 32 + 8 * (i / 4) + 4 * half + i % 4, u = (d * 32 + col) / 4;
+                        return *reinterpret_cast<const float *>(vb + t * TL::ROWB + ((u ^ TL::value_swizzle(t)) << 4) + (col & 3) * 4);
+                    };
+                    if (odd_values) {
+                        for (int part = 0; part < 3; ++part) {       // finite values; where +inf or NaN, where -inf or NaN
+                            f32x16_t y = {};
 #pragma unroll
-                    for (int tb = 0; tb < TB; ++tb)
+                            for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int t = tb * 32 + 8 * (i / 4) + 4 * half + i % 4, u = (d * 32 + col) / 4;
-                            float x = *reinterpret_cast<const float *>(vb + t * TL::ROWB + ((u ^ TL::value_swizzle(t)) << 4) + (col & 3) * 4);
-                            if (odd_values) {
-                                plus = __builtin_amdgcn_mfma_f32_32x32x2f32(x == __builtin_huge_valf() || x != x ? 1.0f : 0.0f, st[tb][i], plus, 0, 0, 0);
-                                minus = __builtin_amdgcn_mfma_f32_32x32x2f32(x == kNegInf || x != x ? 1.0f : 0.0f, st[tb][i], minus, 0, 0, 0);
-                                x = fabsf(x) < __builtin_huge_valf() ? x : 0.0f;
-                            }
-                            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, st[tb][i], o[d], 0, 0, 0);
+                                for (int i = 0; i < 16; ++i) {
+                                    const float x = value(tb, i);
+                                    const bool mine = x != x || x == (part == 1 ? __builtin_huge_valf() : kNegInf);
+                                    const float z = part == 0 ? (fabsf(x) < __builtin_huge_valf() ? x : 0.0f) : mine ? 1.0f : 0.0f;
+                                    y = __builtin_amdgcn_mfma_f32_32x32x2f32(z, st[tb][i], y, 0, 0, 0);
+                                }
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[d][i] += part == 0 ? y[i] : y[i] > 0.0f ? (part == 1 ? __builtin_huge_valf() : kNegInf) : 0.0f;
                         }
-                    if (odd_values)
+                    } else {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[d][i] += (plus[i] > 0.0f ? __builtin_huge_valf() : 0.0f) + (minus[i] > 0.0f ? kNegInf : 0.0f);
+                        for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(tb, i), st[tb][i], o[d], 0, 0, 0);
+                    }
                 }
             } else {
                 u32x4_t p[2 * TB];
@@ -356,30 +415,28 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
                 };
                 if (odd_values) {
 #pragma unroll
-                    for (int d = 0; d < DB; ++d) {
-                        f32x16_t plus = {}, minus = {};
+                    for (int d = 0; d < DB; ++d)
+                        for (int part = 0; part < 3; ++part) {       // finite values; where +inf or NaN, where -inf or NaN
+                            f32x16_t y = {};
 #pragma unroll
-                        for (int k = 0; k < 2 * TB; ++k) {
-                            u32x4_t x = read(k, d), xp, xm;
+                            for (int k = 0; k < 2 * TB; ++k) {
+                                u32x4_t x = read(k, d);
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                xp[c] = xm[c] = 0;
+                                for (int c = 0; c < 4; ++c) {
+                                    uint32_t z = 0;
 #pragma unroll
-                                for (int s = 0; s < 32; s += 16) {
-                                    const uint32_t e = (x[c] >> s) & 0xffff, size = e & 0x7fff;
-                                    if (size == 0x7f80 ? !(e & 0x8000) : size > 0x7f80) xp[c] |= 0x3f80u << s;
-                                    if (size == 0x7f80 ? (e & 0x8000) != 0 : size > 0x7f80) xm[c] |= 0x3f80u << s;
-                                    if (size >= 0x7f80) x[c] &= ~(0xffffu << s);
+                                    for (int s = 0; s < 32; s += 16) {
+                                        const uint32_t e = (x[c] >> s) & 0xffff, size = e & 0x7fff;
+                                        const bool mine = size > 0x7f80 || e == (part == 1 ? 0x7f80u : 0xff80u);
+                                        z |= part == 0 ? (size < 0x7f80 ? e << s : 0u) : mine ? 0x3f80u << s : 0u;
+                                    }
+                                    x[c] = z;
                                 }
+                                y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, p[k]), y, 0, 0, 0);
                             }
-                            const bf16x8_t pk = __builtin_bit_cast(bf16x8_t, p[k]);
-                            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), pk, o[d], 0, 0, 0);
-                            plus = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, xp), pk, plus, 0, 0, 0);
-                            minus = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, xm), pk, minus, 0, 0, 0);
-                        }
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[d][i] += (plus[i] > 0.0f ? __builtin_huge_valf() : 0.0f) + (minus[i] > 0.0f ? kNegInf : 0.0f);
-                    }
+                            for (int i = 0; i < 16; ++i) o[d][i] += part == 0 ? y[i] : y[i] > 0.0f ? (part == 1 ? __builtin_huge_valf() : kNegInf) : 0.0f;
+                        }
                 } else {
 #pragma unroll
                     for (int k = 0; k < 2 * TB; ++k)
@@ -389,7 +446,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
                 }
             }
         }
-        if (tile + 1 < tiles) store(tile + 1, buf ^ 1, on_border(tile + 1));
+        if (tile + 1 < tiles) settle(tile + 1, buf ^ 1, on_border(tile + 1));
         __syncthreads();
     }
     l = sum_halves(l);
