@@ -670,7 +670,7 @@ gp_status_t gp_decode_attention_q8(const gp_kv8_layer_t *kv, const gp_page_state
  * of 16 bytes (GP_ERR_INVALID otherwise).  The work is split by the lengths of the whole
  * batch, so that a row's float32 sums depend on them to rounding (as in
  * gp_decode_attention).  Tables up to 8192 pages, 65535 requests, 8192 KV heads; (num_tokens
- * * G / 128 + num_reqs) * num_kv_heads below 2^24 (GP_ERR_UNSUPPORTED).  Takes the
+ * * G / 128 + num_reqs) * num_kv_heads below 2^23 (GP_ERR_UNSUPPORTED).  Takes the
  * GP_OP_PROMPT workspace of num_tokens or more. */
 gp_status_t gp_prompt_attention(const gp_kv_layer_t *kv, const gp_page_state_t *ps, const int32_t *tok_start,
                                 int32_t num_tokens, int32_t advanced, const void *q, int64_t q_stride,

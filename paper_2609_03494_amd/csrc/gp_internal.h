@@ -38,6 +38,17 @@ constexpr int kMaxPrefixSlotPages = 128;  // and at most (LDS id table)
 constexpr int kMaxDecodePages = 8192;     // table width the decode calls accept
 constexpr float kQ8KeyScale = 65536.0f;   // codes of 8-bit keys in units of their bfloat16 operands (see Page<E4m3>)
 constexpr int kPromptRows = 128;          // (token, query head) rows of a prompt attention item
+#ifndef GP_PROMPT_SLOTS
+#define GP_PROMPT_SLOTS 512
+#endif
+constexpr int kPromptSlots = GP_PROMPT_SLOTS;   // pieces of a small prompt attention call, all KV heads, about
+#ifndef GP_PROMPT_NARROW
+#define GP_PROMPT_NARROW 256
+#endif
+#ifndef GP_PROMPT_WIDE
+#define GP_PROMPT_WIDE 512
+#endif
+constexpr int kPromptLeastNarrow = GP_PROMPT_NARROW, kPromptLeastWide = GP_PROMPT_WIDE;   // tokens of a split item's piece at least
 constexpr int kMaxRopeTokens = 1 << 27;   // tokens one gp_append_rope call takes, and
 constexpr int kMaxListedHeads = 8192;     // KV heads it, the page bounds and the selection take: grids below 2^32 threads
 constexpr size_t kScratchBytes = size_t(8) << 20;   // static scratch of gp_decode_attention_noalloc
@@ -176,7 +187,35 @@ __host__ __device__ inline size_t select_ws(int R, int Hkv, int max_pages) {
     return align_up((size_t)R * Hkv * max_pages * sizeof(float) + 64);
 }
 
-__host__ __device__ inline size_t prompt_ws() { return kAlign; }
+// Division of a prompt attention call (see plan_kernel).  An item has kPromptRows / G
+// new tokens; pieces of a split item cost no less than the batch's share per slot, so all split
+// items together have at most twice as many pieces as there are slots.
+struct PromptWs {
+    size_t counts, pieces, merges, partial, total;
+    int64_t items;
+    int slots, max_pieces, max_merges, part_slots, part_rows;
+};
+__host__ __device__ inline PromptWs prompt_ws(int R, int64_t T, int Hq, int Hkv, int D) {
+    PromptWs w;
+    const int G = Hq / Hkv, tokens = kPromptRows / G;
+    w.items = T / tokens + (R < T ? R : T);
+    w.slots = cdiv(kPromptSlots, Hkv);
+    w.part_slots = 2 * w.slots + 2;
+    w.max_pieces = (int)w.items + w.part_slots;
+    w.max_merges = (int)(w.items < w.slots + 1 ? w.items : w.slots + 1);
+    w.part_rows = T * G < kPromptRows ? (int)(T * G + 31) / 32 * 32 : kPromptRows;
+    size_t off = 0;
+    w.counts = off;
+    off += kAlign;
+    w.pieces = off;
+    off = align_up(off + (size_t)w.max_pieces * 32);
+    w.merges = off;
+    off = align_up(off + (size_t)w.max_merges * 16);
+    w.partial = off;
+    off = align_up(off + (size_t)w.part_slots * Hkv * w.part_rows * (D + 2) * sizeof(float));
+    w.total = off;
+    return w;
+}
 
 struct ScoreWs {
     size_t cand, expz, part, weights, total;
@@ -335,8 +374,15 @@ struct PromptArgs {
     const int32_t *start;             // [R + 1] first token of each request; nullptr: one token each
     int64_t q_stride;                 // elements from token to token
     int R, T, Hkv, G, lg, max_pages, pool_pages, advanced;   // lg: log2 G
-    int tokens, places;               // new tokens of an item, items of one KV head at most
+    int tokens;                       // new tokens of an item
+    int slots;                        // pieces that the batch is divided into where items alone are fewer, about
+    int max_pieces, max_merges, part_rows;   // pieces and split items of one KV head at most; rows of a partial
     float qscale;                     // scale * log2(e); 8-bit: times kQ8KeyScale
+    // workspace regions (PromptWs)
+    int32_t *counts;                  // pieces, split items
+    int4 *pieces;                     // [max_pieces][2]: request, first token, token range; partial slot (-1: whole)
+    int4 *merges;                     // [max_merges]: request, first token, first slot, slots
+    float *partial;                   // [slot][Hkv]: outputs [part_rows][D], maxima and sums [part_rows]
 };
 
 struct BoundsArgs {

@@ -73,7 +73,7 @@ __device__ inline uint32_t pack_bf16(float a, float b) {             // to neare
 
 // 16 bytes a lane from base + off to LDS, `to` + 16 lane, past the registers.  Written as
 // assembly since the compiler makes every LDS read wait for all such loads in flight,
-// those into the other stage included; here the wave waits for them (kWaitVm0) before
+// those into the other stage included; here the wave waits for them (wait_loads) before
 // the barrier that hands the stage over.  No register is written.
 __device__ inline void load_lds(const void *base, uint32_t off, uint32_t to) {
     __asm__ volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(to) : "memory");
@@ -81,7 +81,10 @@ __device__ inline void load_lds(const void *base, uint32_t off, uint32_t to) {
 __device__ inline uint32_t lds_addr(const void *p) {
     return (uint32_t)(size_t)(__attribute__((address_space(3))) const char *)p;
 }
-constexpr int kWaitVm0 = 0x0F70;                                     // s_waitcnt vmcnt(0)
+// all but the newest N vector memory operations; all LDS reads
+template <int N>
+__device__ inline void wait_loads() { __asm__ volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+__device__ inline void wait_lds() { __asm__ volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
 
 // CACHE: bytes of a pool element (1: e4m3 codes, as bfloat16 in LDS).
 template <int CACHE, int D>
@@ -94,6 +97,7 @@ struct Tile {
     static constexpr int PU = D * CACHE;                             // 16-byte units of a page in the pool
     static constexpr int LOADS = PAGES * PU / kThreads;              // units of a thread
     static constexpr int PUR = PU / kPage;                           // units of a token in the pool
+    static constexpr int NARROW = 4 * BYTES / (64 * ROWB) < kWaves ? 4 * BYTES / (64 * ROWB) : kWaves;   // see prompt_kernel
     static_assert(PU % 64 == 0 && LOADS * kThreads == PAGES * PU, "a wave's unit lies in one page");
     // XOR-swizzle of a token's units.  Keys: 32 lanes read one unit of 32 tokens.  Values,
     // 16 bits: 32 lanes read 64 bytes of each of four tokens (transposed); 32 bits: 32 lanes
@@ -127,48 +131,164 @@ __device__ inline Asked asked(const PromptArgs &a, int r) {
     return q;
 }
 
-// the last request whose first place is at or before i (every lane the same)
-__device__ inline int request_at(const PromptArgs &a, int i, int lane) {
-    int lo = 0, hi = a.R;
-    while (hi - lo > 1) {
-        const int step = (hi - lo + 63) / 64, r = lo + lane * step;
-        const bool at = r < hi && max(a.start[min(r, a.R)], 0) / a.tokens + r <= i;
-        const int n = max(__popcll(__ballot(at)), 1);
-        lo += (n - 1) * step;
-        hi = min(hi, lo + step);
-    }
-    return uni(lo);
+// --------------------------------------------------------------- division --
+//
+// One workgroup divides the batch into pieces: an item is up to a.tokens new tokens of a
+// request, its cost the tokens that its last row sees (an item of up to 32 rows reads as many
+// bytes in the time that 128 rows take to multiply them); where items are fewer or longer than the
+// chip has places, an item's tokens are split into pieces of about the batch's share per place, each
+// with a partial result of its own.  Pieces go out longest first, sorted by cost in kBuckets
+// steps; their order within a step is whoever came first and has no bearing on any result.
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kBuckets = 256;
+
+struct Item { int r, j0, seen, parts, per; };          // per: tokens of a piece
+__device__ inline Item item_of(const PromptArgs &a, int r, const Asked &q, int i, int share) {
+    Item x;
+    x.r = r;
+    x.j0 = i * a.tokens;
+    const int n = min(a.tokens, q.n - x.j0);
+    x.seen = max(q.before + x.j0 + n, 0);
+    const int least = (n << a.lg) <= 32 ? kPromptLeastNarrow : kPromptLeastWide;
+    const int piece = max(share, least);
+    x.parts = x.seen > piece + piece / 4 ? (x.seen + piece - 1) / piece : 1;
+    x.per = ((x.seen + x.parts - 1) / x.parts + 63) / 64 * 64;
+    x.parts = max((x.seen + x.per - 1) / max(x.per, 1), 1);
+    return x;
 }
+
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PromptArgs a) {
+    __shared__ Asked s_asked[kPlanThreads];
+    __shared__ unsigned long long s_cost, s_tokens;
+    __shared__ int s_most, s_slots, s_merges, s_hist[kBuckets], s_wave[kBuckets / 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
+    if (tid < kBuckets) s_hist[tid] = 0;
+    if (tid == 0) {
+        s_cost = s_tokens = 0;
+        s_most = s_slots = s_merges = 0;
+    }
+    __syncthreads();
+    // the sum of costs, the largest, and all tokens
+    unsigned long long sum = 0, all = 0;
+    int most = 0;
+    for (int r = tid; r < a.R; r += kPlanThreads) {
+        const Asked q = asked(a, r);
+        if (r < kPlanThreads) s_asked[r] = q;
+        if (!q.in || q.n == 0) continue;
+        const unsigned long long n = q.n, items = (n + a.tokens - 1) / a.tokens;
+        sum += items * max(q.before, 0) + items * (items - 1) / 2 * a.tokens + n;
+        all += n;
+        most = max(most, q.before + q.n);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2) {
+        sum += __shfl_xor(sum, o, 64);
+        all += __shfl_xor(all, o, 64);
+        most = max(most, __shfl_xor(most, o, 64));
+    }
+    if (lane == 0) {
+        atomicAdd(&s_cost, sum);
+        atomicAdd(&s_tokens, all);
+        atomicMax(&s_most, most);
+    }
+    __syncthreads();
+    if (s_tokens > (unsigned long long)a.T) {         // (starts that decrease: more than the workspace is made for)
+        if (tid < 2) a.counts[tid] = 0;
+        return;
+    }
+    const int share = (int)((s_cost + a.slots - 1) / a.slots < INT_MAX / 2 ? (s_cost + a.slots - 1) / a.slots : INT_MAX / 2);
+    // pass 1: pieces per bucket; 2: pieces to their places
+    for (int pass = 1; pass < 3; ++pass) {
+        for (int r0 = 0; r0 < a.R; r0 += kPlanThreads) {
+            if (a.R > kPlanThreads) {
+                __syncthreads();
+                if (r0 + tid < a.R) s_asked[tid] = asked(a, r0 + tid);
+                __syncthreads();
+            }
+            for (int k = wave; k < kPlanThreads && r0 + k < a.R; k += kPlanWaves) {
+                const Asked q = s_asked[k];
+                if (!q.in) continue;
+                const int items = (q.n + a.tokens - 1) / a.tokens;
+                for (int i = lane; i < items; i += 64) {
+                    const Item x = item_of(a, r0 + k, q, i, share);
+                    const int cost = min(x.per, x.seen), bucket = kBuckets - 1 - (int)((int64_t)cost * (kBuckets - 1) / max(s_most, 1));
+                    if (pass == 1) {
+                        atomicAdd(&s_hist[bucket], x.parts);
+                        continue;
+                    }
+                    // (the bounds hold for any batch, see PromptWs)
+                    int slot = -1;
+                    if (x.parts > 1) {
+                        slot = atomicAdd(&s_slots, x.parts);
+                        const int at = atomicAdd(&s_merges, 1);
+                        if (at < a.max_merges) a.merges[at] = make_int4(x.r, x.j0, slot, x.parts);
+                    }
+                    int at = atomicAdd(&s_hist[bucket], x.parts);
+                    for (int p = 0; p < x.parts; ++p, ++at) {
+                        if (at >= a.max_pieces) break;
+                        a.pieces[2 * at] = make_int4(x.r, x.j0, p * x.per, min((p + 1) * x.per, x.seen));
+                        a.pieces[2 * at + 1].x = slot < 0 ? -1 : slot + p;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        if (pass == 1) {
+            // first place of each bucket
+            int n = 0, x = 0;
+            if (tid < kBuckets) {
+                n = x = s_hist[tid];
+#pragma unroll
+                for (int o = 1; o < 64; o *= 2) {
+                    const int y = __shfl_up(x, o, 64);
+                    if (lane >= o) x += y;
+                }
+                if (lane == 63) s_wave[wave] = x;
+            }
+            __syncthreads();
+            if (tid < kBuckets) {
+                for (int w = 0; w < wave; ++w) x += s_wave[w];
+                s_hist[tid] = x - n;
+                if (tid == kBuckets - 1) a.counts[0] = min(x, a.max_pieces);
+            }
+            __syncthreads();
+        }
+    }
+    if (tid == 0) a.counts[1] = min(s_merges, a.max_merges);
+}
+
+// ---------------------------------------------------------------- products --
 
 template <int CACHE, int D>
 __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
     using TL = Tile<CACHE, D>;
     using E = typename std::conditional<CACHE == 4, float, uint16_t>::type;
-    constexpr int TOK = TL::TOK, TB = TOK / 32, DB = D / 32, LOADS = TL::LOADS;
+    constexpr int TOK = TL::TOK, DB = D / 32, LOADS = TL::LOADS;
     constexpr int QS = CACHE == 4 ? D / 8 : D / 16;                  // 16-byte pieces of a row per lane
-    __shared__ __attribute__((aligned(16))) unsigned char s_k[2][TL::BYTES];
-    __shared__ __attribute__((aligned(16))) unsigned char s_v[2][TL::BYTES];
+    // a piece of up to 32 rows: each wave has tiles of 32 tokens, and LDS, to itself
+    constexpr int NW = TL::NARROW, NB = 32 * TL::ROWB, NL = NB / 1024;   // such waves; bytes of a tile's keys; pieces of 1024
+    constexpr int QL = CACHE == 1 ? D / 32 : 1;                      // 8-bit: 16-byte units of a lane, of such a tile
+    __shared__ __attribute__((aligned(16))) unsigned char s_mem[4 * TL::BYTES];
     __shared__ int s_odd[2];                                         // the tile whose values are not all finite
+    static_assert(NW * 2 * NB <= 4 * TL::BYTES && NW * 32 * D * 4 <= 4 * TL::BYTES, "LDS of narrow pieces");
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
-    const int h = blockIdx.x % a.Hkv, place = blockIdx.x / a.Hkv;
-    int r = place, j0 = 0;
-    if (a.start) {
-        r = request_at(a, place, lane);
-        j0 = (place - (max(scalar_load(a.start, r), 0) / a.tokens + r)) * a.tokens;
-    }
+    const int h = blockIdx.x % a.Hkv, at_piece = blockIdx.x / a.Hkv;
+    if (at_piece >= scalar_load(a.counts, 0)) return;
+    const int32_t *piece = reinterpret_cast<const int32_t *>(a.pieces + 2 * (size_t)at_piece);
+    const int r = scalar_load(piece, 0), j0 = scalar_load(piece, 1), from_token = scalar_load(piece, 2), to_token = scalar_load(piece, 3);
+    const int slot = scalar_load(piece, 4);
     const Asked rq = asked(a, r);
-    if (!rq.in || j0 < 0 || j0 >= rq.n) return;
     const int rows = min(a.tokens, rq.n - j0) << a.lg;               // of this item
-    const int first = rq.before + j0 + 1, last = rq.before + j0 + (rows >> a.lg);   // tokens that its first and last row see
-    const int tiles = last > 0 ? (last + TOK - 1) / TOK : 0;
+    const int first = rq.before + j0 + 1, last = to_token;           // tokens that its first row sees, the end of the piece
     const int last_page = max(last - 1, 0) / kPage;
+    const bool narrow = rows <= 32;
 
     // the wave's rows: a lane's row is its column of S^T and O^T
     const int col = lane & 31, half = lane >> 5;
-    const int row = wave * 32 + col, at = min(row, rows - 1);
-    const int sees = rq.before + j0 + (at >> a.lg) + 1;
-    const int wave_first = rq.before + j0 + (min(wave * 32, rows - 1) >> a.lg) + 1;
-    const int wave_last = wave * 32 < rows ? rq.before + j0 + (min(wave * 32 + 31, rows - 1) >> a.lg) + 1 : 0;
+    const int row0 = narrow ? 0 : wave * 32;
+    const int row = row0 + col, at = min(row, rows - 1);
+    const int sees = min(rq.before + j0 + (at >> a.lg) + 1, last);
+    const int wave_first = rq.before + j0 + (min(row0, rows - 1) >> a.lg) + 1;
+    const int wave_last = row0 < rows ? rq.before + j0 + (min(row0 + 31, rows - 1) >> a.lg) + 1 : 0;
     const int64_t token = rq.ts + j0 + (at >> a.lg);
     const int head = h * a.G + (at & (a.G - 1));
     u32x4_t q[QS];
@@ -177,49 +297,173 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
 #pragma unroll
         for (int s = 0; s < QS; ++s) q[s] = load16(src + s * (32 / (int)sizeof(E)));
     }
+    f32x16_t o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[d] = f32x16_t{};
+    float m = kNegInf, l = 0.0f;                                     // the row's maximum (both halves the same), this half's sum
+    const float unit = CACHE == 1 ? 1.0f : a.qscale;                 // scores to units of log2 (8-bit: in them already)
 
-    // a tile's way from the pools to LDS: a wave takes LOADS pieces of 1024 bytes each of
-    // the keys and the values, 8-bit ones through registers, where they are widened
-    const int32_t *table = a.page_table + (size_t)r * a.max_pages;
-    const size_t slice = (size_t)h * kPage * D * CACHE, page_bytes = (size_t)a.Hkv * kPage * D * CACHE;
-    u32x4_t kr[CACHE == 1 ? LOADS : 1], vr[CACHE == 1 ? LOADS : 1];
-    float ks[2][TL::PAGES], vs[2][TL::PAGES];                        // 8-bit: scales, of the tile in work and the next
-    int ids[LOADS], pids[TL::PAGES];                                 // pages of the next pieces; 8-bit: of the next tile
-    auto page_of = [&](int tile, int pg) { return scalar_load(table, min(tile * TL::PAGES + pg, last_page)); };
-    auto inside = [&](int id) { return min(max(id, 0), a.pool_pages - 1); };
-    auto request = [&](int tile) {
+    // S^T of TB blocks of 32 tokens, whose keys lie at kb
+    auto scores = [&](auto &st, const unsigned char *kb) {
+        constexpr int TB = sizeof(st) / sizeof(f32x16_t);
+        kb += col * TL::ROWB;
+        const int sw = TL::key_swizzle(col);
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) ids[i] = page_of(tile, (i * kThreads + wave * 64) / TL::PU);
-        if constexpr (CACHE == 1)
+        for (int tb = 0; tb < TB; ++tb) {
+            st[tb] = f32x16_t{};
 #pragma unroll
-            for (int p = 0; p < TL::PAGES; ++p) pids[p] = page_of(tile, p);
-    };
-    auto load = [&](int buf) {
+            for (int s = 0; s < QS; ++s) {
+                const u32x4_t x = *reinterpret_cast<const u32x4_t *>(kb + tb * 32 * TL::ROWB + (((2 * s + half) ^ sw) << 4));
+                if constexpr (CACHE == 4) {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int piece = i * kWaves + wave;
-            const size_t from = inside(ids[i]) * page_bytes + slice + (size_t)(piece * 64 % TL::PU) * 16;
-            const char *kp = static_cast<const char *>(a.k) + from, *vp = static_cast<const char *>(a.v) + from;
-            if constexpr (CACHE == 1) {
-                kr[i] = reinterpret_cast<const u32x4_t *>(kp)[lane];
-                vr[i] = reinterpret_cast<const u32x4_t *>(vp)[lane];
-            } else {
-                // the unit that belongs at the lane's place in LDS
-                const int t = (piece * 64 + lane) / TL::UPR, c = lane % TL::UPR;
-                const int ku = (lane & ~(TL::UPR - 1)) + (c ^ TL::key_swizzle(t)), vu = (lane & ~(TL::UPR - 1)) + (c ^ TL::value_swizzle(t));
-                load_lds(kp, ku * 16, lds_addr(s_k[buf] + piece * 1024));
-                load_lds(vp, vu * 16, lds_addr(s_v[buf] + piece * 1024));
+                    for (int e = 0; e < 4; ++e)
+                        st[tb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(q[s][e]), st[tb], 0, 0, 0);
+                } else {
+                    st[tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, q[s]), st[tb], 0, 0, 0);
+                }
             }
         }
+    };
+    // scores of tokens t0 .. to weights, the maximum, sum and outputs so far to the new maximum;
+    // ks, vs: 8-bit pages' scales
+    auto weigh = [&](auto &st, int t0, const float *ks, const float *vs) {
+        constexpr int TB = sizeof(st) / sizeof(f32x16_t);
         if constexpr (CACHE == 1) {
 #pragma unroll
-            for (int p = 0; p < TL::PAGES; ++p) {
-                const int64_t sc = (int64_t)inside(pids[p]) * a.Hkv + h;
-                ks[1][p] = scalar_load(a.k_scale, sc);
-                vs[1][p] = scalar_load(a.v_scale, sc);
+            for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st[tb][i] *= __builtin_amdgcn_fmed3f(a.qscale * ks[2 * tb + i / 8], FLT_TRUE_MIN, FLT_MAX);
+        }
+        if (t0 + 32 * TB > min(wave_first, last)) {
+            const int left = sees - t0 - 4 * half;                   // tokens that the row sees, from this half's first on
+#pragma unroll
+            for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st[tb][i] = masked(st[tb][i], tb * 32 + 8 * (i / 4) + i % 4 - left);
+        }
+        float top = st[0][0];
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, st[tb][i]);
+        top = max_halves(top);
+        // (a maximum may lag by 8 in log2: weights up to 2^8, relative errors as they are)
+        if (__any(top * unit > m * unit + 8.0f)) {
+            const float up = fmaxf(m, top), f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f((m - up) * unit);
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+            m = up;
+        }
+        const float from = m == kNegInf ? 0.0f : m * unit;           // (a row that sees nothing yet)
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                st[tb][i] = __builtin_amdgcn_exp2f(fmaf(st[tb][i], unit, -from));
+                l += st[tb][i];
+            }
+        if constexpr (CACHE == 1) {
+#pragma unroll
+            for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st[tb][i] *= vs[2 * tb + i / 8];
+        }
+    };
+    // O^T += V^T P^T.  odd_values: some value of a token that not every row sees is infinite or NaN,
+    // and a weight of zero would not keep it out; then the finite values, and where there are infinite
+    // ones or NaN, are multiplied on their own
+    auto values = [&](auto &st, const unsigned char *vb, bool odd_values) {
+        constexpr int TB = sizeof(st) / sizeof(f32x16_t);
+        auto add_part = [&](int d, int part, const f32x16_t &y) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] += part == 0 ? y[i] : y[i] > 0.0f ? (part == 1 ? __builtin_huge_valf() : kNegInf) : 0.0f;
+        };
+        if constexpr (CACHE == 4) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                auto value = [&](int tb, int i) {
+                    const int t = tb * 32 + 8 * (i / 4) + 4 * half + i % 4, u = (d * 32 + col) / 4;
+                    return *reinterpret_cast<const float *>(vb + t * TL::ROWB + ((u ^ TL::value_swizzle(t)) << 4) + (col & 3) * 4);
+                };
+                if (odd_values) {
+                    for (int part = 0; part < 3; ++part) {           // finite values; where +inf or NaN, where -inf or NaN
+                        f32x16_t y = {};
+#pragma unroll
+                        for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const float x = value(tb, i);
+                                const bool mine = x != x || x == (part == 1 ? __builtin_huge_valf() : kNegInf);
+                                const float z = part == 0 ? (fabsf(x) < __builtin_huge_valf() ? x : 0.0f) : mine ? 1.0f : 0.0f;
+                                y = __builtin_amdgcn_mfma_f32_32x32x2f32(z, st[tb][i], y, 0, 0, 0);
+                            }
+                        add_part(d, part, y);
+                    }
+                } else {
+#pragma unroll
+                    for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(tb, i), st[tb][i], o[d], 0, 0, 0);
+                }
+            }
+        } else {
+            u32x4_t p[2 * TB];
+#pragma unroll
+            for (int k = 0; k < 2 * TB; ++k)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) p[k][c] = pack_bf16(st[k / 2][8 * (k % 2) + 2 * c], st[k / 2][8 * (k % 2) + 2 * c + 1]);
+            // lane j of a group of 16 names four dims of token j / 4 and receives dim j of the four tokens
+            const int g = (lane >> 4) & 1, tt = 4 * half + ((lane & 15) >> 2), cc = 2 * g + ((lane & 3) >> 1);
+            const uint32_t v0 = (uint32_t)(tt * TL::ROWB + ((cc ^ TL::value_swizzle(tt)) << 4) + (lane & 1) * 8);
+            typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+            auto read = [&](int k, int d) {                          // values of k-step k, dims 32 d ..: V^T's operand
+                // (units 4 d of a token: the swizzle flips units of 4, which 4 d xors with)
+                const unsigned char *x = vb + (v0 ^ (uint32_t)(d << 6)) + k * 16 * TL::ROWB;
+                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(x));
+                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(x + 8 * TL::ROWB));
+                const u32x2_t y0 = __builtin_bit_cast(u32x2_t, lo), y1 = __builtin_bit_cast(u32x2_t, hi);
+                return u32x4_t{y0[0], y0[1], y1[0], y1[1]};
+            };
+            if (odd_values) {
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+                    for (int part = 0; part < 3; ++part) {
+                        f32x16_t y = {};
+#pragma unroll
+                        for (int k = 0; k < 2 * TB; ++k) {
+                            u32x4_t x = read(k, d);
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                uint32_t z = 0;
+#pragma unroll
+                                for (int s = 0; s < 32; s += 16) {
+                                    const uint32_t e = (x[c] >> s) & 0xffff, size = e & 0x7fff;
+                                    const bool mine = size > 0x7f80 || e == (part == 1 ? 0x7f80u : 0xff80u);
+                                    z |= part == 0 ? (size < 0x7f80 ? e << s : 0u) : mine ? 0x3f80u << s : 0u;
+                                }
+                                x[c] = z;
+                            }
+                            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, p[k]), y, 0, 0, 0);
+                        }
+                        add_part(d, part, y);
+                    }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 2 * TB; ++k)
+#pragma unroll
+                    for (int d = 0; d < DB; ++d)
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, read(k, d)), __builtin_bit_cast(bf16x8_t, p[k]), o[d], 0, 0, 0);
             }
         }
     };
+
+    const int32_t *table = a.page_table + (size_t)r * a.max_pages;
+    const size_t slice = (size_t)h * kPage * D * CACHE, page_bytes = (size_t)a.Hkv * kPage * D * CACHE;
+    auto page_of = [&](int page) { return scalar_load(table, min(page, last_page)); };
+    auto inside = [&](int id) { return min(max(id, 0), a.pool_pages - 1); };
     auto widen = [](uint32_t x0, uint32_t x1, float scale) {
         const bf16x2_t p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x0, scale, false), p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x0, scale, true);
         const bf16x2_t p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x1, scale, false), p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x1, scale, true);
@@ -234,229 +478,261 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
         }
         return is;
     };
-    // the loaded tile stands in LDS after this and a barrier.  border: some row does not see
-    // all of its tokens: values behind the request's tokens become zero (whatever lies there),
-    // and a tile is marked that has infinite values or NaN among the others
-    auto settle = [&](int tile, int buf, bool border) {
-        bool found = false;
-        if constexpr (CACHE == 1) {
+    constexpr float key_unit = 1.0f / kQ8KeyScale;                   // (see Page<E4m3>::kKeyUnit of the decode kernel)
+    // 16 codes of unit c of token t, widened, to the rows at `to`
+    auto put_codes = [&](unsigned char *to, int t, int c, int swizzle, const u32x4_t &x, float scale) {
+        u32x4_t *row_ = reinterpret_cast<u32x4_t *>(to + t * TL::ROWB);
+        row_[(2 * c) ^ swizzle] = widen(x[0], x[1], scale);
+        row_[(2 * c + 1) ^ swizzle] = widen(x[2], x[3], scale);
+    };
+    u32x4_t kr[QL], vr[QL];
+    static_assert(CACHE != 1 || QL >= LOADS, "registers of both kinds of tile");
+
+    if (!narrow) {
+        // a tile's way from the pools to LDS: a wave takes LOADS pieces of 1024 bytes each of
+        // the keys and the values, 8-bit ones through registers, where they are widened
+        const int tile0 = from_token / TOK, tiles = (last + TOK - 1) / TOK;
+        float ks[2][TL::PAGES], vs[2][TL::PAGES];                    // 8-bit: scales, of the tile in work and the next
+        int ids[LOADS], pids[TL::PAGES];                             // pages of the next pieces; 8-bit: of the next tile
+        auto s_k = [&](int buf) { return s_mem + buf * TL::BYTES; };
+        auto s_v = [&](int buf) { return s_mem + (2 + buf) * TL::BYTES; };
+        auto request = [&](int tile) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) ids[i] = page_of(tile * TL::PAGES + (i * kThreads + wave * 64) / TL::PU);
+            if constexpr (CACHE == 1)
+#pragma unroll
+                for (int p = 0; p < TL::PAGES; ++p) pids[p] = page_of(tile * TL::PAGES + p);
+        };
+        auto load = [&](int buf) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                const int u = i * kThreads + tid, t = u / TL::PUR, c = u % TL::PUR;
-                u32x4_t *kt = reinterpret_cast<u32x4_t *>(s_k[buf] + t * TL::ROWB), *vt = reinterpret_cast<u32x4_t *>(s_v[buf] + t * TL::ROWB);
-                const int sk = TL::key_swizzle(t), sv = TL::value_swizzle(t);
-                if (border && tile * TOK + t >= last) vr[i] = u32x4_t{};
-                constexpr float unit = 1.0f / kQ8KeyScale;           // (see Page<E4m3>::kKeyUnit of the decode kernel)
-                const u32x4_t v0 = widen(vr[i][0], vr[i][1], 1.0f), v1 = widen(vr[i][2], vr[i][3], 1.0f);
-                kt[(2 * c) ^ sk] = widen(kr[i][0], kr[i][1], unit);
-                kt[(2 * c + 1) ^ sk] = widen(kr[i][2], kr[i][3], unit);
-                vt[(2 * c) ^ sv] = v0;
-                vt[(2 * c + 1) ^ sv] = v1;
-                if (border) found |= odd(v0) || odd(v1);
+                const int part = i * kWaves + wave;
+                const size_t from = inside(ids[i]) * page_bytes + slice + (size_t)(part * 64 % TL::PU) * 16;
+                const char *kp = static_cast<const char *>(a.k) + from, *vp = static_cast<const char *>(a.v) + from;
+                if constexpr (CACHE == 1) {
+                    kr[i] = reinterpret_cast<const u32x4_t *>(kp)[lane];
+                    vr[i] = reinterpret_cast<const u32x4_t *>(vp)[lane];
+                } else {
+                    // the unit that belongs at the lane's place in LDS
+                    const int t = (part * 64 + lane) / TL::UPR, c = lane % TL::UPR;
+                    const int ku = (lane & ~(TL::UPR - 1)) + (c ^ TL::key_swizzle(t)), vu = (lane & ~(TL::UPR - 1)) + (c ^ TL::value_swizzle(t));
+                    load_lds(kp, ku * 16, lds_addr(s_k(buf) + part * 1024));
+                    load_lds(vp, vu * 16, lds_addr(s_v(buf) + part * 1024));
+                }
             }
-        } else {
-            __builtin_amdgcn_s_waitcnt(kWaitVm0);
-            if (border) {
-                __asm__ volatile("" ::: "memory");
+            if constexpr (CACHE == 1) {
+#pragma unroll
+                for (int p = 0; p < TL::PAGES; ++p) {
+                    const int64_t sc = (int64_t)inside(pids[p]) * a.Hkv + h;
+                    ks[1][p] = scalar_load(a.k_scale, sc);
+                    vs[1][p] = scalar_load(a.v_scale, sc);
+                }
+            }
+        };
+        // the loaded tile stands in LDS after this and a barrier.  On the border, where some row does not
+        // see all of its tokens, values behind the piece's tokens become zero (whatever lies there),
+        // and a tile is marked that has infinite values or NaN among the others
+        auto settle = [&](int tile, int buf) {
+            const bool border = (tile + 1) * TOK > min(first, last);
+            bool found = false;
+            if constexpr (CACHE == 1) {
 #pragma unroll
                 for (int i = 0; i < LOADS; ++i) {
-                    const int u = (i * kWaves + wave) * 64 + lane;
-                    u32x4_t *at = reinterpret_cast<u32x4_t *>(s_v[buf]) + u;
-                    if (tile * TOK + u / TL::UPR >= last) *at = u32x4_t{};
-                    else found |= odd(*at);
-                }
-            }
-        }
-        if (border && __any(found) && lane == 0) s_odd[buf] = tile;
-    };
-    auto on_border = [&](int tile) { return (tile + 1) * TOK > first; };
-
-    f32x16_t o[DB];
-#pragma unroll
-    for (int d = 0; d < DB; ++d) o[d] = f32x16_t{};
-    float m = kNegInf, l = 0.0f;                                     // the row's maximum (both halves the same), this half's sum
-    if (tid < 2) s_odd[tid] = -1;
-    if (tiles > 0) {
-        request(0);
-        load(0);
-        request(1);
-    }
-    __syncthreads();
-    if (tiles > 0) settle(0, 0, on_border(0));
-    __syncthreads();
-    for (int tile = 0; tile < tiles; ++tile) {
-        const int buf = tile & 1;
-        if constexpr (CACHE == 1) {
-#pragma unroll
-            for (int p = 0; p < TL::PAGES; ++p) {
-                ks[0][p] = ks[1][p];
-                vs[0][p] = vs[1][p];
-            }
-        }
-        if (tile + 1 < tiles) {
-            load(buf ^ 1);
-            request(tile + 2);
-        }
-        if (tile * TOK < wave_last) {
-            // S^T
-            f32x16_t st[TB];
-            const unsigned char *kb = s_k[buf] + col * TL::ROWB;
-            const int sw = TL::key_swizzle(col);
-#pragma unroll
-            for (int tb = 0; tb < TB; ++tb) {
-                st[tb] = f32x16_t{};
-#pragma unroll
-                for (int s = 0; s < QS; ++s) {
-                    const u32x4_t x = *reinterpret_cast<const u32x4_t *>(kb + tb * 32 * TL::ROWB + (((2 * s + half) ^ sw) << 4));
-                    if constexpr (CACHE == 4) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            st[tb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(q[s][e]), st[tb], 0, 0, 0);
-                    } else {
-                        st[tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, q[s]), st[tb], 0, 0, 0);
-                    }
-                }
-            }
-            // (8-bit: in units of log2, with the page's scale; the others' scale comes with the difference)
-            if constexpr (CACHE == 1) {
-#pragma unroll
-                for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) st[tb][i] *= __builtin_amdgcn_fmed3f(a.qscale * ks[0][2 * tb + i / 8], FLT_TRUE_MIN, FLT_MAX);
-            }
-            const float unit = CACHE == 1 ? 1.0f : a.qscale;
-            if ((tile + 1) * TOK > wave_first) {
-                const int left = sees - tile * TOK - 4 * half;       // tokens of the tile that the row sees, from this half's first on
-#pragma unroll
-                for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        st[tb][i] = masked(st[tb][i], tb * 32 + 8 * (i / 4) + i % 4 - left);
-            }
-            float top = st[0][0];
-#pragma unroll
-            for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, st[tb][i]);
-            top = max_halves(top);
-            // (a maximum may lag by 8 in log2: weights up to 2^8, relative errors as they are)
-            if (__any(top * unit > m * unit + 8.0f)) {
-                const float up = fmaxf(m, top), f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f((m - up) * unit);
-                l *= f;
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= f;
-                m = up;
-            }
-            const float from = m == kNegInf ? 0.0f : m * unit;       // (a row that sees nothing yet)
-#pragma unroll
-            for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    st[tb][i] = __builtin_amdgcn_exp2f(fmaf(st[tb][i], unit, -from));
-                    l += st[tb][i];
-                }
-            if constexpr (CACHE == 1) {
-#pragma unroll
-                for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) st[tb][i] *= vs[0][2 * tb + i / 8];
-            }
-            // O^T
-            const bool odd_values = uni(s_odd[buf]) == tile;
-            const unsigned char *vb = s_v[buf];
-            if constexpr (CACHE == 4) {
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    auto value = [&](int tb, int i) {
-                        const int t = tb * 32 + 8 * (i / 4) + 4 * half + i % 4, u = (d * 32 + col) / 4;
-                        return *reinterpret_cast<const float *>(vb + t * TL::ROWB + ((u ^ TL::value_swizzle(t)) << 4) + (col & 3) * 4);
-                    };
-                    if (odd_values) {
-                        for (int part = 0; part < 3; ++part) {       // finite values; where +inf or NaN, where -inf or NaN
-                            f32x16_t y = {};
-#pragma unroll
-                            for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) {
-                                    const float x = value(tb, i);
-                                    const bool mine = x != x || x == (part == 1 ? __builtin_huge_valf() : kNegInf);
-                                    const float z = part == 0 ? (fabsf(x) < __builtin_huge_valf() ? x : 0.0f) : mine ? 1.0f : 0.0f;
-                                    y = __builtin_amdgcn_mfma_f32_32x32x2f32(z, st[tb][i], y, 0, 0, 0);
-                                }
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[d][i] += part == 0 ? y[i] : y[i] > 0.0f ? (part == 1 ? __builtin_huge_valf() : kNegInf) : 0.0f;
-                        }
-                    } else {
-#pragma unroll
-                        for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(tb, i), st[tb][i], o[d], 0, 0, 0);
-                    }
+                    const int u = i * kThreads + tid, t = u / TL::PUR, c = u % TL::PUR;
+                    if (border && tile * TOK + t >= last) vr[i] = u32x4_t{};
+                    put_codes(s_k(buf), t, c, TL::key_swizzle(t), kr[i], key_unit);
+                    put_codes(s_v(buf), t, c, TL::value_swizzle(t), vr[i], 1.0f);
+                    if (border) found |= odd(widen(vr[i][0], vr[i][1], 1.0f)) || odd(widen(vr[i][2], vr[i][3], 1.0f));
                 }
             } else {
-                u32x4_t p[2 * TB];
+                wait_loads<0>();
+                if (border) {
 #pragma unroll
-                for (int k = 0; k < 2 * TB; ++k)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) p[k][c] = pack_bf16(st[k / 2][8 * (k % 2) + 2 * c], st[k / 2][8 * (k % 2) + 2 * c + 1]);
-                // lane j of a group of 16 names four dims of token j / 4 and receives dim j of the four tokens
-                const int g = (lane >> 4) & 1, tt = 4 * half + ((lane & 15) >> 2), cc = 2 * g + ((lane & 3) >> 1);
-                const uint32_t v0 = (uint32_t)(tt * TL::ROWB + ((cc ^ TL::value_swizzle(tt)) << 4) + (lane & 1) * 8);
-                typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
-                auto read = [&](int k, int d) {                      // values of k-step k, dims 32 d ..: V^T's operand
-                    // (units 4 d of a token: the swizzle flips units of 4, which 4 d xors with)
-                    const unsigned char *x = vb + (v0 ^ (uint32_t)(d << 6)) + k * 16 * TL::ROWB;
-                    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(x));
-                    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(x + 8 * TL::ROWB));
-                    const u32x2_t y0 = __builtin_bit_cast(u32x2_t, lo), y1 = __builtin_bit_cast(u32x2_t, hi);
-                    return u32x4_t{y0[0], y0[1], y1[0], y1[1]};
-                };
-                if (odd_values) {
-#pragma unroll
-                    for (int d = 0; d < DB; ++d)
-                        for (int part = 0; part < 3; ++part) {       // finite values; where +inf or NaN, where -inf or NaN
-                            f32x16_t y = {};
-#pragma unroll
-                            for (int k = 0; k < 2 * TB; ++k) {
-                                u32x4_t x = read(k, d);
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) {
-                                    uint32_t z = 0;
-#pragma unroll
-                                    for (int s = 0; s < 32; s += 16) {
-                                        const uint32_t e = (x[c] >> s) & 0xffff, size = e & 0x7fff;
-                                        const bool mine = size > 0x7f80 || e == (part == 1 ? 0x7f80u : 0xff80u);
-                                        z |= part == 0 ? (size < 0x7f80 ? e << s : 0u) : mine ? 0x3f80u << s : 0u;
-                                    }
-                                    x[c] = z;
-                                }
-                                y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, p[k]), y, 0, 0, 0);
-                            }
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[d][i] += part == 0 ? y[i] : y[i] > 0.0f ? (part == 1 ? __builtin_huge_valf() : kNegInf) : 0.0f;
-                        }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 2 * TB; ++k)
-#pragma unroll
-                        for (int d = 0; d < DB; ++d)
-                            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, read(k, d)), __builtin_bit_cast(bf16x8_t, p[k]), o[d], 0, 0, 0);
+                    for (int i = 0; i < LOADS; ++i) {
+                        const int u = (i * kWaves + wave) * 64 + lane;
+                        u32x4_t *to = reinterpret_cast<u32x4_t *>(s_v(buf)) + u;
+                        if (tile * TOK + u / TL::UPR >= last) *to = u32x4_t{};
+                        else found |= odd(*to);
+                    }
                 }
             }
+            if (border && __any(found) && lane == 0) s_odd[buf] = tile;
+        };
+        if (tid < 2) s_odd[tid] = -1;
+        if (tiles > tile0) {
+            request(tile0);
+            load(tile0 & 1);
+            request(tile0 + 1);
         }
-        if (tile + 1 < tiles) settle(tile + 1, buf ^ 1, on_border(tile + 1));
         __syncthreads();
+        if (tiles > tile0) settle(tile0, tile0 & 1);
+        __syncthreads();
+        for (int tile = tile0; tile < tiles; ++tile) {
+            const int buf = tile & 1;
+            if constexpr (CACHE == 1) {
+#pragma unroll
+                for (int p = 0; p < TL::PAGES; ++p) {
+                    ks[0][p] = ks[1][p];
+                    vs[0][p] = vs[1][p];
+                }
+            }
+            if (tile + 1 < tiles) {
+                load(buf ^ 1);
+                request(tile + 2);
+            }
+            if (tile * TOK < wave_last) {
+                f32x16_t st[TOK / 32];
+                scores(st, s_k(buf));
+                weigh(st, tile * TOK, ks[0], vs[0]);
+                values(st, s_v(buf), uni(s_odd[buf]) == tile);
+            }
+            if (tile + 1 < tiles) settle(tile + 1, buf ^ 1);
+            __syncthreads();
+        }
+        l = sum_halves(l);
+    } else {
+        // every wave has its own tiles of 32 tokens, NW apart, keys and values in LDS once: the next
+        // keys are on their way as soon as the scores are there, the next values after the product
+        unsigned char *s_k = s_mem + wave * 2 * NB, *s_v = s_k + NB;
+        const int b1 = (last + 31) / 32, step = NW;
+        int b = wave < NW ? from_token / 32 + wave : b1;
+        int ids[2];
+        float ks[2], vs[2], kn[2], vn[2];
+        auto request = [&](int blk) {
+            ids[0] = page_of(2 * blk);
+            ids[1] = page_of(2 * blk + 1);
+        };
+        // keys (which: 0) or values of the requested tile
+        auto load = [&](int which) {
+            const char *pool = static_cast<const char *>(which ? a.v : a.k);
+            if constexpr (CACHE == 1) {
+#pragma unroll
+                for (int i = 0; i < QL; ++i) {
+                    const size_t from = inside(ids[i / (QL / 2)]) * page_bytes + slice + (size_t)(i % (QL / 2)) * 1024;
+                    (which ? vr : kr)[i] = reinterpret_cast<const u32x4_t *>(pool + from)[lane];
+                }
+#pragma unroll
+                for (int p = 0; p < 2; ++p) (which ? vn : kn)[p] = scalar_load(which ? a.v_scale : a.k_scale, (int64_t)inside(ids[p]) * a.Hkv + h);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NL; ++i) {
+                    const int t = (i * 64 + lane) / TL::UPR, c = lane % TL::UPR;
+                    const int u = (lane & ~(TL::UPR - 1)) + (c ^ (which ? TL::value_swizzle(t) : TL::key_swizzle(t)));
+                    const size_t from = inside(ids[i / (NL / 2)]) * page_bytes + slice + (size_t)(i % (NL / 2)) * 1024;
+                    load_lds(pool + from, u * 16, lds_addr((which ? s_v : s_k) + i * 1024));
+                }
+            }
+        };
+        if (b < b1) {
+            request(b);
+            load(0);
+            load(1);
+        }
+        for (; b < b1; b += step) {
+            const bool more = b + step < b1;
+            if (more) request(b + step);
+            if constexpr (CACHE == 1) {
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    ks[p] = kn[p];
+                    vs[p] = vn[p];
+                }
+#pragma unroll
+                for (int i = 0; i < QL; ++i) {
+                    const int t = (i * 64 + lane) / TL::PUR, c = lane % TL::PUR;
+                    put_codes(s_k, t, c, TL::key_swizzle(t), kr[i], key_unit);
+                }
+            } else {
+                wait_loads<NL>();                                    // (the values, behind the keys, may be under way)
+            }
+            f32x16_t st[1];
+            scores(st, s_k);
+            wait_lds();                                              // the keys are read
+            if (more) load(0);
+            weigh(st, b * 32, ks, vs);
+            const bool border = (b + 1) * 32 > min(first, last);
+            bool found = false;
+            if constexpr (CACHE == 1) {
+#pragma unroll
+                for (int i = 0; i < QL; ++i) {
+                    const int t = (i * 64 + lane) / TL::PUR, c = lane % TL::PUR;
+                    if (border && b * 32 + t >= last) vr[i] = u32x4_t{};
+                    put_codes(s_v, t, c, TL::value_swizzle(t), vr[i], 1.0f);
+                    if (border) found |= odd(widen(vr[i][0], vr[i][1], 1.0f)) || odd(widen(vr[i][2], vr[i][3], 1.0f));
+                }
+            } else {
+                if (more) wait_loads<NL>();
+                else wait_loads<0>();
+                if (border) {
+                    for (int i = 0; i < NL; ++i) {
+                        u32x4_t *to = reinterpret_cast<u32x4_t *>(s_v + i * 1024) + lane;
+                        if (b * 32 + (i * 64 + lane) / TL::UPR >= last) *to = u32x4_t{};
+                        else found |= odd(*to);
+                    }
+                }
+            }
+            values(st, s_v, border && __any(found));
+            wait_lds();
+            if (more) load(1);
+        }
+        l = sum_halves(l);
+        // the waves' parts meet in LDS: outputs as [wave][32 rows][D], swizzled by 16-byte units
+        __syncthreads();
+        __shared__ float s_ml[2][NW][32];
+        float *s_o = reinterpret_cast<float *>(s_mem);
+        auto unit_of = [&](int rr, int u) { return rr * (D / 4) + (u ^ (rr & 15)); };
+        if (wave < NW) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    reinterpret_cast<f32x4_t *>(s_o + wave * 32 * D)[unit_of(col, 8 * d + 2 * i + half)] =
+                        f32x4_t{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+            if (half == 0) {
+                s_ml[0][wave][col] = m;
+                s_ml[1][wave][col] = l;
+            }
+        }
+        __syncthreads();
+        float mx = kNegInf, f[NW], sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) mx = fmaxf(mx, s_ml[0][w][col]);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float mw = s_ml[0][w][col], lw = s_ml[1][w][col];
+            f[w] = mw == kNegInf ? 0.0f : __builtin_amdgcn_exp2f((mw - mx) * unit);
+            sum += lw * f[w];                                        // (no weight: lw is 0, or NaN, which stays)
+        }
+        // wave w finishes a share of the units
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if ((d * 4 + i) % kWaves != wave) continue;
+                f32x4_t y = {};
+#pragma unroll
+                for (int w = 0; w < NW; ++w) {
+                    const f32x4_t x = reinterpret_cast<const f32x4_t *>(s_o + w * 32 * D)[unit_of(col, 8 * d + 2 * i + half)];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) y[c] += f[w] == 0.0f ? 0.0f : x[c] * f[w];
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) o[d][4 * i + c] = y[c];
+            }
+        m = mx;
+        l = sum;
     }
-    l = sum_halves(l);
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    if (row < rows) {
+
+    // a whole item's outputs, or a piece's part of them (wave-uniform).  Narrow: every wave its share of the dims
+    if (row >= rows) return;
+    if (slot < 0) {
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
         E *to = reinterpret_cast<E *>(a.out) + (token * a.Hkv * a.G + head) * D + 4 * half;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
+                if (narrow && (d * 4 + i) % kWaves != wave) continue;
                 float x[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) x[c] = l > 0.0f ? o[d][4 * i + c] * inv : 0.0f;
@@ -465,16 +741,77 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
                 else
                     *reinterpret_cast<u32x2_e2_t *>(to + 32 * d + 8 * i) = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
             }
+    } else {
+        float *to = a.partial + ((size_t)slot * a.Hkv + h) * a.part_rows * (D + 2);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (narrow && (d * 4 + i) % kWaves != wave) continue;
+                *reinterpret_cast<f32x4_t *>(to + (size_t)row * D + 32 * d + 8 * i + 4 * half) =
+                    f32x4_t{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+            }
+        if (half == 0 && (!narrow || wave == 0)) {
+            float *ml = to + (size_t)a.part_rows * D;
+            ml[row] = m * unit;
+            ml[a.part_rows + row] = l;
+        }
     }
+}
+
+// Parts of split items to outputs: 32 rows of an item and KV head, D / 4 threads a row.
+template <typename E, int D>
+__global__ __launch_bounds__(256) void merge_kernel(PromptArgs a) {
+    constexpr int LANES = D / 4, ROWS = 256 / LANES;
+    const int h = blockIdx.x % a.Hkv, at = blockIdx.x / a.Hkv;
+    if (at >= scalar_load(a.counts, 1)) return;
+    const int4 x = a.merges[at];
+    const Asked rq = asked(a, x.x);
+    const int rows = min(a.tokens, rq.n - x.y) << a.lg;
+    const int u = threadIdx.x % LANES;
+    for (int row = blockIdx.y * 32 + threadIdx.x / LANES; row < min(rows, (int)blockIdx.y * 32 + 32); row += ROWS) {
+        const size_t stride = (size_t)a.Hkv * a.part_rows * (D + 2);
+        const float *p = a.partial + ((size_t)x.z * a.Hkv + h) * a.part_rows * (D + 2);
+        const float *ml = p + (size_t)a.part_rows * D + row;
+        float m = kNegInf, l = 0.0f;
+        f32x4_t o = {};
+        for (int k = 0; k < x.w; ++k) {
+            const float mk = ml[k * stride], lk = ml[k * stride + a.part_rows];
+            const f32x4_t ok = *reinterpret_cast<const f32x4_t *>(p + k * stride + (size_t)row * D + 4 * u);
+            const float up = fmaxf(m, mk);
+            const float f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - up), g = mk == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(mk - up);
+            l = l * f + lk * g;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[c] = (f == 0.0f ? 0.0f : o[c] * f) + (g == 0.0f ? 0.0f : ok[c] * g);
+            m = up;
+        }
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        float y[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] = l > 0.0f ? o[c] * inv : 0.0f;
+        const int64_t token = rq.ts + x.y + (row >> a.lg);
+        E *to = reinterpret_cast<E *>(a.out) + (token * a.Hkv * a.G + h * a.G + (row & (a.G - 1))) * D + 4 * u;
+        if constexpr (sizeof(E) == 4)
+            *reinterpret_cast<u32x4_e4_t *>(to) = u32x4_t{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])};
+        else
+            *reinterpret_cast<u32x2_e2_t *>(to) = u32x2_t{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+    }
+}
+
+template <int CACHE, int D>
+void launch_cd(const PromptArgs &a, hipStream_t s) {
+    plan_kernel<<<1, kPlanThreads, 0, s>>>(a);
+    prompt_kernel<CACHE, D><<<a.max_pieces * a.Hkv, kThreads, 0, s>>>(a);
+    using E = typename std::conditional<CACHE == 4, float, uint16_t>::type;
+    if (a.max_merges) merge_kernel<E, D><<<dim3(a.max_merges * a.Hkv, a.part_rows / 32), 256, 0, s>>>(a);
 }
 
 }  // namespace
 
 hipError_t launch_prompt(int cache, int D, const PromptArgs &a, hipStream_t s) {
-    const int grid = a.places * a.Hkv;
-    if (cache == 1) D == 128 ? prompt_kernel<1, 128><<<grid, kThreads, 0, s>>>(a) : prompt_kernel<1, 64><<<grid, kThreads, 0, s>>>(a);
-    else if (cache == 2) D == 128 ? prompt_kernel<2, 128><<<grid, kThreads, 0, s>>>(a) : prompt_kernel<2, 64><<<grid, kThreads, 0, s>>>(a);
-    else D == 128 ? prompt_kernel<4, 128><<<grid, kThreads, 0, s>>>(a) : prompt_kernel<4, 64><<<grid, kThreads, 0, s>>>(a);
+    if (cache == 1) D == 128 ? launch_cd<1, 128>(a, s) : launch_cd<1, 64>(a, s);
+    else if (cache == 2) D == 128 ? launch_cd<2, 128>(a, s) : launch_cd<2, 64>(a, s);
+    else D == 128 ? launch_cd<4, 128>(a, s) : launch_cd<4, 64>(a, s);
     return hipGetLastError();
 }
 
