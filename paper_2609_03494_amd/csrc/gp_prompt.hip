@@ -86,19 +86,19 @@ template <int N>
 __device__ inline void wait_loads() { __asm__ volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
 __device__ inline void wait_lds() { __asm__ volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
 
-// CACHE: bytes of a pool element (1: e4m3 codes, as bfloat16 in LDS).
+// CACHE: bytes of a pool element (1: e4m3 codes, as bfloat16 in LDS).  Keys and values go
+// through LDS in blocks of 32 tokens.
 template <int CACHE, int D>
-struct Tile {
+struct Block {
     static constexpr int LB = CACHE == 4 ? 4 : 2;                    // bytes of an element in LDS
-    static constexpr int TOK = CACHE == 4 && D == 128 ? 32 : 64;     // tokens of a tile
     static constexpr int ROWB = D * LB, UPR = ROWB / 16;             // bytes and 16-byte units of a token
-    static constexpr int BYTES = TOK * ROWB;                         // of the keys, or the values
-    static constexpr int PAGES = TOK / kPage;
-    static constexpr int PU = D * CACHE;                             // 16-byte units of a page in the pool
-    static constexpr int LOADS = PAGES * PU / kThreads;              // units of a thread
-    static constexpr int PUR = PU / kPage;                           // units of a token in the pool
-    static constexpr int NARROW = 4 * BYTES / (64 * ROWB) < kWaves ? 4 * BYTES / (64 * ROWB) : kWaves;   // see prompt_kernel
-    static_assert(PU % 64 == 0 && LOADS * kThreads == PAGES * PU, "a wave's unit lies in one page");
+    static constexpr int BYTES = 32 * ROWB;                          // of the keys, or the values
+    static constexpr int PU = D * CACHE, PUR = PU / kPage;           // 16-byte units of a page in the pool, of a token
+    static constexpr int STAGES = CACHE == 4 && D == 128 ? 2 : 3;    // blocks of keys, and of values, in LDS
+    static constexpr int LOADS = CACHE == 1 ? 2 * PU / kThreads : BYTES / 1024 / kWaves;   // pieces of 1024 bytes of a wave
+    static constexpr int NARROW = CACHE == 4 && D == 128 ? 2 : kWaves;   // waves with a block of their own, see prompt_kernel
+    static constexpr int MEM = 2 * BYTES * (STAGES > NARROW ? STAGES : NARROW);
+    static_assert(LOADS >= 1 || CACHE == 1, "each wave has a piece");
     // XOR-swizzle of a token's units.  Keys: 32 lanes read one unit of 32 tokens.  Values,
     // 16 bits: 32 lanes read 64 bytes of each of four tokens (transposed); 32 bits: 32 lanes
     // 128 bytes of one token, the other lanes of the fourth after it.
@@ -260,16 +260,16 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PromptArgs a) {
 
 template <int CACHE, int D>
 __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
-    using TL = Tile<CACHE, D>;
+    using TL = Block<CACHE, D>;
     using E = typename std::conditional<CACHE == 4, float, uint16_t>::type;
-    constexpr int TOK = TL::TOK, DB = D / 32, LOADS = TL::LOADS;
+    constexpr int DB = D / 32, LOADS = TL::LOADS;
     constexpr int QS = CACHE == 4 ? D / 8 : D / 16;                  // 16-byte pieces of a row per lane
-    // a piece of up to 32 rows: each wave has tiles of 32 tokens, and LDS, to itself
-    constexpr int NW = TL::NARROW, NB = 32 * TL::ROWB, NL = NB / 1024;   // such waves; bytes of a tile's keys; pieces of 1024
-    constexpr int QL = CACHE == 1 ? D / 32 : 1;                      // 8-bit: 16-byte units of a lane, of such a tile
-    __shared__ __attribute__((aligned(16))) unsigned char s_mem[4 * TL::BYTES];
-    __shared__ int s_odd[2];                                         // the tile whose values are not all finite
-    static_assert(NW * 2 * NB <= 4 * TL::BYTES && NW * 32 * D * 4 <= 4 * TL::BYTES, "LDS of narrow pieces");
+    // a piece of up to 32 rows: each wave has blocks, and LDS, to itself
+    constexpr int NW = TL::NARROW, NB = TL::BYTES, NL = NB / 1024;   // such waves; a block's keys, in pieces of 1024 bytes
+    constexpr int QL = CACHE == 1 ? D / 32 : 1;                      // 8-bit: 16-byte units of a lane, of such a block
+    __shared__ __attribute__((aligned(16))) unsigned char s_mem[TL::MEM];
+    __shared__ uint32_t s_odd[4];                                    // wide: tokens of block b whose values are not all finite, b % 4; narrow: of the wave's
+    static_assert(NW * 32 * D * 4 <= TL::MEM, "the waves' parts meet in LDS");
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
     const int h = blockIdx.x % a.Hkv, at_piece = blockIdx.x / a.Hkv;
     if (at_piece >= scalar_load(a.counts, 0)) return;
@@ -303,49 +303,38 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
     float m = kNegInf, l = 0.0f;                                     // the row's maximum (both halves the same), this half's sum
     const float unit = CACHE == 1 ? 1.0f : a.qscale;                 // scores to units of log2 (8-bit: in them already)
 
-    // S^T of TB blocks of 32 tokens, whose keys lie at kb
-    auto scores = [&](auto &st, const unsigned char *kb) {
-        constexpr int TB = sizeof(st) / sizeof(f32x16_t);
+    // S^T of the 32 tokens whose keys lie at kb
+    auto scores = [&](f32x16_t &st, const unsigned char *kb) __attribute__((always_inline)) {
         kb += col * TL::ROWB;
         const int sw = TL::key_swizzle(col);
+        st = f32x16_t{};
 #pragma unroll
-        for (int tb = 0; tb < TB; ++tb) {
-            st[tb] = f32x16_t{};
+        for (int s = 0; s < QS; ++s) {
+            const u32x4_t x = *reinterpret_cast<const u32x4_t *>(kb + (((2 * s + half) ^ sw) << 4));
+            if constexpr (CACHE == 4) {
 #pragma unroll
-            for (int s = 0; s < QS; ++s) {
-                const u32x4_t x = *reinterpret_cast<const u32x4_t *>(kb + tb * 32 * TL::ROWB + (((2 * s + half) ^ sw) << 4));
-                if constexpr (CACHE == 4) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        st[tb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(q[s][e]), st[tb], 0, 0, 0);
-                } else {
-                    st[tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, q[s]), st[tb], 0, 0, 0);
-                }
+                for (int e = 0; e < 4; ++e)
+                    st = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(q[s][e]), st, 0, 0, 0);
+            } else {
+                st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, q[s]), st, 0, 0, 0);
             }
         }
     };
-    // scores of tokens t0 .. to weights, the maximum, sum and outputs so far to the new maximum;
-    // ks, vs: 8-bit pages' scales
-    auto weigh = [&](auto &st, int t0, const float *ks, const float *vs) {
-        constexpr int TB = sizeof(st) / sizeof(f32x16_t);
+    // scores of tokens t0 .. as far as the row sees them (8-bit: in units of log2, with the pages' scales ks);
+    // the maximum, sum and outputs so far follow
+    auto settle_scores = [&](f32x16_t &st, int t0, const float *ks, bool border) __attribute__((always_inline)) {
         if constexpr (CACHE == 1) {
 #pragma unroll
-            for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) st[tb][i] *= __builtin_amdgcn_fmed3f(a.qscale * ks[2 * tb + i / 8], FLT_TRUE_MIN, FLT_MAX);
+            for (int i = 0; i < 16; ++i) st[i] *= __builtin_amdgcn_fmed3f(a.qscale * ks[i / 8], FLT_TRUE_MIN, FLT_MAX);
         }
-        if (t0 + 32 * TB > min(wave_first, last)) {
+        if (border && t0 + 32 > min(wave_first, last)) {
             const int left = sees - t0 - 4 * half;                   // tokens that the row sees, from this half's first on
 #pragma unroll
-            for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) st[tb][i] = masked(st[tb][i], tb * 32 + 8 * (i / 4) + i % 4 - left);
+            for (int i = 0; i < 16; ++i) st[i] = masked(st[i], 8 * (i / 4) + i % 4 - left);
         }
-        float top = st[0][0];
+        float top = st[0];
 #pragma unroll
-        for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, st[tb][i]);
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, st[i]);
         top = max_halves(top);
         // (a maximum may lag by 8 in log2: weights up to 2^8, relative errors as they are)
         if (__any(top * unit > m * unit + 8.0f)) {
@@ -357,258 +346,331 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
                 for (int i = 0; i < 16; ++i) o[d][i] *= f;
             m = up;
         }
+    };
+    // scores to weights, which the sum takes in (8-bit: then times the pages' value scales vs)
+    auto weigh = [&](f32x16_t &st, const float *vs) __attribute__((always_inline)) {
         const float from = m == kNegInf ? 0.0f : m * unit;           // (a row that sees nothing yet)
 #pragma unroll
-        for (int tb = 0; tb < TB; ++tb)
+        for (int i = 0; i < 16; ++i) st[i] = __builtin_amdgcn_exp2f(fmaf(st[i], unit, -from));
+        float sum[4];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                st[tb][i] = __builtin_amdgcn_exp2f(fmaf(st[tb][i], unit, -from));
-                l += st[tb][i];
-            }
+        for (int i = 0; i < 4; ++i) sum[i] = (st[i] + st[i + 4]) + (st[i + 8] + st[i + 12]);
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         if constexpr (CACHE == 1) {
 #pragma unroll
-            for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) st[tb][i] *= vs[2 * tb + i / 8];
+            for (int i = 0; i < 16; ++i) st[i] *= vs[i / 8];
         }
     };
-    // O^T += V^T P^T.  odd_values: some value of a token that not every row sees is infinite or NaN,
-    // and a weight of zero would not keep it out; then the finite values, and where there are infinite
-    // ones or NaN, are multiplied on their own
-    auto values = [&](auto &st, const unsigned char *vb, bool odd_values) {
-        constexpr int TB = sizeof(st) / sizeof(f32x16_t);
-        auto add_part = [&](int d, int part, const f32x16_t &y) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] += part == 0 ? y[i] : y[i] > 0.0f ? (part == 1 ? __builtin_huge_valf() : kNegInf) : 0.0f;
-        };
+    // O^T += V^T P^T
+    auto values = [&](const f32x16_t &st, const unsigned char *vb) __attribute__((always_inline)) {
         if constexpr (CACHE == 4) {
 #pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                auto value = [&](int tb, int i) {
-                    const int t = tb * 32 + 8 * (i / 4) + 4 * half + i % 4, u = (d * 32 + col) / 4;
-                    return *reinterpret_cast<const float *>(vb + t * TL::ROWB + ((u ^ TL::value_swizzle(t)) << 4) + (col & 3) * 4);
-                };
-                if (odd_values) {
-                    for (int part = 0; part < 3; ++part) {           // finite values; where +inf or NaN, where -inf or NaN
-                        f32x16_t y = {};
+            for (int d = 0; d < DB; ++d)
 #pragma unroll
-                        for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const float x = value(tb, i);
-                                const bool mine = x != x || x == (part == 1 ? __builtin_huge_valf() : kNegInf);
-                                const float z = part == 0 ? (fabsf(x) < __builtin_huge_valf() ? x : 0.0f) : mine ? 1.0f : 0.0f;
-                                y = __builtin_amdgcn_mfma_f32_32x32x2f32(z, st[tb][i], y, 0, 0, 0);
-                            }
-                        add_part(d, part, y);
-                    }
-                } else {
-#pragma unroll
-                    for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(tb, i), st[tb][i], o[d], 0, 0, 0);
+                for (int i = 0; i < 16; ++i) {
+                    const int t = 8 * (i / 4) + 4 * half + i % 4, u = (d * 32 + col) / 4;
+                    const float x = *reinterpret_cast<const float *>(vb + t * TL::ROWB + ((u ^ TL::value_swizzle(t)) << 4) + (col & 3) * 4);
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, st[i], o[d], 0, 0, 0);
                 }
-            }
         } else {
-            u32x4_t p[2 * TB];
-#pragma unroll
-            for (int k = 0; k < 2 * TB; ++k)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) p[k][c] = pack_bf16(st[k / 2][8 * (k % 2) + 2 * c], st[k / 2][8 * (k % 2) + 2 * c + 1]);
             // lane j of a group of 16 names four dims of token j / 4 and receives dim j of the four tokens
             const int g = (lane >> 4) & 1, tt = 4 * half + ((lane & 15) >> 2), cc = 2 * g + ((lane & 3) >> 1);
             const uint32_t v0 = (uint32_t)(tt * TL::ROWB + ((cc ^ TL::value_swizzle(tt)) << 4) + (lane & 1) * 8);
             typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
-            auto read = [&](int k, int d) {                          // values of k-step k, dims 32 d ..: V^T's operand
-                // (units 4 d of a token: the swizzle flips units of 4, which 4 d xors with)
-                const unsigned char *x = vb + (v0 ^ (uint32_t)(d << 6)) + k * 16 * TL::ROWB;
-                const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(x));
-                const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(x + 8 * TL::ROWB));
-                const u32x2_t y0 = __builtin_bit_cast(u32x2_t, lo), y1 = __builtin_bit_cast(u32x2_t, hi);
-                return u32x4_t{y0[0], y0[1], y1[0], y1[1]};
-            };
-            if (odd_values) {
 #pragma unroll
-                for (int d = 0; d < DB; ++d)
-                    for (int part = 0; part < 3; ++part) {
-                        f32x16_t y = {};
+            for (int k = 0; k < 2; ++k) {
+                u32x4_t p;
 #pragma unroll
-                        for (int k = 0; k < 2 * TB; ++k) {
-                            u32x4_t x = read(k, d);
+                for (int c = 0; c < 4; ++c) p[c] = pack_bf16(st[8 * k + 2 * c], st[8 * k + 2 * c + 1]);
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) {
-                                uint32_t z = 0;
-#pragma unroll
-                                for (int s = 0; s < 32; s += 16) {
-                                    const uint32_t e = (x[c] >> s) & 0xffff, size = e & 0x7fff;
-                                    const bool mine = size > 0x7f80 || e == (part == 1 ? 0x7f80u : 0xff80u);
-                                    z |= part == 0 ? (size < 0x7f80 ? e << s : 0u) : mine ? 0x3f80u << s : 0u;
-                                }
-                                x[c] = z;
-                            }
-                            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, p[k]), y, 0, 0, 0);
-                        }
-                        add_part(d, part, y);
-                    }
-            } else {
-#pragma unroll
-                for (int k = 0; k < 2 * TB; ++k)
-#pragma unroll
-                    for (int d = 0; d < DB; ++d)
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, read(k, d)), __builtin_bit_cast(bf16x8_t, p[k]), o[d], 0, 0, 0);
+                for (int d = 0; d < DB; ++d) {
+                    // (units 4 d of a token: the swizzle flips units of 4, which 4 d xors with)
+                    const unsigned char *x = vb + (v0 ^ (uint32_t)(d << 6)) + k * 16 * TL::ROWB;
+                    const u32x2_t y0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)x));
+                    const u32x2_t y1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(x + 8 * TL::ROWB)));
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, u32x4_t{y0[0], y0[1], y1[0], y1[1]}),
+                                                                   __builtin_bit_cast(bf16x8_t, p), o[d], 0, 0, 0);
+                }
             }
         }
     };
 
     const int32_t *table = a.page_table + (size_t)r * a.max_pages;
-    const size_t slice = (size_t)h * kPage * D * CACHE, page_bytes = (size_t)a.Hkv * kPage * D * CACHE;
-    auto page_of = [&](int page) { return scalar_load(table, min(page, last_page)); };
-    auto inside = [&](int id) { return min(max(id, 0), a.pool_pages - 1); };
-    auto widen = [](uint32_t x0, uint32_t x1, float scale) {
+    const size_t slice = (size_t)h * kPage * D * CACHE;
+    const uint32_t page_bytes = (uint32_t)a.Hkv * kPage * D * CACHE;
+    auto page_of = [&](int page) __attribute__((always_inline)) { return scalar_load(table, min(page, last_page)); };
+    auto inside = [&](int id) __attribute__((always_inline)) { return min(max(id, 0), a.pool_pages - 1); };
+    auto page_at = [&](int id) __attribute__((always_inline)) { return (uint64_t)(uint32_t)inside(id) * page_bytes; };
+    auto widen = [](uint32_t x0, uint32_t x1, float scale) __attribute__((always_inline)) {
         const bf16x2_t p0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x0, scale, false), p1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x0, scale, true);
         const bf16x2_t p2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x1, scale, false), p3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x1, scale, true);
         return u32x4_t{__builtin_bit_cast(uint32_t, p0), __builtin_bit_cast(uint32_t, p1), __builtin_bit_cast(uint32_t, p2), __builtin_bit_cast(uint32_t, p3)};
     };
-    auto odd = [](const u32x4_t &x) {                                // infinite or NaN among the elements
-        bool is = false;
+    // On the border, where some row does not see all of a block's tokens, a weight of zero would not
+    // keep an infinite value or NaN out: 16 bytes of token t of block blk in LDS become zero if the
+    // token lies behind the piece's, else its infinite values and NaN do, and the token's bit says so
+    auto clean = [&](unsigned char *to, int blk, int t, uint32_t *odd) __attribute__((always_inline)) {
+        u32x4_t x = *reinterpret_cast<u32x4_t *>(to);
+        if (blk * 32 + t >= last) {
+            x = u32x4_t{};
+        } else {
+            bool found = false;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            if (CACHE == 4) is |= (x[c] & 0x7f800000u) == 0x7f800000u;
-            else is |= (x[c] & 0x7f80u) == 0x7f80u || (x[c] & 0x7f800000u) == 0x7f800000u;
+            for (int c = 0; c < 4; ++c) {
+                if constexpr (CACHE == 4) {
+                    const bool is = (x[c] & 0x7f800000u) == 0x7f800000u;
+                    x[c] = is ? 0u : x[c];
+                    found |= is;
+                } else {
+                    const bool lo = (x[c] & 0x7f80u) == 0x7f80u, hi = (x[c] & 0x7f800000u) == 0x7f800000u;
+                    x[c] &= (lo ? 0xffff0000u : 0xffffffffu) & (hi ? 0xffffu : 0xffffffffu);
+                    found |= lo || hi;
+                }
+            }
+            if (!found) return;
+            atomicOr(odd, 1u << t);
         }
-        return is;
+        *reinterpret_cast<u32x4_t *>(to) = x;
+    };
+    // ... and the rows that see such a token take them in from the pool: the result is infinite or NaN at any weight
+    auto add_odd = [&](int blk, uint32_t odd) __attribute__((always_inline)) {
+        for (; odd; odd &= odd - 1) {
+            const int t = __builtin_ctz(odd);
+            const size_t at_token = page_at(page_of(2 * blk + t / kPage)) + slice + (size_t)(t % kPage) * D * CACHE;
+            const unsigned char *v = static_cast<const unsigned char *>(a.v) + at_token;
+            const bool seen = blk * 32 + t < sees;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int dim = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
+                    float x;
+                    if constexpr (CACHE == 4) x = reinterpret_cast<const float *>(v)[dim];
+                    else if constexpr (CACHE == 2) x = bf16_to_f32(reinterpret_cast<const uint16_t *>(v)[dim]);
+                    else x = (v[dim] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.0f;
+                    if (seen && !(fabsf(x) < __builtin_huge_valf())) o[d][i] += x;
+                }
+        }
     };
     constexpr float key_unit = 1.0f / kQ8KeyScale;                   // (see Page<E4m3>::kKeyUnit of the decode kernel)
     // 16 codes of unit c of token t, widened, to the rows at `to`
-    auto put_codes = [&](unsigned char *to, int t, int c, int swizzle, const u32x4_t &x, float scale) {
+    auto put_codes = [&](unsigned char *to, int t, int c, int swizzle, const u32x4_t &x, float scale) __attribute__((always_inline)) {
         u32x4_t *row_ = reinterpret_cast<u32x4_t *>(to + t * TL::ROWB);
         row_[(2 * c) ^ swizzle] = widen(x[0], x[1], scale);
         row_[(2 * c + 1) ^ swizzle] = widen(x[2], x[3], scale);
     };
     u32x4_t kr[QL], vr[QL];
-    static_assert(CACHE != 1 || QL >= LOADS, "registers of both kinds of tile");
 
     if (!narrow) {
-        // a tile's way from the pools to LDS: a wave takes LOADS pieces of 1024 bytes each of
-        // the keys and the values, 8-bit ones through registers, where they are widened
-        const int tile0 = from_token / TOK, tiles = (last + TOK - 1) / TOK;
-        float ks[2][TL::PAGES], vs[2][TL::PAGES];                    // 8-bit: scales, of the tile in work and the next
-        int ids[LOADS], pids[TL::PAGES];                             // pages of the next pieces; 8-bit: of the next tile
-        auto s_k = [&](int buf) { return s_mem + buf * TL::BYTES; };
-        auto s_v = [&](int buf) { return s_mem + (2 + buf) * TL::BYTES; };
-        auto request = [&](int tile) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) ids[i] = page_of(tile * TL::PAGES + (i * kThreads + wave * 64) / TL::PU);
-            if constexpr (CACHE == 1)
-#pragma unroll
-                for (int p = 0; p < TL::PAGES; ++p) pids[p] = page_of(tile * TL::PAGES + p);
+        // Blocks of keys and values have STAGES places each in LDS.  In step b the workgroup reads the
+        // keys of block b + 1 and the values of block b, so that the scores of the one and the weights of
+        // the other are independent work; on their way are later blocks, up to keys b + STAGES and
+        // values b + STAGES - 1, whose places step b - 1 was the last to read.  8-bit blocks go through
+        // registers, where they are widened, a step before they are read.
+        constexpr int ST = TL::STAGES;
+        const int b0 = from_token / 32, b1 = (last + 31) / 32, border = min(first, last);
+        // LDS offsets of the places of blocks b - 1, b and b + 1 (ST = 2: the first is the last)
+        uint32_t at_p = (ST - 1) * TL::BYTES, at_c = 0, at_n = TL::BYTES;
+        auto turn = [&]() __attribute__((always_inline)) {
+            const uint32_t x = ST == 3 ? at_p : at_c;
+            at_p = at_c;
+            at_c = at_n;
+            at_n = x;
         };
-        auto load = [&](int buf) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int part = i * kWaves + wave;
-                const size_t from = inside(ids[i]) * page_bytes + slice + (size_t)(part * 64 % TL::PU) * 16;
-                const char *kp = static_cast<const char *>(a.k) + from, *vp = static_cast<const char *>(a.v) + from;
-                if constexpr (CACHE == 1) {
-                    kr[i] = reinterpret_cast<const u32x4_t *>(kp)[lane];
-                    vr[i] = reinterpret_cast<const u32x4_t *>(vp)[lane];
-                } else {
-                    // the unit that belongs at the lane's place in LDS
-                    const int t = (part * 64 + lane) / TL::UPR, c = lane % TL::UPR;
-                    const int ku = (lane & ~(TL::UPR - 1)) + (c ^ TL::key_swizzle(t)), vu = (lane & ~(TL::UPR - 1)) + (c ^ TL::value_swizzle(t));
-                    load_lds(kp, ku * 16, lds_addr(s_k(buf) + part * 1024));
-                    load_lds(vp, vu * 16, lds_addr(s_v(buf) + part * 1024));
-                }
-            }
+        unsigned char *const s_k = s_mem, *const s_v = s_mem + ST * TL::BYTES;
+        constexpr int PIECES = TL::BYTES / 1024;                     // (CACHE != 1) of a block
+        const char *const kbase = static_cast<const char *>(a.k) + slice, *const vbase = static_cast<const char *>(a.v) + slice;
+        // keys (which: 0) or values of two pages, to the place at `to`
+        auto load = [&](int which, const int (&ids)[2], uint32_t to) __attribute__((always_inline)) {
+            const char *pool = which ? vbase : kbase;
             if constexpr (CACHE == 1) {
-#pragma unroll
-                for (int p = 0; p < TL::PAGES; ++p) {
-                    const int64_t sc = (int64_t)inside(pids[p]) * a.Hkv + h;
-                    ks[1][p] = scalar_load(a.k_scale, sc);
-                    vs[1][p] = scalar_load(a.v_scale, sc);
-                }
-            }
-        };
-        // the loaded tile stands in LDS after this and a barrier.  On the border, where some row does not
-        // see all of its tokens, values behind the piece's tokens become zero (whatever lies there),
-        // and a tile is marked that has infinite values or NaN among the others
-        auto settle = [&](int tile, int buf) {
-            const bool border = (tile + 1) * TOK > min(first, last);
-            bool found = false;
-            if constexpr (CACHE == 1) {
+                if (2 * TL::PU >= kThreads || tid < 2 * TL::PU)
+                    (which ? vr : kr)[0] = reinterpret_cast<const u32x4_t *>(pool + page_at(ids[wave * 64 / TL::PU]) + (wave * 64 % TL::PU) * 16)[lane];
+            } else {
 #pragma unroll
                 for (int i = 0; i < LOADS; ++i) {
-                    const int u = i * kThreads + tid, t = u / TL::PUR, c = u % TL::PUR;
-                    if (border && tile * TOK + t >= last) vr[i] = u32x4_t{};
-                    put_codes(s_k(buf), t, c, TL::key_swizzle(t), kr[i], key_unit);
-                    put_codes(s_v(buf), t, c, TL::value_swizzle(t), vr[i], 1.0f);
-                    if (border) found |= odd(widen(vr[i][0], vr[i][1], 1.0f)) || odd(widen(vr[i][2], vr[i][3], 1.0f));
-                }
-            } else {
-                wait_loads<0>();
-                if (border) {
-#pragma unroll
-                    for (int i = 0; i < LOADS; ++i) {
-                        const int u = (i * kWaves + wave) * 64 + lane;
-                        u32x4_t *to = reinterpret_cast<u32x4_t *>(s_v(buf)) + u;
-                        if (tile * TOK + u / TL::UPR >= last) *to = u32x4_t{};
-                        else found |= odd(*to);
-                    }
+                    const int part = i * kWaves + wave;
+                    // the unit that belongs at the lane's place in LDS
+                    const int t = (part * 64 + lane) / TL::UPR, c = lane % TL::UPR;
+                    const int u = (lane & ~(TL::UPR - 1)) + (c ^ (which ? TL::value_swizzle(t) : TL::key_swizzle(t)));
+                    const int pg = LOADS == 1 ? wave / (kWaves / 2) : i / (LOADS / 2);
+                    load_lds(pool + page_at(ids[pg]) + (part % (PIECES / 2)) * 1024, u * 16, lds_addr((which ? s_v : s_k) + part * 1024) + to);
                 }
             }
-            if (border && __any(found) && lane == 0) s_odd[buf] = tile;
         };
-        if (tid < 2) s_odd[tid] = -1;
-        if (tiles > tile0) {
-            request(tile0);
-            load(tile0 & 1);
-            request(tile0 + 1);
-        }
-        __syncthreads();
-        if (tiles > tile0) settle(tile0, tile0 & 1);
-        __syncthreads();
-        for (int tile = tile0; tile < tiles; ++tile) {
-            const int buf = tile & 1;
-            if constexpr (CACHE == 1) {
+        auto ids_of = [&](int blk, int (&ids)[2]) __attribute__((always_inline)) {
+            ids[0] = page_of(2 * blk);
+            ids[1] = page_of(2 * blk + 1);
+        };
+        auto scales_of = [&](const float *scales, const int (&ids)[2], float (&x)[2]) __attribute__((always_inline)) {
+            if constexpr (CACHE == 1)
 #pragma unroll
-                for (int p = 0; p < TL::PAGES; ++p) {
-                    ks[0][p] = ks[1][p];
-                    vs[0][p] = vs[1][p];
+                for (int p = 0; p < 2; ++p) x[p] = scalar_load(scales, (int64_t)inside(ids[p]) * a.Hkv + h);
+        };
+        // 8-bit: the loaded block to LDS
+        auto put = [&](int which, uint32_t to) __attribute__((always_inline)) {
+            if constexpr (CACHE == 1) {
+                const int t = tid / TL::PUR, c = tid % TL::PUR;
+                if (2 * TL::PU >= kThreads || tid < 2 * TL::PU) {
+                    if (which) put_codes(s_v + to, t, c, TL::value_swizzle(t), vr[0], 1.0f);
+                    else put_codes(s_k + to, t, c, TL::key_swizzle(t), kr[0], key_unit);
                 }
             }
-            if (tile + 1 < tiles) {
-                load(buf ^ 1);
-                request(tile + 2);
+        };
+        // the units of a block's values that this thread brought (see clean)
+        auto settle_values = [&](int blk, uint32_t to) __attribute__((always_inline)) {
+            if ((blk + 1) * 32 <= border) return;
+            constexpr int UNITS = CACHE == 1 ? 2 : LOADS;
+#pragma unroll
+            for (int i = 0; i < UNITS; ++i) {
+                const int u = CACHE == 1 ? (tid / TL::PUR) * TL::UPR + (((tid % TL::PUR) * 2 + i) ^ TL::value_swizzle(tid / TL::PUR)) : (i * kWaves + wave) * 64 + lane;
+                if (CACHE == 1 && tid >= 2 * TL::PU) continue;
+                clean(s_v + to + u * 16, blk, u / TL::UPR, &s_odd[blk & 3]);
             }
-            if (tile * TOK < wave_last) {
-                f32x16_t st[TOK / 32];
-                scores(st, s_k(buf));
-                weigh(st, tile * TOK, ks[0], vs[0]);
-                values(st, s_v(buf), uni(s_odd[buf]) == tile);
+        };
+        if (tid < 4) s_odd[tid] = 0;
+        int kid[2], vid[2];                                          // pages of the next keys and values to be loaded
+        float ks[2] = {}, kn[2] = {}, vs[2] = {}, vn[2] = {};        // 8-bit: scales of the keys, values in work, and the next
+        f32x16_t sa, sb;
+        if (b0 < b1) {
+            ids_of(b0, kid);
+            load(0, kid, at_c);
+            load(1, kid, at_c);
+            if constexpr (CACHE == 1) {
+                scales_of(a.k_scale, kid, ks);
+                scales_of(a.v_scale, kid, vs);
+                put(0, at_c);
+                put(1, at_c);
             }
-            if (tile + 1 < tiles) settle(tile + 1, buf ^ 1);
-            __syncthreads();
+            ids_of(b0 + 1, kid);
+            load(0, kid, at_n);
+            if constexpr (CACHE == 1) {
+                load(1, kid, at_n);
+                scales_of(a.k_scale, kid, kn);
+                scales_of(a.v_scale, kid, vn);
+                put(0, at_n);
+            } else if (ST == 3) {
+                load(1, kid, at_n);
+                ids_of(b0 + 2, kid);
+                load(0, kid, at_p);
+            }
+            if constexpr (CACHE != 1) wait_loads<0>();
         }
+        __syncthreads();
+        if (b0 < b1) settle_values(b0, at_c);
+        __syncthreads();
+        if (b0 < b1) {
+            if (b0 * 32 < wave_last) {
+                scores(sa, s_k + at_c);
+                settle_scores(sa, b0 * 32, ks, true);
+            }
+            vid[0] = kid[0], vid[1] = kid[1];                        // (the last keys loaded are the next values)
+            ids_of(b0 + (CACHE == 1 ? 2 : ST), kid);
+        }
+        __syncthreads();                                             // (the first keys' place is free)
+        // what is loaded in step b.  Page ids behind the last are the last's: the loads are the same number in every step
+        auto fetch = [&](int b) __attribute__((always_inline)) {
+            if constexpr (CACHE == 1) {
+                put(1, at_n);
+                load(0, kid, 0);
+                load(1, kid, 0);
+            } else {
+                load(0, kid, at_c);
+                load(1, vid, at_p);
+                vid[0] = kid[0], vid[1] = kid[1];
+                ids_of(b + ST + 1, kid);
+            }
+        };
+        // ... and what step b + 1 reads of it, in place
+        auto arrive = [&](int b) __attribute__((always_inline)) {
+            if constexpr (CACHE == 1) {
+                put(0, at_p);                                        // (keys b + 2 in the place of b - 1)
+                vs[0] = vn[0], vs[1] = vn[1];
+                scales_of(a.k_scale, kid, kn);
+                scales_of(a.v_scale, kid, vn);
+                ids_of(b + 3, kid);
+            } else {
+                wait_loads<ST == 3 ? 2 * LOADS : 0>();
+            }
+        };
+        // step b: `st` holds the scores of block b.  Away from the border every row sees blocks b and b + 1
+        auto inner = [&](int b, f32x16_t &st, f32x16_t &nx) __attribute__((always_inline)) {
+            fetch(b);
+            const float vc[2] = {vs[0], vs[1]};
+            scores(nx, s_k + at_n);
+            weigh(st, vc);
+            values(st, s_v + at_c);
+            settle_scores(nx, (b + 1) * 32, kn, false);
+            arrive(b);
+            turn();
+            __syncthreads();
+        };
+        auto step = [&](int b, f32x16_t &st, f32x16_t &nx) __attribute__((always_inline)) {
+            const bool next = b + 1 < b1, mine = b * 32 < wave_last, more = next && (b + 1) * 32 < wave_last;
+            const float vc[2] = {vs[0], vs[1]};
+            if (next) fetch(b);
+            // (block b + 2's mark: last read two steps ago, made in the next one)
+            if (tid == 0) s_odd[(b + 2) & 3] = 0;
+            if (mine) {
+                weigh(st, vc);
+                values(st, s_v + at_c);
+                if ((b + 1) * 32 > border) {
+                    const uint32_t odd = uni(s_odd[b & 3]);
+                    if (odd) add_odd(b, odd);
+                }
+            }
+            if (more) {
+                scores(nx, s_k + at_n);
+                settle_scores(nx, (b + 1) * 32, kn, true);
+            }
+            if (next) {
+                arrive(b);
+                settle_values(b + 1, at_n);
+            }
+            turn();
+            __syncthreads();
+        };
+        int b = b0;
+        if (row0 < rows) {
+            for (; (b + 3) * 32 <= border; b += 2) {
+                inner(b, sa, sb);
+                inner(b + 1, sb, sa);
+            }
+        } else {
+            for (; (b + 3) * 32 <= border; b += 2)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    fetch(b + k);
+                    arrive(b + k);
+                    turn();
+                    __syncthreads();
+                }
+        }
+        for (; b < b1; b += 2) {
+            step(b, sa, sb);
+            if (b + 1 < b1) step(b + 1, sb, sa);
+        }
+        if constexpr (CACHE != 1) wait_loads<0>();
         l = sum_halves(l);
     } else {
         // every wave has its own tiles of 32 tokens, NW apart, keys and values in LDS once: the next
         // keys are on their way as soon as the scores are there, the next values after the product
         unsigned char *s_k = s_mem + wave * 2 * NB, *s_v = s_k + NB;
-        const int b1 = (last + 31) / 32, step = NW;
+        const int b1 = (last + 31) / 32;
         int b = wave < NW ? from_token / 32 + wave : b1;
         int ids[2];
         float ks[2], vs[2], kn[2], vn[2];
-        auto request = [&](int blk) {
+        auto request = [&](int blk) __attribute__((always_inline)) {
             ids[0] = page_of(2 * blk);
             ids[1] = page_of(2 * blk + 1);
         };
         // keys (which: 0) or values of the requested tile
-        auto load = [&](int which) {
+        auto load = [&](int which) __attribute__((always_inline)) {
             const char *pool = static_cast<const char *>(which ? a.v : a.k);
             if constexpr (CACHE == 1) {
 #pragma unroll
                 for (int i = 0; i < QL; ++i) {
-                    const size_t from = inside(ids[i / (QL / 2)]) * page_bytes + slice + (size_t)(i % (QL / 2)) * 1024;
+                    const size_t from = page_at(ids[i / (QL / 2)]) + slice + (size_t)(i % (QL / 2)) * 1024;
                     (which ? vr : kr)[i] = reinterpret_cast<const u32x4_t *>(pool + from)[lane];
                 }
 #pragma unroll
@@ -618,7 +680,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
                 for (int i = 0; i < NL; ++i) {
                     const int t = (i * 64 + lane) / TL::UPR, c = lane % TL::UPR;
                     const int u = (lane & ~(TL::UPR - 1)) + (c ^ (which ? TL::value_swizzle(t) : TL::key_swizzle(t)));
-                    const size_t from = inside(ids[i / (NL / 2)]) * page_bytes + slice + (size_t)(i % (NL / 2)) * 1024;
+                    const size_t from = page_at(ids[i / (NL / 2)]) + slice + (size_t)(i % (NL / 2)) * 1024;
                     load_lds(pool + from, u * 16, lds_addr((which ? s_v : s_k) + i * 1024));
                 }
             }
@@ -628,9 +690,9 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
             load(0);
             load(1);
         }
-        for (; b < b1; b += step) {
-            const bool more = b + step < b1;
-            if (more) request(b + step);
+        for (; b < b1; b += NW) {
+            const bool more = b + NW < b1;
+            if (more) request(b + NW);
             if constexpr (CACHE == 1) {
 #pragma unroll
                 for (int p = 0; p < 2; ++p) {
@@ -645,33 +707,31 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
             } else {
                 wait_loads<NL>();                                    // (the values, behind the keys, may be under way)
             }
-            f32x16_t st[1];
+            f32x16_t st;
             scores(st, s_k);
             wait_lds();                                              // the keys are read
             if (more) load(0);
-            weigh(st, b * 32, ks, vs);
+            settle_scores(st, b * 32, ks, true);
+            weigh(st, vs);
             const bool border = (b + 1) * 32 > min(first, last);
-            bool found = false;
+            if (border && lane == 0) s_odd[wave] = 0;
             if constexpr (CACHE == 1) {
 #pragma unroll
                 for (int i = 0; i < QL; ++i) {
                     const int t = (i * 64 + lane) / TL::PUR, c = lane % TL::PUR;
-                    if (border && b * 32 + t >= last) vr[i] = u32x4_t{};
                     put_codes(s_v, t, c, TL::value_swizzle(t), vr[i], 1.0f);
-                    if (border) found |= odd(widen(vr[i][0], vr[i][1], 1.0f)) || odd(widen(vr[i][2], vr[i][3], 1.0f));
                 }
             } else {
                 if (more) wait_loads<NL>();
                 else wait_loads<0>();
-                if (border) {
-                    for (int i = 0; i < NL; ++i) {
-                        u32x4_t *to = reinterpret_cast<u32x4_t *>(s_v + i * 1024) + lane;
-                        if (b * 32 + (i * 64 + lane) / TL::UPR >= last) *to = u32x4_t{};
-                        else found |= odd(*to);
-                    }
-                }
             }
-            values(st, s_v, border && __any(found));
+            if (border)
+                for (int i = 0; i < NL; ++i) clean(s_v + i * 1024 + lane * 16, b, (i * 64 + lane) / TL::UPR, &s_odd[wave]);
+            values(st, s_v);
+            if (border) {
+                const uint32_t odd = uni(s_odd[wave]);
+                if (odd) add_odd(b, odd);
+            }
             wait_lds();
             if (more) load(1);
         }
@@ -680,7 +740,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
         __syncthreads();
         __shared__ float s_ml[2][NW][32];
         float *s_o = reinterpret_cast<float *>(s_mem);
-        auto unit_of = [&](int rr, int u) { return rr * (D / 4) + (u ^ (rr & 15)); };
+        auto unit_of = [&](int rr, int u) __attribute__((always_inline)) { return rr * (D / 4) + (u ^ (rr & 15)); };
         if (wave < NW) {
 #pragma unroll
             for (int d = 0; d < DB; ++d)
