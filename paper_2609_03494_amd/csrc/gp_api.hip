@@ -528,6 +528,7 @@ gp_status_t prompt_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, cons
     if (w.items * kv->num_kv_heads >= int64_t(1) << 23) return GP_ERR_UNSUPPORTED;     // (a grid below 2^32 threads)
     if (ws_bytes < w.total) return GP_ERR_WORKSPACE;
     unsigned char *base = static_cast<unsigned char *>(ws);
+    a.direct = ps->num_reqs <= 64 && (!tok_start || num_tokens <= a.tokens);
     a.slots = w.slots;
     a.max_pieces = w.max_pieces;
     a.max_merges = w.max_merges;

@@ -375,6 +375,7 @@ struct PromptArgs {
     int64_t q_stride;                 // elements from token to token
     int R, T, Hkv, G, lg, max_pages, pool_pages, advanced;   // lg: log2 G
     int tokens;                       // new tokens of an item
+    bool direct;                      // one item per request, no more than 64: without a list of pieces
     int slots;                        // pieces that the batch is divided into where items alone are fewer, about
     int max_pieces, max_merges, part_rows;   // pieces and split items of one KV head at most; rows of a partial
     float qscale;                     // scale * log2(e); 8-bit: times kQ8KeyScale

@@ -141,97 +141,121 @@ __device__ inline Asked asked(const PromptArgs &a, int r) {
 // steps; their order within a step is whoever came first and has no bearing on any result.
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kBuckets = 256;
 
-struct Item { int r, j0, seen, parts, per; };          // per: tokens of a piece
-__device__ inline Item item_of(const PromptArgs &a, int r, const Asked &q, int i, int share) {
-    Item x;
-    x.r = r;
-    x.j0 = i * a.tokens;
-    const int n = min(a.tokens, q.n - x.j0);
-    x.seen = max(q.before + x.j0 + n, 0);
-    const int least = (n << a.lg) <= 32 ? kPromptLeastNarrow : kPromptLeastWide;
-    const int piece = max(share, least);
-    x.parts = x.seen > piece + piece / 4 ? (x.seen + piece - 1) / piece : 1;
-    x.per = ((x.seen + x.parts - 1) / x.parts + 63) / 64 * 64;
-    x.parts = max((x.seen + x.per - 1) / max(x.per, 1), 1);
+// An item's pieces: `per` tokens each (a multiple of 64), the last one less.  Quotients by
+// reciprocals, put right where they have to be exact: integer divisions were most of this
+// kernel's time.
+struct Split { int parts, per; };
+__device__ inline Split split_of(int seen, int rows, int share) {
+    const int piece = max(share, rows <= 32 ? kPromptLeastNarrow : kPromptLeastWide);
+    Split x = {1, seen};
+    if (seen <= piece + piece / 4) return x;
+    const int parts = (int)((float)seen / (float)piece) + 1;             // at most 1.8 seen / piece
+    x.per = ((int)((float)seen / (float)parts) + 64) & ~63;              // at least seen / parts
+    x.parts = (int)((float)seen / (float)x.per);
+    while (x.parts * x.per < seen) ++x.parts;
+    while (x.parts > 1 && (x.parts - 1) * x.per >= seen) --x.parts;
     return x;
+}
+__device__ inline int share_of(unsigned long long cost, int slots) {
+    const unsigned long long x = (cost + slots - 1) / slots;
+    return x < INT_MAX / 2 ? (int)x : INT_MAX / 2;
 }
 
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PromptArgs a) {
+    constexpr int kFew = 4;                           // a thread takes requests of up to so many items, a wave the others
     __shared__ Asked s_asked[kPlanThreads];
+    __shared__ int s_many[kPlanThreads];
     __shared__ unsigned long long s_cost, s_tokens;
-    __shared__ int s_most, s_slots, s_merges, s_hist[kBuckets], s_wave[kBuckets / 64];
+    __shared__ int s_most, s_items, s_slots, s_merges, s_nmany, s_hist[kBuckets], s_wave[kBuckets / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
     if (tid < kBuckets) s_hist[tid] = 0;
     if (tid == 0) {
         s_cost = s_tokens = 0;
-        s_most = s_slots = s_merges = 0;
+        s_most = s_items = s_slots = s_merges = s_nmany = 0;
     }
     __syncthreads();
-    // the sum of costs, the largest, and all tokens
-    unsigned long long sum = 0, all = 0;
-    int most = 0;
-    for (int r = tid; r < a.R; r += kPlanThreads) {
-        const Asked q = asked(a, r);
-        if (r < kPlanThreads) s_asked[r] = q;
-        if (!q.in || q.n == 0) continue;
-        const unsigned long long n = q.n, items = (n + a.tokens - 1) / a.tokens;
-        sum += items * max(q.before, 0) + items * (items - 1) / 2 * a.tokens + n;
-        all += n;
-        most = max(most, q.before + q.n);
-    }
+    // the sum of costs, the largest, all items and tokens
+    {
+        unsigned long long sum = 0, all = 0;
+        int most = 0, items_ = 0;
+        for (int r = tid; r < a.R; r += kPlanThreads) {
+            const Asked q = asked(a, r);
+            if (r < kPlanThreads) s_asked[r] = q;
+            if (!q.in || q.n == 0) continue;
+            const int items = (q.n + a.tokens - 1) / a.tokens;
+            sum += (unsigned long long)items * max(q.before, 0) + (unsigned long long)items * (items - 1) / 2 * a.tokens + q.n;
+            all += q.n;
+            items_ += items;
+            most = max(most, q.before + q.n);
+        }
 #pragma unroll
-    for (int o = 32; o > 0; o /= 2) {
-        sum += __shfl_xor(sum, o, 64);
-        all += __shfl_xor(all, o, 64);
-        most = max(most, __shfl_xor(most, o, 64));
-    }
-    if (lane == 0) {
-        atomicAdd(&s_cost, sum);
-        atomicAdd(&s_tokens, all);
-        atomicMax(&s_most, most);
+        for (int o = 32; o > 0; o /= 2) {
+            sum += __shfl_xor(sum, o, 64);
+            all += __shfl_xor(all, o, 64);
+            items_ += __shfl_xor(items_, o, 64);
+            most = max(most, __shfl_xor(most, o, 64));
+        }
+        if (lane == 0 && all) {
+            atomicAdd(&s_cost, sum);
+            atomicAdd(&s_tokens, all);
+            atomicAdd(&s_items, items_);
+            atomicMax(&s_most, most);
+        }
     }
     __syncthreads();
     if (s_tokens > (unsigned long long)a.T) {         // (starts that decrease: more than the workspace is made for)
         if (tid < 2) a.counts[tid] = 0;
         return;
     }
-    const int share = (int)((s_cost + a.slots - 1) / a.slots < INT_MAX / 2 ? (s_cost + a.slots - 1) / a.slots : INT_MAX / 2);
-    // pass 1: pieces per bucket; 2: pieces to their places
-    for (int pass = 1; pass < 3; ++pass) {
+    const int share = share_of(s_cost, a.slots);
+    const float scale = (float)(kBuckets - 1) / (float)max(s_most, 1);
+    // pass 1: pieces per bucket; 2: pieces to their places.  Few items all start at once: any order
+    const bool sorted = s_items > a.slots / 2;
+    for (int pass = sorted ? 1 : 2; pass < 3; ++pass) {
+        auto take = [&](int r, const Asked &q, int i) {
+            const int j0 = i * a.tokens, n = min(a.tokens, q.n - j0), seen = max(q.before + j0 + n, 0);
+            const Split x = split_of(seen, n << a.lg, share);
+            const int bucket = sorted ? max(kBuckets - 1 - (int)((float)min(x.per, seen) * scale), 0) : 0;
+            if (pass == 1) {
+                atomicAdd(&s_hist[bucket], x.parts);
+                return;
+            }
+            // (the bounds hold for any batch, see PromptWs)
+            int slot = -1;
+            if (x.parts > 1) {
+                slot = atomicAdd(&s_slots, x.parts);
+                const int at = atomicAdd(&s_merges, 1);
+                if (at < a.max_merges) a.merges[at] = make_int4(r, j0, slot, x.parts);
+            }
+            int at = atomicAdd(&s_hist[bucket], x.parts);
+            for (int p = 0; p < x.parts; ++p, ++at) {
+                if (at >= a.max_pieces) break;
+                a.pieces[2 * at] = make_int4(r, j0, p * x.per, min((p + 1) * x.per, seen));
+                a.pieces[2 * at + 1].x = slot < 0 ? -1 : slot + p;
+            }
+        };
         for (int r0 = 0; r0 < a.R; r0 += kPlanThreads) {
-            if (a.R > kPlanThreads) {
-                __syncthreads();
-                if (r0 + tid < a.R) s_asked[tid] = asked(a, r0 + tid);
-                __syncthreads();
+            const int r = r0 + tid;
+            Asked q = {};
+            if (r < a.R) q = r0 == 0 ? s_asked[tid] : asked(a, r);
+            const int items = q.in ? (q.n + a.tokens - 1) / a.tokens : 0;
+            if (items > kFew) {
+                const int at = atomicAdd(&s_nmany, 1);
+                s_many[at] = r;
+            } else {
+                for (int i = 0; i < items; ++i) take(r, q, i);
             }
-            for (int k = wave; k < kPlanThreads && r0 + k < a.R; k += kPlanWaves) {
-                const Asked q = s_asked[k];
-                if (!q.in) continue;
-                const int items = (q.n + a.tokens - 1) / a.tokens;
-                for (int i = lane; i < items; i += 64) {
-                    const Item x = item_of(a, r0 + k, q, i, share);
-                    const int cost = min(x.per, x.seen), bucket = kBuckets - 1 - (int)((int64_t)cost * (kBuckets - 1) / max(s_most, 1));
-                    if (pass == 1) {
-                        atomicAdd(&s_hist[bucket], x.parts);
-                        continue;
-                    }
-                    // (the bounds hold for any batch, see PromptWs)
-                    int slot = -1;
-                    if (x.parts > 1) {
-                        slot = atomicAdd(&s_slots, x.parts);
-                        const int at = atomicAdd(&s_merges, 1);
-                        if (at < a.max_merges) a.merges[at] = make_int4(x.r, x.j0, slot, x.parts);
-                    }
-                    int at = atomicAdd(&s_hist[bucket], x.parts);
-                    for (int p = 0; p < x.parts; ++p, ++at) {
-                        if (at >= a.max_pieces) break;
-                        a.pieces[2 * at] = make_int4(x.r, x.j0, p * x.per, min((p + 1) * x.per, x.seen));
-                        a.pieces[2 * at + 1].x = slot < 0 ? -1 : slot + p;
-                    }
-                }
+            __syncthreads();
+            for (int k = wave; k < s_nmany; k += kPlanWaves) {
+                const int rr = uni(s_many[k]);
+                const Asked big = r0 == 0 ? s_asked[rr] : asked(a, rr);
+                const int count = (big.n + a.tokens - 1) / a.tokens;
+                for (int i = lane; i < count; i += 64) take(rr, big, i);
             }
+            __syncthreads();
+            if (tid == 0) s_nmany = 0;
+            __syncthreads();
         }
-        __syncthreads();
         if (pass == 1) {
             // first place of each bucket
             int n = 0, x = 0;
@@ -248,12 +272,55 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PromptArgs a) {
             if (tid < kBuckets) {
                 for (int w = 0; w < wave; ++w) x += s_wave[w];
                 s_hist[tid] = x - n;
-                if (tid == kBuckets - 1) a.counts[0] = min(x, a.max_pieces);
             }
             __syncthreads();
         }
     }
-    if (tid == 0) a.counts[1] = min(s_merges, a.max_merges);
+    if (tid == 0) {
+        a.counts[0] = min(s_hist[sorted ? kBuckets - 1 : 0], a.max_pieces);   // (where the last bucket's last piece ended)
+        a.counts[1] = min(s_merges, a.max_merges);
+    }
+}
+
+// A call of up to 64 requests of one item each needs no list: every workgroup finds its piece,
+// and every merging one its item, by a scan over the requests, a lane each.
+// piece: piece `index` (merge: split item `index`); r < 0: none.
+struct Place { int r, j0, from, to, slot, parts; };
+__device__ inline int wave_sums(int x, int lane) {
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int y = __shfl_up(x, o, 64);
+        if (lane >= o) x += y;
+    }
+    return x;
+}
+__device__ inline Place direct_place(const PromptArgs &a, int index, bool merge, int lane) {
+    Asked q = {};
+    if (lane < a.R) q = asked(a, lane);
+    const bool in = q.in && q.n > 0;
+    const int seen = in ? max(q.before + q.n, 0) : 0;
+    // (starts that decrease can ask for more than T tokens: none is served)
+    const int all = __shfl(wave_sums(in ? q.n : 0, lane), 63, 64), cost = __shfl(wave_sums(seen, lane), 63, 64);
+    const Split x = split_of(seen, (in ? q.n : 0) << a.lg, share_of(cost, a.slots));
+    const int parts = in ? x.parts : 0, split = parts > 1 ? parts : 0;
+    const int slot_end = wave_sums(split, lane), end = merge ? wave_sums(split ? 1 : 0, lane) : wave_sums(parts, lane);
+    const int begin = end - (merge ? (split ? 1 : 0) : parts);
+    const uint64_t who = __ballot(index >= begin && index < end);
+    Place p = {-1, 0, 0, 0, -1, 0};
+    if (!who || all > a.T) return p;
+    const int r = __builtin_ctzll(who);
+    p.r = r;
+    p.parts = uni(__shfl(parts, r, 64));
+    const int slot0 = uni(__shfl(slot_end, r, 64)) - p.parts;
+    if (merge) {
+        p.slot = slot0;
+        return p;
+    }
+    const int part = index - uni(__shfl(begin, r, 64)), per = uni(__shfl(x.per, r, 64));
+    p.from = part * per;
+    p.to = min(p.from + per, uni(__shfl(seen, r, 64)));
+    p.slot = p.parts > 1 ? slot0 + part : -1;
+    return p;
 }
 
 // ---------------------------------------------------------------- products --
@@ -272,10 +339,16 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
     static_assert(NW * 32 * D * 4 <= TL::MEM, "the waves' parts meet in LDS");
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
     const int h = blockIdx.x % a.Hkv, at_piece = blockIdx.x / a.Hkv;
-    if (at_piece >= scalar_load(a.counts, 0)) return;
-    const int32_t *piece = reinterpret_cast<const int32_t *>(a.pieces + 2 * (size_t)at_piece);
-    const int r = scalar_load(piece, 0), j0 = scalar_load(piece, 1), from_token = scalar_load(piece, 2), to_token = scalar_load(piece, 3);
-    const int slot = scalar_load(piece, 4);
+    Place piece;
+    if (a.direct) {
+        piece = direct_place(a, at_piece, false, lane);
+        if (piece.r < 0) return;
+    } else {
+        if (at_piece >= scalar_load(a.counts, 0)) return;
+        const int32_t *x = reinterpret_cast<const int32_t *>(a.pieces + 2 * (size_t)at_piece);
+        piece = {scalar_load(x, 0), scalar_load(x, 1), scalar_load(x, 2), scalar_load(x, 3), scalar_load(x, 4), 0};
+    }
+    const int r = uni(piece.r), j0 = uni(piece.j0), from_token = uni(piece.from), to_token = uni(piece.to), slot = uni(piece.slot);
     const Asked rq = asked(a, r);
     const int rows = min(a.tokens, rq.n - j0) << a.lg;               // of this item
     const int first = rq.before + j0 + 1, last = to_token;           // tokens that its first row sees, the end of the piece
@@ -824,8 +897,15 @@ template <typename E, int D>
 __global__ __launch_bounds__(256) void merge_kernel(PromptArgs a) {
     constexpr int LANES = D / 4, ROWS = 256 / LANES;
     const int h = blockIdx.x % a.Hkv, at = blockIdx.x / a.Hkv;
-    if (at >= scalar_load(a.counts, 1)) return;
-    const int4 x = a.merges[at];
+    int4 x;
+    if (a.direct) {
+        const Place p = direct_place(a, at, true, threadIdx.x & 63);
+        if (p.r < 0) return;
+        x = make_int4(p.r, 0, p.slot, p.parts);
+    } else {
+        if (at >= scalar_load(a.counts, 1)) return;
+        x = a.merges[at];
+    }
     const Asked rq = asked(a, x.x);
     const int rows = min(a.tokens, rq.n - x.y) << a.lg;
     const int u = threadIdx.x % LANES;
@@ -860,7 +940,7 @@ __global__ __launch_bounds__(256) void merge_kernel(PromptArgs a) {
 
 template <int CACHE, int D>
 void launch_cd(const PromptArgs &a, hipStream_t s) {
-    plan_kernel<<<1, kPlanThreads, 0, s>>>(a);
+    if (!a.direct) plan_kernel<<<1, kPlanThreads, 0, s>>>(a);
     prompt_kernel<CACHE, D><<<a.max_pieces * a.Hkv, kThreads, 0, s>>>(a);
     using E = typename std::conditional<CACHE == 4, float, uint16_t>::type;
     if (a.max_merges) merge_kernel<E, D><<<dim3(a.max_merges * a.Hkv, a.part_rows / 32), 256, 0, s>>>(a);
