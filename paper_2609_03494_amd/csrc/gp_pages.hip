@@ -39,12 +39,26 @@ __device__ inline int block_sums(int x, int *s_wave, int *total) {
     return before + x;
 }
 
+// Which of n ascending ends is the first behind x (the last is).
+__device__ inline int first_behind(const int *s_end, int n, int x) {
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (s_end[mid] > x) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo;
+}
+
+// Pages in flight per thread, of whatever requests they are.
+constexpr int kBatch = 8;
+
 // ---------------------------------------------------------------- reserve --
 
 __global__ __launch_bounds__(kThreads) void reserve_kernel(PagesArgs a) {
     __shared__ int s_wave[kWaves];
-    __shared__ int s_first[kThreads], s_need[kThreads], s_held[kThreads];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ int s_end[kThreads], s_held[kThreads];  // pages granted up to a request; pages that it had
+    const int tid = threadIdx.x;
     const int height = min(max(*a.free_count, 0), a.pool_pages);
     int64_t asked = 0;                                // pages asked for by the requests so far
     int taken = 0;
@@ -59,24 +73,26 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(PagesArgs a) {
             fits = m >= 0 && P >= 0 && P <= a.max_pages && want <= a.max_pages;
             need = fits ? max((int)want - P, 0) : 0;
         }
-        int all;
+        int all, got;
         const int upto = block_sums(need, s_wave, &all);
         const bool ok = fits && (need == 0 || asked + upto <= height - a.keep_free);
         if (r < a.R) a.flags[r] = ok;
-        s_first[tid] = (int)asked + upto - need;      // (read only where it is below the height)
-        s_need[tid] = ok ? need : 0;
+        // (requests are served until one cannot be: what is granted is asked for without a gap)
+        s_end[tid] = block_sums(ok ? need : 0, s_wave, &got);
         s_held[tid] = P;
         if (ok && need) a.num_pages[r] = P + need;
-        int got;
-        block_sums(ok ? need : 0, s_wave, &got);
         __syncthreads();
-        for (int i = wave; i < kThreads && r0 + i < a.R; i += kWaves) {
-            const int n = s_need[i];
-            int32_t *row = a.page_table + (size_t)(r0 + i) * a.max_pages + s_held[i];
-            for (int j = lane; j < n; j += 64) {
-                const int page = a.free_list[height - 1 - s_first[i] - j];
-                row[j] = page;
-                if (page >= 0 && page < a.pool_pages) a.refcount[page] = 1;
+        for (int x0 = tid; x0 < got; x0 += kThreads * kBatch) {
+            int page[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) page[k] = a.free_list[height - 1 - taken - min(x0 + k * kThreads, got - 1)];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int x = x0 + k * kThreads;
+                if (x >= got) break;
+                const int i = first_behind(s_end, kThreads, x);
+                a.page_table[(size_t)(r0 + i) * a.max_pages + s_held[i] + x - (i ? s_end[i - 1] : 0)] = page[k];
+                if (page[k] >= 0 && page[k] < a.pool_pages) a.refcount[page[k]] = 1;
             }
         }
         __syncthreads();
@@ -90,18 +106,44 @@ __global__ __launch_bounds__(kThreads) void reserve_kernel(PagesArgs a) {
 
 constexpr int kReleaseList = 2048;                    // requests whose pages are walked at a time
 constexpr int kBitWords = 32768;                      // pages of pools up to 2^20 are marked in LDS
-constexpr int kBatch = 4;                             // pages in flight per thread
 
-// MARKS: larger pools: a page whose last reference goes is marked by a count of -1.
+// The pages marked in s_bits onto the stack from `height` on, in ascending order: their number.
+// A wave has a run of words, a lane one of 64 at a time, so that a wave's ids go to a few
+// lines of the stack; a barrier between stores would wait for them (16 us for 6000 pages).
+__device__ inline int push_marked(const PagesArgs &a, const uint32_t *s_bits, int *s_wave, int height) {
+    const int words = cdiv(a.pool_pages, 32), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int per = cdiv(cdiv(words, kWaves), 64) * 64, w0 = min(wave * per, words), w1 = min(w0 + per, words);
+    int mine = 0;
+    for (int w = w0 + lane; w < w1; w += 64) mine += __popc(s_bits[w]);
+    int pushed;
+    int at = block_sums(mine, s_wave, &pushed);
+    at = height + __shfl(at - mine, 0, 64);           // the wave's first place
+    for (int w = w0; w < w1; w += 64) {
+        uint32_t u = w + lane < w1 ? s_bits[w + lane] : 0;
+        const int n = __popc(u);
+        int upto = n;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int y = __shfl_up(upto, o, 64);
+            if (lane >= o) upto += y;
+        }
+        int to = at + upto - n;
+        for (; u; u &= u - 1, ++to)
+            if (to < a.pool_pages) a.free_list[to] = 32 * (w + lane) + __ffs(u) - 1;
+        at += __shfl(upto, 63, 64);
+    }
+    return pushed;
+}
+
+// All in one launch.  MARKS: larger pools: a page whose last reference goes is marked by a count of -1.
 template <bool MARKS>
 __global__ __launch_bounds__(kThreads) void release_kernel(PagesArgs a) {
     __shared__ int s_wave[kWaves];
     __shared__ int s_req[kReleaseList], s_end[kReleaseList];
     __shared__ uint32_t s_bits[MARKS ? 1 : kBitWords];
     const int tid = threadIdx.x;
-    const int words = cdiv(a.pool_pages, 32);
     if (!MARKS)
-        for (int i = tid; i < words; i += kThreads) s_bits[i] = 0;
+        for (int i = tid; i < cdiv(a.pool_pages, 32); i += kThreads) s_bits[i] = 0;
     const int height = min(max(*a.free_count, 0), a.pool_pages);
     for (int i0 = 0; i0 < a.n; i0 += kReleaseList) {
         const int n = min(a.n - i0, kReleaseList);
@@ -126,30 +168,25 @@ __global__ __launch_bounds__(kThreads) void release_kernel(PagesArgs a) {
             sum += all;
         }
         __syncthreads();
-        for (int x0 = tid; x0 < sum; x0 += kThreads * kBatch) {
+        for (int base = 0; base < sum; base += kThreads * kBatch) {
             int page[kBatch], old[kBatch];
+            // (base + k * kThreads < sum: none of the threads has the page otherwise)
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
-                const int x = x0 + k * kThreads;
                 page[k] = -1;
-                if (x < sum) {
-                    int lo = 0, hi = n - 1;           // the first request whose pages end behind x
-                    while (lo < hi) {
-                        const int mid = (lo + hi) / 2;
-                        if (s_end[mid] > x) hi = mid;
-                        else lo = mid + 1;
-                    }
-                    page[k] = a.page_table[(size_t)s_req[lo] * a.max_pages + (x - (lo ? s_end[lo - 1] : 0))];
-                }
+                if (base + k * kThreads >= sum) continue;
+                const int x = base + k * kThreads + tid, i = first_behind(s_end, n, x);
+                if (x < sum) page[k] = a.page_table[(size_t)s_req[i] * a.max_pages + (x - (i ? s_end[i - 1] : 0))];
             }
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
+                if (base + k * kThreads >= sum) continue;
                 old[k] = 0;
                 if (page[k] >= 0 && page[k] < a.pool_pages) old[k] = atomicSub(&a.refcount[page[k]], 1);
             }
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
-                if (old[k] != 1) continue;
+                if (base + k * kThreads >= sum || old[k] != 1) continue;
                 if (MARKS) atomicExch(&a.refcount[page[k]], -1);
                 else atomicOr(&s_bits[page[k] >> 5], 1u << (page[k] & 31));
             }
@@ -158,29 +195,112 @@ __global__ __launch_bounds__(kThreads) void release_kernel(PagesArgs a) {
     }
     int pushed = 0;
     if (MARKS) {
-        for (int p0 = 0; p0 < a.pool_pages; p0 += kThreads) {
-            const int p = p0 + tid;
-            const bool mine = p < a.pool_pages && a.refcount[p] == -1;
+        for (int p0 = 0; p0 < a.pool_pages; p0 += kThreads * kBatch) {
+            int count[kBatch], mine = 0;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) count[k] = a.refcount[min(p0 + tid * kBatch + k, a.pool_pages - 1)];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) mine += p0 + tid * kBatch + k < a.pool_pages && count[k] == -1;
             int all;
-            const int upto = block_sums(mine, s_wave, &all);
-            if (mine) {
+            int at = height + pushed + block_sums(mine, s_wave, &all) - mine;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int p = p0 + tid * kBatch + k;
+                if (p >= a.pool_pages || count[k] != -1) continue;
                 a.refcount[p] = 0;
-                const int at = height + pushed + upto - 1;
                 if (at < a.pool_pages) a.free_list[at] = p;
+                ++at;
             }
             pushed += all;
         }
     } else {
-        const int per = cdiv(words, kThreads), w0 = min(tid * per, words), w1 = min(w0 + per, words);
-        int mine = 0;
-        for (int w = w0; w < w1; ++w) mine += __popc(s_bits[w]);
-        const int upto = block_sums(mine, s_wave, &pushed);
-        int at = height + upto - mine;
-        for (int w = w0; w < w1; ++w)
-            for (uint32_t u = s_bits[w]; u; u &= u - 1, ++at)
-                if (at < a.pool_pages) a.free_list[at] = 32 * w + __ffs(u) - 1;
+        pushed = push_marked(a, s_bits, s_wave, height);
     }
     if (tid == 0 && pushed) *a.free_count = min(height + pushed, a.pool_pages);
+}
+
+// Many pages in two launches: one workgroup's references to scattered counts take 2-3 ns each.  First a workgroup per request, which
+// puts the pages that go onto the stack in any order and leaves -2 - (their number) as the
+// request's page count; whoever takes the count away first works, so a request listed
+// twice counts once.
+constexpr int kRowThreads = 256, kOneReleaseLaunch = 32768;
+__global__ __launch_bounds__(kRowThreads) void release_rows_kernel(PagesArgs a) {
+    __shared__ int s_pages, s_freed;
+    const int tid = threadIdx.x, r = a.reqs[blockIdx.x];
+    if (r < 0 || r >= a.R || a.seq_lens[r] < 0) return;
+    if (tid == 0) {
+        const int P = a.num_pages[r];
+        s_pages = P > 0 && atomicCAS(&a.num_pages[r], P, -1) == P ? min(P, a.max_pages) : 0;
+        s_freed = 0;
+    }
+    __syncthreads();
+    const int P = s_pages;
+    if (P == 0) return;
+    for (int base = 0; base < P; base += kRowThreads * kBatch) {
+        int page[kBatch], old[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int j = base + k * kRowThreads + tid;
+            page[k] = j < P ? a.page_table[(size_t)r * a.max_pages + j] : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            old[k] = 0;
+            if (page[k] >= 0 && page[k] < a.pool_pages) old[k] = atomicSub(&a.refcount[page[k]], 1);
+        }
+        int mine = 0;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) mine += old[k] == 1;
+        // places for the wave's pages, and in them for the lane's
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int y = __shfl_up(upto, o, 64);
+            if ((tid & 63) >= o) upto += y;
+        }
+        int at = 0;
+        if ((tid & 63) == 63 && upto) {
+            at = atomicAdd(a.free_count, upto);
+            atomicAdd(&s_freed, upto);
+        }
+        at = __shfl(at, 63, 64) + upto - mine;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            if (old[k] != 1) continue;
+            if (at >= 0 && at < a.pool_pages) a.free_list[at] = page[k];
+            ++at;
+        }
+    }
+    __syncthreads();
+    if (tid == 0) a.num_pages[r] = -2 - s_freed;
+}
+
+// Then the stack's new part in order, and the rows empty.
+__global__ __launch_bounds__(kThreads) void release_order_kernel(PagesArgs a) {
+    __shared__ int s_wave[kWaves];
+    __shared__ int s_total;
+    __shared__ uint32_t s_bits[kBitWords];
+    const int tid = threadIdx.x, words = cdiv(a.pool_pages, 32);
+    for (int i = tid; i < words; i += kThreads) s_bits[i] = 0;
+    if (tid == 0) s_total = 0;
+    const int end = *a.free_count;
+    __syncthreads();
+    for (int i = tid; i < a.n; i += kThreads) {
+        const int r = a.reqs[i];
+        if (r < 0 || r >= a.R || a.seq_lens[r] < 0) continue;
+        const int x = atomicExch(&a.num_pages[r], 0);
+        if (x <= -2) atomicAdd(&s_total, -2 - x);
+        a.seq_lens[r] = 0;
+    }
+    __syncthreads();
+    const int top = min(end, a.pool_pages), height = max(end - s_total, 0);
+    for (int j = height + tid; j < top; j += kThreads) {
+        const int page = a.free_list[j];
+        if (page >= 0 && page < a.pool_pages) atomicOr(&s_bits[page >> 5], 1u << (page & 31));
+    }
+    __syncthreads();
+    push_marked(a, s_bits, s_wave, height);
+    if (tid == 0 && end > top) *a.free_count = top;
 }
 
 // ------------------------------------------------------------------- fork --
@@ -308,7 +428,12 @@ hipError_t launch_reserve(const PagesArgs &a, hipStream_t s) {
 }
 
 hipError_t launch_pages_release(const PagesArgs &a, hipStream_t s) {
-    if (a.pool_pages <= 32 * kBitWords) release_kernel<false><<<1, kThreads, 0, s>>>(a);
+    // (the table's width is all that is known of the rows' pages: 32 rows of up to 1026, 6200 in all, take 19.6
+    // us in one launch, 5.2 and 12.7 in two; fewer less in one, more in two)
+    if (a.pool_pages <= 32 * kBitWords && a.n > 1 && (int64_t)a.n * a.max_pages > kOneReleaseLaunch) {
+        release_rows_kernel<<<a.n, kRowThreads, 0, s>>>(a);
+        release_order_kernel<<<1, kThreads, 0, s>>>(a);
+    } else if (a.pool_pages <= 32 * kBitWords) release_kernel<false><<<1, kThreads, 0, s>>>(a);
     else release_kernel<true><<<1, kThreads, 0, s>>>(a);
     return hipGetLastError();
 }

@@ -195,15 +195,19 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
 
     // rows that go out in their own type, in pieces of two 16-byte units that
     // rotate into each other (side by side: each in itself): the queries, and the keys and
-    // values of such a pool.  Behind the rotated part units go out as they came, by twos.
+    // values of such a pool.  Behind the rotated part units go out as they came.
     {
         const int kv = CACHE == 1 || pid < 0 ? 0 : a.Hkv;
         const int heads = a.Hq + 2 * kv, total = rows * heads;
         constexpr int GROUPS = kThreads / UPH;        // threads of one row and head
-        const int u = tid % UPH, hu = half / EPU;
-        const bool inside = FORM == kWhole || u < hu;     // (side by side: units 2 u and 2 u + 1, of 2 hu rotated ones)
-        const int at0 = (FORM == kWhole || (FORM == kPart && inside) ? u : 2 * u) * EPU;
-        const int at1 = FORM == kWhole ? at0 + H : FORM == kPart && inside ? at0 + half : at0 + EPU;
+        // A row's threads take whole runs of it at a time in every form, units u and u + UPH each: where a
+        // part of the head turns, its partners come from the threads that hold them (pairs in one
+        // thread, hence runs of 32 and 64 bytes: half of the head of 64 / 8 heads 335 us for 1.34 GB, a quarter 518 for 1.44; now 271 and 287)
+        const int u = tid % UPH, hu = half / EPU, lane_u = lane - u;
+        const int at0 = u * EPU, at1 = at0 + H;
+        const bool in0 = u < 2 * hu, in1 = u + UPH < 2 * hu;     // (kPart, kBeside) the units turn
+        // kPart: the lanes that hold the partners of the two units, the first's in its own first or second
+        const int px = u < hu ? u + hu : u - hu, from0 = lane_u + (px & (UPH - 1)), from1 = lane_u + ((u + UPH - hu) & (UPH - 1));
         for (int x0 = tid / UPH + GROUPS * kBatch * (int)blockIdx.y; x0 < total; x0 += GROUPS * kBatch * (int)gridDim.y) {
             u32x4_t p[kBatch], q[kBatch];
             E *to[kBatch];
@@ -216,7 +220,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                 const int hh = x - row[k] * heads;
                 const int64_t t = tok + row[k];
                 const E *src;
-                turn[k] = inside;
+                turn[k] = true;
                 if (hh < a.Hq) {
                     src = reinterpret_cast<const E *>(a.q) + t * a.q_stride + (int64_t)hh * D;
                     to[k] = reinterpret_cast<E *>(a.q_out) + (t * a.Hq + hh) * D;
@@ -225,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                     const int h = hh - a.Hq - (isv ? kv : 0);
                     src = reinterpret_cast<const E *>(isv ? a.v_new : a.k_new) + t * (isv ? a.v_stride : a.k_stride) + (int64_t)h * D;
                     to[k] = reinterpret_cast<E *>(isv ? a.v : a.k) + (((size_t)pid * a.Hkv + h) * kPage + lo + row[k]) * D;
-                    turn[k] = inside && !isv;
+                    turn[k] = !isv;
                 }
                 p[k] = load16<STREAM>(src + at0);
                 q[k] = load16<STREAM>(src + at1);
@@ -237,18 +241,61 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                     float xa[EPU], xb[EPU];
                     widen(p[k], xa);
                     widen(q[k], xb);
-                    if constexpr (FORM == kBeside) {
-#pragma unroll
-                        for (int e = 0; e < EPU; e += 2) {
-                            rotate(xa[e], xa[e + 1], s_cs[row[k]][u * EPU + e / 2]);
-                            rotate(xb[e], xb[e + 1], s_cs[row[k]][u * EPU + (EPU + e) / 2]);
-                        }
-                    } else {
+                    if constexpr (FORM == kWhole) {
 #pragma unroll
                         for (int e = 0; e < EPU; ++e) rotate(xa[e], xb[e], s_cs[row[k]][u * EPU + e]);
+                        p[k] = narrow(xa);
+                        q[k] = narrow(xb);
+                    } else if constexpr (FORM == kBeside) {
+                        if (in0) {
+#pragma unroll
+                            for (int e = 0; e < EPU; e += 2) rotate(xa[e], xa[e + 1], s_cs[row[k]][(at0 + e) / 2]);
+                            p[k] = narrow(xa);
+                        }
+                        if (in1) {
+#pragma unroll
+                            for (int e = 0; e < EPU; e += 2) rotate(xb[e], xb[e + 1], s_cs[row[k]][(at1 + e) / 2]);
+                            q[k] = narrow(xb);
+                        }
+                    } else {
+                        // (all of a row's threads are here: x0 is theirs in common)
+                        const u32x4_t p0 = p[k], q0 = q[k];
+                        u32x4_t z;
+                        float zz[EPU];
+                        const bool far = 2 * hu > UPH;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) z[c] = __shfl(p0[c], from0, 64);
+                        if (far) {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) {
+                                const uint32_t y = __shfl(q0[c], from0, 64);
+                                if (px >= UPH) z[c] = y;
+                            }
+                        }
+                        widen(z, zz);
+                        if (in0) {
+#pragma unroll
+                            for (int e = 0; e < EPU; ++e) {
+                                float lo_ = u < hu ? xa[e] : zz[e], hi_ = u < hu ? zz[e] : xa[e];
+                                rotate(lo_, hi_, s_cs[row[k]][(u < hu ? u : u - hu) * EPU + e]);
+                                xa[e] = u < hu ? lo_ : hi_;
+                            }
+                            p[k] = narrow(xa);
+                        }
+                        if (far) {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) z[c] = __shfl(p0[c], from1, 64);
+                            widen(z, zz);
+                            if (in1) {                    // (a unit behind the first half: its partner is a first one)
+#pragma unroll
+                                for (int e = 0; e < EPU; ++e) {
+                                    float lo_ = zz[e];
+                                    rotate(lo_, xb[e], s_cs[row[k]][(u + UPH - hu) * EPU + e]);
+                                }
+                                q[k] = narrow(xb);
+                            }
+                        }
                     }
-                    p[k] = narrow(xa);
-                    q[k] = narrow(xb);
                 }
                 store16<STREAM>(to[k] + at0, p[k]);
                 store16<STREAM>(to[k] + at1, q[k]);
