@@ -892,10 +892,12 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
     }
 }
 
-// Parts of split items to outputs: kMergeRows rows of an item and KV head, D / 4 threads a row,
-// kMergeBatch parts in flight (one after the other 24 parts took 17 us).
-constexpr int kMergeRows = 16, kMergeBatch = 8;
-template <typename E, int D>
+// Parts of split items to outputs: ROWS rows of an item and KV head a workgroup, D / 4 threads a row,
+// BATCH parts in flight.  Few rows (calls of up to 32): many parts, so eight at a time and eight rows
+// a workgroup (5 tokens behind 6001: 25.6 us a call with one part after the other, 15.0 so).  Many:
+// few parts, and workgroups without an item cost more than theirs take (a prompt of 2048: 80.9 us
+// in that form, 72 with 32 rows and four parts).
+template <typename E, int D, int RPW, int BATCH>
 __global__ __launch_bounds__(256) void merge_kernel(PromptArgs a) {
     constexpr int LANES = D / 4, ROWS = 256 / LANES;
     const int h = blockIdx.x % a.Hkv, at = blockIdx.x / a.Hkv;
@@ -910,35 +912,38 @@ __global__ __launch_bounds__(256) void merge_kernel(PromptArgs a) {
     }
     const Asked rq = asked(a, x.x);
     const int rows = min(a.tokens, rq.n - x.y) << a.lg;
-    const int u = threadIdx.x % LANES;
-    for (int row = blockIdx.y * kMergeRows + threadIdx.x / LANES; row < min(rows, (int)(blockIdx.y + 1) * kMergeRows); row += ROWS) {
+    const int u = threadIdx.x % LANES, parts = uni(x.w);
+    for (int row = blockIdx.y * RPW + threadIdx.x / LANES; row < min(rows, (int)(blockIdx.y + 1) * RPW); row += ROWS) {
         const size_t stride = (size_t)a.Hkv * a.part_rows * (D + 2);
         const float *p = a.partial + ((size_t)x.z * a.Hkv + h) * a.part_rows * (D + 2);
         const float *ml = p + (size_t)a.part_rows * D + row;
         float m = kNegInf, l = 0.0f;
         f32x4_t o = {};
-        for (int k0 = 0; k0 < x.w; k0 += kMergeBatch) {
-            float mk[kMergeBatch], lk[kMergeBatch];
-            f32x4_t ok[kMergeBatch];
+        for (int k0 = 0; k0 < parts; k0 += BATCH) {
+            float mk[BATCH], lk[BATCH];
+            f32x4_t ok[BATCH];
 #pragma unroll
-            for (int k = 0; k < kMergeBatch; ++k) {
-                const size_t part = min(k0 + k, x.w - 1) * stride;
+            for (int k = 0; k < BATCH; ++k) {
+                mk[k] = kNegInf;
+                lk[k] = 0.0f;
+                ok[k] = f32x4_t{};
+                if (k0 + k >= parts) continue;            // (the same for all threads)
+                const size_t part = (k0 + k) * stride;
                 mk[k] = ml[part];
                 lk[k] = ml[part + a.part_rows];
                 ok[k] = *reinterpret_cast<const f32x4_t *>(p + part + (size_t)row * D + 4 * u);
             }
             float up = m;
 #pragma unroll
-            for (int k = 0; k < kMergeBatch; ++k) up = fmaxf(up, mk[k]);
+            for (int k = 0; k < BATCH; ++k) up = fmaxf(up, mk[k]);
             const float f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - up);
             l *= f;
 #pragma unroll
             for (int c = 0; c < 4; ++c) o[c] = f == 0.0f ? 0.0f : o[c] * f;
 #pragma unroll
-            for (int k = 0; k < kMergeBatch; ++k) {
-                if (k0 + k >= x.w) break;
+            for (int k = 0; k < BATCH; ++k) {
                 const float g = mk[k] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(mk[k] - up);
-                l += lk[k] * g;
+                l += lk[k] * g;                           // (a sum that is NaN stays so)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) o[c] += g == 0.0f ? 0.0f : ok[k][c] * g;
             }
@@ -962,7 +967,8 @@ void launch_cd(const PromptArgs &a, hipStream_t s) {
     if (!a.direct) plan_kernel<<<1, kPlanThreads, 0, s>>>(a);
     prompt_kernel<CACHE, D><<<a.max_pieces * a.Hkv, kThreads, 0, s>>>(a);
     using E = typename std::conditional<CACHE == 4, float, uint16_t>::type;
-    if (a.max_merges) merge_kernel<E, D><<<dim3(a.max_merges * a.Hkv, a.part_rows / kMergeRows), 256, 0, s>>>(a);
+    if (a.part_rows <= 32) merge_kernel<E, D, 8, 8><<<dim3(a.max_merges * a.Hkv, a.part_rows / 8), 256, 0, s>>>(a);
+    else merge_kernel<E, D, 32, 4><<<dim3(a.max_merges * a.Hkv, a.part_rows / 32), 256, 0, s>>>(a);
 }
 
 }  // namespace
