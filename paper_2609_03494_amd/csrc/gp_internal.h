@@ -379,6 +379,7 @@ struct PromptArgs {
     int slots;                        // pieces that the batch is divided into where items alone are fewer, about
     int max_pieces, max_merges, part_rows;   // pieces and split items of one KV head at most; rows of a partial
     float qscale;                     // scale * log2(e); 8-bit: times kQ8KeyScale
+    float lag;                        // 8 / qscale
     // workspace regions (PromptWs)
     int32_t *counts;                  // pieces, split items
     int4 *pieces;                     // [max_pieces][2]: request, first token, token range; partial slot (-1: whole)

@@ -94,7 +94,7 @@ struct Block {
     static constexpr int ROWB = D * LB, UPR = ROWB / 16;             // bytes and 16-byte units of a token
     static constexpr int BYTES = 32 * ROWB;                          // of the keys, or the values
     static constexpr int PU = D * CACHE, PUR = PU / kPage;           // 16-byte units of a page in the pool, of a token
-    static constexpr int STAGES = CACHE == 4 && D == 128 ? 2 : 3;    // blocks of keys, and of values, in LDS
+    static constexpr int STAGES = CACHE == 4 && D == 128 ? 2 : 4;    // blocks of keys, and of values, in LDS
     static constexpr int LOADS = CACHE == 1 ? 2 * PU / kThreads : BYTES / 1024 / kWaves;   // pieces of 1024 bytes of a wave
     static constexpr int NARROW = CACHE == 4 && D == 128 ? 2 : kWaves;   // waves with a block of their own, see prompt_kernel
     static constexpr int MEM = 2 * BYTES * (STAGES > NARROW ? STAGES : NARROW);
@@ -373,8 +373,12 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
     f32x16_t o[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = f32x16_t{};
-    float m = kNegInf, l = 0.0f;                                     // the row's maximum (both halves the same), this half's sum
-    const float unit = CACHE == 1 ? 1.0f : a.qscale;                 // scores to units of log2 (8-bit: in them already)
+    // The row's maximum (both halves the same) and this half's sum of weights 2^(score - from).  The
+    // maximum may lag by 8 in log2, so that outputs are rarely rescaled: relative errors are as they are.
+    // Of 8-bit caches the weights are kept below one, since they are multiplied by the values' scales.
+    const float unit = CACHE == 1 ? 1.0f : a.qscale;                 // maxima to units of log2 (8-bit: in them already)
+    const float lag = CACHE == 1 ? 8.0f : a.lag, offset = CACHE == 1 ? 8.0f : 0.0f;
+    float m = kNegInf, l = 0.0f, above = kNegInf, from = 0.0f;       // above: the score that moves the maximum
 
     // S^T of the 32 tokens whose keys lie at kb
     auto scores = [&](f32x16_t &st, const unsigned char *kb) __attribute__((always_inline)) {
@@ -393,24 +397,27 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
             }
         }
     };
-    // scores of tokens t0 .. as far as the row sees them (8-bit: in units of log2, with the pages' scales ks);
-    // the maximum, sum and outputs so far follow
-    auto settle_scores = [&](f32x16_t &st, int t0, const float *ks, bool border) __attribute__((always_inline)) {
-        if constexpr (CACHE == 1) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) st[i] *= __builtin_amdgcn_fmed3f(a.qscale * ks[i / 8], FLT_TRUE_MIN, FLT_MAX);
-        }
+    // the factors of a block's two pages of scores to units of log2 (8-bit: with the pages' key scales)
+    auto factor = [&](float ks) __attribute__((always_inline)) {
+        return CACHE == 1 ? __builtin_amdgcn_fmed3f(a.qscale * ks, FLT_TRUE_MIN, FLT_MAX) : unit;
+    };
+    // scores of tokens t0 .. as far as the row sees them; the maximum, sum and outputs so far follow
+    auto settle_scores = [&](f32x16_t &st, int t0, const float (&ks)[2], bool border) __attribute__((always_inline)) {
         if (border && t0 + 32 > min(wave_first, last)) {
             const int left = sees - t0 - 4 * half;                   // tokens that the row sees, from this half's first on
 #pragma unroll
             for (int i = 0; i < 16; ++i) st[i] = masked(st[i], 8 * (i / 4) + i % 4 - left);
         }
-        float top = st[0];
+        float t[2];
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, st[i]);
-        top = max_halves(top);
-        // (a maximum may lag by 8 in log2: weights up to 2^8, relative errors as they are)
-        if (__any(top * unit > m * unit + 8.0f)) {
+        for (int p = 0; p < 2; ++p) {
+            t[p] = st[8 * p];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) t[p] = fmaxf(t[p], st[8 * p + i]);
+            if (CACHE == 1) t[p] *= factor(ks[p]);
+        }
+        const float top = max_halves(fmaxf(t[0], t[1]));
+        if (__any(top > above)) {
             const float up = fmaxf(m, top), f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f((m - up) * unit);
             l *= f;
 #pragma unroll
@@ -418,13 +425,14 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= f;
             m = up;
+            above = up + lag;
+            from = up == kNegInf ? 0.0f : up * unit + offset;        // (a row that sees nothing yet)
         }
     };
     // scores to weights, which the sum takes in (8-bit: then times the pages' value scales vs)
-    auto weigh = [&](f32x16_t &st, const float *vs) __attribute__((always_inline)) {
-        const float from = m == kNegInf ? 0.0f : m * unit;           // (a row that sees nothing yet)
+    auto weigh = [&](f32x16_t &st, const float (&ks)[2], const float (&vs)[2]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) st[i] = __builtin_amdgcn_exp2f(fmaf(st[i], unit, -from));
+        for (int i = 0; i < 16; ++i) st[i] = __builtin_amdgcn_exp2f(fmaf(st[i], factor(ks[i / 8]), -from));
         float sum[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[i] = (st[i] + st[i + 4]) + (st[i + 8] + st[i + 12]);
@@ -535,21 +543,15 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
     u32x4_t kr[QL], vr[QL];
 
     if (!narrow) {
-        // Blocks of keys and values have STAGES places each in LDS.  In step b the workgroup reads the
+        // Blocks of keys and values have STAGES (a power of two) places each in LDS.  In step b the workgroup reads the
         // keys of block b + 1 and the values of block b, so that the scores of the one and the weights of
         // the other are independent work; on their way are later blocks, up to keys b + STAGES and
         // values b + STAGES - 1, whose places step b - 1 was the last to read.  8-bit blocks go through
         // registers, where they are widened, a step before they are read.
         constexpr int ST = TL::STAGES;
         const int b0 = from_token / 32, b1 = (last + 31) / 32, border = min(first, last);
-        // LDS offsets of the places of blocks b - 1, b and b + 1 (ST = 2: the first is the last)
-        uint32_t at_p = (ST - 1) * TL::BYTES, at_c = 0, at_n = TL::BYTES;
-        auto turn = [&]() __attribute__((always_inline)) {
-            const uint32_t x = ST == 3 ? at_p : at_c;
-            at_p = at_c;
-            at_c = at_n;
-            at_n = x;
-        };
+        // the place of block b0 + i in LDS
+        auto place = [&](int i) __attribute__((always_inline)) { return (uint32_t)(i & (ST - 1)) * TL::BYTES; };
         unsigned char *const s_k = s_mem, *const s_v = s_mem + ST * TL::BYTES;
         constexpr int PIECES = TL::BYTES / 1024;                     // (CACHE != 1) of a block
         const char *const kbase = static_cast<const char *>(a.k) + slice, *const vbase = static_cast<const char *>(a.v) + slice;
@@ -606,116 +608,121 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
         float ks[2] = {}, kn[2] = {}, vs[2] = {}, vn[2] = {};        // 8-bit: scales of the keys, values in work, and the next
         f32x16_t sa, sb;
         if (b0 < b1) {
-            ids_of(b0, kid);
-            load(0, kid, at_c);
-            load(1, kid, at_c);
             if constexpr (CACHE == 1) {
+                ids_of(b0, kid);
+                load(0, kid, 0);
+                load(1, kid, 0);
                 scales_of(a.k_scale, kid, ks);
                 scales_of(a.v_scale, kid, vs);
-                put(0, at_c);
-                put(1, at_c);
-            }
-            ids_of(b0 + 1, kid);
-            load(0, kid, at_n);
-            if constexpr (CACHE == 1) {
-                load(1, kid, at_n);
+                put(0, place(0));
+                put(1, place(0));
+                ids_of(b0 + 1, kid);
+                load(0, kid, 0);
+                load(1, kid, 0);
                 scales_of(a.k_scale, kid, kn);
                 scales_of(a.v_scale, kid, vn);
-                put(0, at_n);
-            } else if (ST == 3) {
-                load(1, kid, at_n);
-                ids_of(b0 + 2, kid);
-                load(0, kid, at_p);
+                put(0, place(1));
+            } else {
+#pragma unroll
+                for (int i = 0; i < ST; ++i) {
+                    ids_of(b0 + i, kid);
+                    load(0, kid, place(i));
+                    if (i < ST - 1) load(1, kid, place(i));
+                }
+                wait_loads<0>();
             }
-            if constexpr (CACHE != 1) wait_loads<0>();
         }
         __syncthreads();
-        if (b0 < b1) settle_values(b0, at_c);
+        if (b0 < b1) settle_values(b0, place(0));
         __syncthreads();
         if (b0 < b1) {
             if (b0 * 32 < wave_last) {
-                scores(sa, s_k + at_c);
+                scores(sa, s_k + place(0));
                 settle_scores(sa, b0 * 32, ks, true);
             }
             vid[0] = kid[0], vid[1] = kid[1];                        // (the last keys loaded are the next values)
             ids_of(b0 + (CACHE == 1 ? 2 : ST), kid);
         }
         __syncthreads();                                             // (the first keys' place is free)
-        // what is loaded in step b.  Page ids behind the last are the last's: the loads are the same number in every step
-        auto fetch = [&](int b) __attribute__((always_inline)) {
+        // what is loaded in step b, the i-th (`i` counts modulo ST).  Page ids behind the last are the last's: the
+        // loads are the same number in every step
+        auto fetch = [&](int b, int i) __attribute__((always_inline)) {
             if constexpr (CACHE == 1) {
-                put(1, at_n);
+                put(1, place(i + 1));
                 load(0, kid, 0);
                 load(1, kid, 0);
             } else {
-                load(0, kid, at_c);
-                load(1, vid, at_p);
+                load(0, kid, place(i));
+                load(1, vid, place(i + ST - 1));
                 vid[0] = kid[0], vid[1] = kid[1];
                 ids_of(b + ST + 1, kid);
             }
         };
-        // ... and what step b + 1 reads of it, in place
-        auto arrive = [&](int b) __attribute__((always_inline)) {
+        // ... and what step b + 1 reads, in place
+        auto arrive = [&](int b, int i) __attribute__((always_inline)) {
             if constexpr (CACHE == 1) {
-                put(0, at_p);                                        // (keys b + 2 in the place of b - 1)
-                vs[0] = vn[0], vs[1] = vn[1];
+                put(0, place(i + 2));
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    ks[p] = kn[p];
+                    vs[p] = vn[p];
+                }
                 scales_of(a.k_scale, kid, kn);
                 scales_of(a.v_scale, kid, vn);
                 ids_of(b + 3, kid);
             } else {
-                wait_loads<ST == 3 ? 2 * LOADS : 0>();
+                wait_loads<2 * LOADS * (ST - 2)>();
             }
         };
         // step b: `st` holds the scores of block b.  Away from the border every row sees blocks b and b + 1
-        auto inner = [&](int b, f32x16_t &st, f32x16_t &nx) __attribute__((always_inline)) {
-            fetch(b);
-            const float vc[2] = {vs[0], vs[1]};
-            scores(nx, s_k + at_n);
-            weigh(st, vc);
-            values(st, s_v + at_c);
+        auto inner = [&](int b, int i, f32x16_t &st, f32x16_t &nx) __attribute__((always_inline)) {
+            fetch(b, i);
+            scores(nx, s_k + place(i + 1));
+            weigh(st, ks, vs);
+            values(st, s_v + place(i));
             settle_scores(nx, (b + 1) * 32, kn, false);
-            arrive(b);
-            turn();
+            arrive(b, i);
             __syncthreads();
         };
         auto step = [&](int b, f32x16_t &st, f32x16_t &nx) __attribute__((always_inline)) {
             const bool next = b + 1 < b1, mine = b * 32 < wave_last, more = next && (b + 1) * 32 < wave_last;
-            const float vc[2] = {vs[0], vs[1]};
-            if (next) fetch(b);
+            const int i = b - b0;
+            if (next) fetch(b, i);
             // (block b + 2's mark: last read two steps ago, made in the next one)
             if (tid == 0) s_odd[(b + 2) & 3] = 0;
             if (mine) {
-                weigh(st, vc);
-                values(st, s_v + at_c);
+                weigh(st, ks, vs);
+                values(st, s_v + place(i));
                 if ((b + 1) * 32 > border) {
                     const uint32_t odd = uni(s_odd[b & 3]);
                     if (odd) add_odd(b, odd);
                 }
             }
             if (more) {
-                scores(nx, s_k + at_n);
+                scores(nx, s_k + place(i + 1));
                 settle_scores(nx, (b + 1) * 32, kn, true);
             }
             if (next) {
-                arrive(b);
-                settle_values(b + 1, at_n);
+                arrive(b, i);
+                settle_values(b + 1, place(i + 1));
             }
-            turn();
             __syncthreads();
         };
+        // (ST steps at a time: the places are constants, and with them 12 additions of addresses a step fall away)
         int b = b0;
         if (row0 < rows) {
-            for (; (b + 3) * 32 <= border; b += 2) {
-                inner(b, sa, sb);
-                inner(b + 1, sb, sa);
-            }
-        } else {
-            for (; (b + 3) * 32 <= border; b += 2)
+            for (; (b + ST + 1) * 32 <= border; b += ST)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    fetch(b + k);
-                    arrive(b + k);
-                    turn();
+                for (int k = 0; k < ST; k += 2) {
+                    inner(b + k, k, sa, sb);
+                    inner(b + k + 1, k + 1, sb, sa);
+                }
+        } else {
+            for (; (b + ST + 1) * 32 <= border; b += ST)
+#pragma unroll
+                for (int k = 0; k < ST; ++k) {
+                    fetch(b + k, k);
+                    arrive(b + k, k);
                     __syncthreads();
                 }
         }
@@ -785,7 +792,7 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
             wait_lds();                                              // the keys are read
             if (more) load(0);
             settle_scores(st, b * 32, ks, true);
-            weigh(st, vs);
+            weigh(st, ks, vs);
             const bool border = (b + 1) * 32 > min(first, last);
             if (border && lane == 0) s_odd[wave] = 0;
             if constexpr (CACHE == 1) {
