@@ -382,8 +382,8 @@ struct PromptArgs {
     float lag;                        // 8 / qscale
     // workspace regions (PromptWs)
     int32_t *counts;                  // pieces, split items
-    int4 *pieces;                     // [max_pieces][2]: request, first token, token range; partial slot (-1: whole)
-    int4 *merges;                     // [max_merges]: request, first token, first slot, slots
+    int4 *pieces;                     // [max_pieces][2]: see Piece
+    int4 *merges;                     // [max_merges]: see Merge
     float *partial;                   // [slot][Hkv]: outputs [part_rows][D], maxima and sums [part_rows]
 };
 

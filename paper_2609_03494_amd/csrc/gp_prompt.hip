@@ -225,13 +225,13 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PromptArgs a) {
             if (x.parts > 1) {
                 slot = atomicAdd(&s_slots, x.parts);
                 const int at = atomicAdd(&s_merges, 1);
-                if (at < a.max_merges) a.merges[at] = make_int4(r, j0, slot, x.parts);
+                if (at < a.max_merges) a.merges[at] = make_int4(slot, x.parts, q.ts + j0, n);
             }
             int at = atomicAdd(&s_hist[bucket], x.parts);
             for (int p = 0; p < x.parts; ++p, ++at) {
                 if (at >= a.max_pieces) break;
-                a.pieces[2 * at] = make_int4(r, j0, p * x.per, min((p + 1) * x.per, seen));
-                a.pieces[2 * at + 1].x = slot < 0 ? -1 : slot + p;
+                a.pieces[2 * at] = make_int4(r, slot < 0 ? -1 : slot + p, p * x.per, min((p + 1) * x.per, seen));
+                a.pieces[2 * at + 1] = make_int4(q.ts + j0, n, q.before + j0, 0);
             }
         };
         for (int r0 = 0; r0 < a.R; r0 += kPlanThreads) {
@@ -285,7 +285,14 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PromptArgs a) {
 // A call of up to 64 requests of one item each needs no list: every workgroup finds its piece,
 // and every merging one its item, by a scan over the requests, a lane each.
 // piece: piece `index` (merge: split item `index`); r < 0: none.
-struct Place { int r, j0, from, to, slot, parts; };
+// (A piece and a split item as the lists have them: all that a workgroup has to know, so that
+// it does not look its request up first.)
+struct Piece {
+    int r, slot;                  // request (-1: none); partial slot (-1: a whole item)
+    int from, to;                 // tokens that the piece reads
+    int ts, n, before;            // the item's first row of q and out, its tokens, those that precede them
+};
+struct Merge { int slot, parts, ts, n; };
 __device__ inline int wave_sums(int x, int lane) {
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) {
@@ -294,7 +301,8 @@ __device__ inline int wave_sums(int x, int lane) {
     }
     return x;
 }
-__device__ inline Place direct_place(const PromptArgs &a, int index, bool merge, int lane) {
+template <bool MERGE>
+__device__ inline typename std::conditional<MERGE, Merge, Piece>::type direct_place(const PromptArgs &a, int index, int lane) {
     Asked q = {};
     if (lane < a.R) q = asked(a, lane);
     const bool in = q.in && q.n > 0;
@@ -303,30 +311,23 @@ __device__ inline Place direct_place(const PromptArgs &a, int index, bool merge,
     const int all = __shfl(wave_sums(in ? q.n : 0, lane), 63, 64), cost = __shfl(wave_sums(seen, lane), 63, 64);
     const Split x = split_of(seen, (in ? q.n : 0) << a.lg, share_of(cost, a.slots));
     const int parts = in ? x.parts : 0, split = parts > 1 ? parts : 0;
-    const int slot_end = wave_sums(split, lane), end = merge ? wave_sums(split ? 1 : 0, lane) : wave_sums(parts, lane);
-    const int begin = end - (merge ? (split ? 1 : 0) : parts);
-    const uint64_t who = __ballot(index >= begin && index < end);
-    Place p = {-1, 0, 0, 0, -1, 0};
-    if (!who || all > a.T) return p;
-    const int r = __builtin_ctzll(who);
-    p.r = r;
-    p.parts = uni(__shfl(parts, r, 64));
-    const int slot0 = uni(__shfl(slot_end, r, 64)) - p.parts;
-    if (merge) {
-        p.slot = slot0;
-        return p;
+    const int slot_end = wave_sums(split, lane), end = MERGE ? wave_sums(split ? 1 : 0, lane) : wave_sums(parts, lane);
+    const int begin = end - (MERGE ? (split ? 1 : 0) : parts);
+    const uint64_t who = all > a.T ? 0 : __ballot(index >= begin && index < end);
+    const int r = who ? __builtin_ctzll(who) : 0, parts_r = __shfl(parts, r, 64), slot0 = __shfl(slot_end, r, 64) - parts_r;
+    const int ts = __shfl(q.ts, r, 64), n = __shfl(q.n, r, 64), before = __shfl(q.before, r, 64);
+    if constexpr (MERGE) {
+        return {slot0, who ? parts_r : 0, ts, n};
+    } else {
+        const int part = index - __shfl(begin, r, 64), per = __shfl(x.per, r, 64);
+        return {who ? r : -1, parts_r > 1 ? slot0 + part : -1, part * per, min(part * per + per, __shfl(seen, r, 64)), ts, n, before};
     }
-    const int part = index - uni(__shfl(begin, r, 64)), per = uni(__shfl(x.per, r, 64));
-    p.from = part * per;
-    p.to = min(p.from + per, uni(__shfl(seen, r, 64)));
-    p.slot = p.parts > 1 ? slot0 + part : -1;
-    return p;
 }
 
 // ---------------------------------------------------------------- products --
 
 template <int CACHE, int D>
-__global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
+__global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void prompt_kernel(PromptArgs a) {
     using TL = Block<CACHE, D>;
     using E = typename std::conditional<CACHE == 4, float, uint16_t>::type;
     constexpr int DB = D / 32, LOADS = TL::LOADS;
@@ -339,19 +340,18 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
     static_assert(NW * 32 * D * 4 <= TL::MEM, "the waves' parts meet in LDS");
     const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
     const int h = blockIdx.x % a.Hkv, at_piece = blockIdx.x / a.Hkv;
-    Place piece;
+    Piece piece;
     if (a.direct) {
-        piece = direct_place(a, at_piece, false, lane);
+        piece = direct_place<false>(a, at_piece, lane);
         if (piece.r < 0) return;
     } else {
         if (at_piece >= scalar_load(a.counts, 0)) return;
         const int32_t *x = reinterpret_cast<const int32_t *>(a.pieces + 2 * (size_t)at_piece);
-        piece = {scalar_load(x, 0), scalar_load(x, 1), scalar_load(x, 2), scalar_load(x, 3), scalar_load(x, 4), 0};
+        piece = {scalar_load(x, 0), scalar_load(x, 1), scalar_load(x, 2), scalar_load(x, 3), scalar_load(x, 4), scalar_load(x, 5), scalar_load(x, 6)};
     }
-    const int r = uni(piece.r), j0 = uni(piece.j0), from_token = uni(piece.from), to_token = uni(piece.to), slot = uni(piece.slot);
-    const Asked rq = asked(a, r);
-    const int rows = min(a.tokens, rq.n - j0) << a.lg;               // of this item
-    const int first = rq.before + j0 + 1, last = to_token;           // tokens that its first row sees, the end of the piece
+    const int r = uni(piece.r), slot = uni(piece.slot), from_token = uni(piece.from), ts = uni(piece.ts), before = uni(piece.before);
+    const int rows = uni(piece.n) << a.lg;                           // of this item
+    const int first = before + 1, last = uni(piece.to);              // tokens that its first row sees, the end of the piece
     const int last_page = max(last - 1, 0) / kPage;
     const bool narrow = rows <= 32;
 
@@ -359,10 +359,10 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_kernel(PromptArgs a) {
     const int col = lane & 31, half = lane >> 5;
     const int row0 = narrow ? 0 : wave * 32;
     const int row = row0 + col, at = min(row, rows - 1);
-    const int sees = min(rq.before + j0 + (at >> a.lg) + 1, last);
-    const int wave_first = rq.before + j0 + (min(row0, rows - 1) >> a.lg) + 1;
-    const int wave_last = row0 < rows ? rq.before + j0 + (min(row0 + 31, rows - 1) >> a.lg) + 1 : 0;
-    const int64_t token = rq.ts + j0 + (at >> a.lg);
+    const int sees = min(before + (at >> a.lg) + 1, last);
+    const int wave_first = before + (min(row0, rows - 1) >> a.lg) + 1;
+    const int wave_last = row0 < rows ? before + (min(row0 + 31, rows - 1) >> a.lg) + 1 : 0;
+    const int64_t token = ts + (at >> a.lg);
     const int head = h * a.G + (at & (a.G - 1));
     u32x4_t q[QS];
     {
@@ -908,21 +908,20 @@ template <typename E, int D, int RPW, int BATCH>
 __global__ __launch_bounds__(256) void merge_kernel(PromptArgs a) {
     constexpr int LANES = D / 4, ROWS = 256 / LANES;
     const int h = blockIdx.x % a.Hkv, at = blockIdx.x / a.Hkv;
-    int4 x;
+    Merge x;
     if (a.direct) {
-        const Place p = direct_place(a, at, true, threadIdx.x & 63);
-        if (p.r < 0) return;
-        x = make_int4(p.r, 0, p.slot, p.parts);
+        x = direct_place<true>(a, at, threadIdx.x & 63);
+        if (x.parts == 0) return;
     } else {
         if (at >= scalar_load(a.counts, 1)) return;
-        x = a.merges[at];
+        const int4 y = a.merges[at];
+        x = {y.x, y.y, y.z, y.w};
     }
-    const Asked rq = asked(a, x.x);
-    const int rows = min(a.tokens, rq.n - x.y) << a.lg;
-    const int u = threadIdx.x % LANES, parts = uni(x.w);
+    const int rows = x.n << a.lg;
+    const int u = threadIdx.x % LANES, parts = uni(x.parts);
     for (int row = blockIdx.y * RPW + threadIdx.x / LANES; row < min(rows, (int)(blockIdx.y + 1) * RPW); row += ROWS) {
         const size_t stride = (size_t)a.Hkv * a.part_rows * (D + 2);
-        const float *p = a.partial + ((size_t)x.z * a.Hkv + h) * a.part_rows * (D + 2);
+        const float *p = a.partial + ((size_t)x.slot * a.Hkv + h) * a.part_rows * (D + 2);
         const float *ml = p + (size_t)a.part_rows * D + row;
         float m = kNegInf, l = 0.0f;
         f32x4_t o = {};
@@ -960,7 +959,7 @@ __global__ __launch_bounds__(256) void merge_kernel(PromptArgs a) {
         float y[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) y[c] = l > 0.0f ? o[c] * inv : 0.0f;
-        const int64_t token = rq.ts + x.y + (row >> a.lg);
+        const int64_t token = x.ts + (row >> a.lg);
         E *to = reinterpret_cast<E *>(a.out) + (token * a.Hkv * a.G + h * a.G + (row & (a.G - 1))) * D + 4 * u;
         if constexpr (sizeof(E) == 4)
             *reinterpret_cast<u32x4_e4_t *>(to) = u32x4_t{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])};
