@@ -171,7 +171,7 @@ size_t gp_workspace_bytes(int32_t op, int32_t num_reqs, int32_t num_bnd, int32_t
             return decode_ws(num_reqs, num_q_heads, num_kv_heads, head_dim, max_pages, decode_waves(elem_bytes(dtype), head_dim)).total;
         case GP_OP_SCORE: return score_ws(num_bnd, num_q_heads, num_kv_heads, max_pages).total;
         case GP_OP_SELECT: return select_ws(num_reqs, num_kv_heads, max_pages);
-        case GP_OP_PROMPT: return prompt_ws(num_reqs, num_bnd, num_q_heads, num_kv_heads, head_dim).total;
+        case GP_OP_PROMPT: return prompt_ws(num_reqs, num_bnd, num_q_heads, num_kv_heads, head_dim, false).total;
         case GP_OP_APPLY:
             return apply_ws(num_bnd, num_kv_heads, head_dim, elem_bytes(dtype), max_pages, n_layers).total;
     }
@@ -524,12 +524,13 @@ gp_status_t prompt_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, cons
     a.G = num_q_heads / kv->num_kv_heads;
     while (1 << a.lg < a.G) ++a.lg;
     a.tokens = kPromptRows / a.G;
-    const PromptWs w = prompt_ws(ps->num_reqs, num_tokens, num_q_heads, kv->num_kv_heads, kv->head_dim);
+    a.direct = ps->num_reqs <= 64 && (!tok_start || num_tokens <= a.tokens);
+    const PromptWs w = prompt_ws(ps->num_reqs, num_tokens, num_q_heads, kv->num_kv_heads, kv->head_dim, a.direct);
     if (w.items * kv->num_kv_heads >= int64_t(1) << 23) return GP_ERR_UNSUPPORTED;     // (a grid below 2^32 threads)
     if (ws_bytes < w.total) return GP_ERR_WORKSPACE;
     unsigned char *base = static_cast<unsigned char *>(ws);
-    a.direct = ps->num_reqs <= 64 && (!tok_start || num_tokens <= a.tokens);
     a.slots = w.slots;
+    a.fine = w.fine;
     a.max_pieces = w.max_pieces;
     a.max_merges = w.max_merges;
     a.part_rows = w.part_rows;

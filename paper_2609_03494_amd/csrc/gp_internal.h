@@ -188,22 +188,25 @@ __host__ __device__ inline size_t select_ws(int R, int Hkv, int max_pages) {
 }
 
 // Division of a prompt attention call (see plan_kernel).  An item has kPromptRows / G
-// new tokens; pieces of a split item cost no less than the batch's share per slot, so all split
-// items together have at most twice as many pieces as there are slots.
+// new tokens; pieces of a split item cost no less than the batch's share per slot (of up to 32
+// rows: 1 / fine of it), and an item is split only where it is a quarter more than that: all
+// split items together have at most 1.8 slots pieces of many rows, or fine times as many of few.
 struct PromptWs {
     size_t counts, pieces, merges, partial, total;
     int64_t items;
-    int slots, max_pieces, max_merges, part_slots, part_rows;
+    int slots, fine, max_pieces, max_merges, part_rows;
 };
-__host__ __device__ inline PromptWs prompt_ws(int R, int64_t T, int Hq, int Hkv, int D) {
+__host__ __device__ inline PromptWs prompt_ws(int R, int64_t T, int Hq, int Hkv, int D, bool direct) {
     PromptWs w;
     const int G = Hq / Hkv, tokens = kPromptRows / G;
     w.items = T / tokens + (R < T ? R : T);
     w.slots = cdiv(kPromptSlots, Hkv);
-    w.part_slots = 2 * w.slots + 2;
-    w.max_pieces = (int)w.items + w.part_slots;
-    w.max_merges = (int)(w.items < w.slots + 1 ? w.items : w.slots + 1);
+    w.fine = direct ? 1 : 2;
+    const int parts = 2 * w.slots + 2;
+    w.max_pieces = (int)w.items + parts * w.fine;
+    w.max_merges = (int)(w.items < parts * w.fine / 2 ? w.items : parts * w.fine / 2);
     w.part_rows = T * G < kPromptRows ? (int)(T * G + 31) / 32 * 32 : kPromptRows;
+    const int units = w.part_rows / 32 > w.fine ? w.part_rows / 32 : w.fine;
     size_t off = 0;
     w.counts = off;
     off += kAlign;
@@ -211,8 +214,8 @@ __host__ __device__ inline PromptWs prompt_ws(int R, int64_t T, int Hq, int Hkv,
     off = align_up(off + (size_t)w.max_pieces * 32);
     w.merges = off;
     off = align_up(off + (size_t)w.max_merges * 16);
-    w.partial = off;
-    off = align_up(off + (size_t)w.part_slots * Hkv * w.part_rows * (D + 2) * sizeof(float));
+    w.partial = off;    // float: [unit][Hkv][32][D + 2]
+    off = align_up(off + (size_t)parts * units * Hkv * 32 * (D + 2) * sizeof(float));
     w.total = off;
     return w;
 }
@@ -377,14 +380,15 @@ struct PromptArgs {
     int tokens;                       // new tokens of an item
     bool direct;                      // one item per request, no more than 64: without a list of pieces
     int slots;                        // pieces that the batch is divided into where items alone are fewer, about
-    int max_pieces, max_merges, part_rows;   // pieces and split items of one KV head at most; rows of a partial
+    int fine;                         // pieces of up to 32 rows are so much smaller
+    int max_pieces, max_merges, part_rows;   // pieces and split items of one KV head at most; rows of a partial of more than 32
     float qscale;                     // scale * log2(e); 8-bit: times kQ8KeyScale
     float lag;                        // 8 / qscale
     // workspace regions (PromptWs)
     int32_t *counts;                  // pieces, split items
     int4 *pieces;                     // [max_pieces][2]: see Piece
     int4 *merges;                     // [max_merges]: see Merge
-    float *partial;                   // [slot][Hkv]: outputs [part_rows][D], maxima and sums [part_rows]
+    float *partial;                   // [unit][Hkv]: of a part (its units together) outputs [rows][D], maxima, sums [rows]
 };
 
 struct BoundsArgs {

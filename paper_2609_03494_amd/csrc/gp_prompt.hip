@@ -145,10 +145,13 @@ constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kBuckets = 25
 // reciprocals, put right where they have to be exact: integer divisions were most of this
 // kernel's time.
 struct Split { int parts, per; };
-__device__ inline Split split_of(int seen, int rows, int share) {
-    const int piece = max(share, rows <= 32 ? kPromptLeastNarrow : kPromptLeastWide);
+__device__ inline Split split_of(int seen, int rows, int share, int fine) {
+    // (fine: pieces of few rows per share, of an item that is more than one; their parts cost little, and
+    // finer ones even out the places: 64 requests of 1024-8143 tokens, one token each, 243 -> 234 us)
+    const int least = rows <= 32 ? kPromptLeastNarrow : kPromptLeastWide, limit = max(share, least);
+    const int piece = rows <= 32 ? max(share / fine, least) : limit;
     Split x = {1, seen};
-    if (seen <= piece + piece / 4) return x;
+    if (seen <= limit + limit / 4) return x;
     const int parts = (int)((float)seen / (float)piece) + 1;             // at most 1.8 seen / piece
     x.per = ((int)((float)seen / (float)parts) + 64) & ~63;              // at least seen / parts
     x.parts = (int)((float)seen / (float)x.per);
@@ -156,6 +159,8 @@ __device__ inline Split split_of(int seen, int rows, int share) {
     while (x.parts > 1 && (x.parts - 1) * x.per >= seen) --x.parts;
     return x;
 }
+// What a part takes of the workspace, in units of 32 rows.
+__device__ inline int part_units(const PromptArgs &a, int rows) { return rows <= 32 ? 1 : a.part_rows / 32; }
 __device__ inline int share_of(unsigned long long cost, int slots) {
     const unsigned long long x = (cost + slots - 1) / slots;
     return x < INT_MAX / 2 ? (int)x : INT_MAX / 2;
@@ -214,7 +219,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PromptArgs a) {
     for (int pass = sorted ? 1 : 2; pass < 3; ++pass) {
         auto take = [&](int r, const Asked &q, int i) {
             const int j0 = i * a.tokens, n = min(a.tokens, q.n - j0), seen = max(q.before + j0 + n, 0);
-            const Split x = split_of(seen, n << a.lg, share);
+            const Split x = split_of(seen, n << a.lg, share, a.fine);
             const int bucket = sorted ? max(kBuckets - 1 - (int)((float)min(x.per, seen) * scale), 0) : 0;
             if (pass == 1) {
                 atomicAdd(&s_hist[bucket], x.parts);
@@ -222,15 +227,16 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PromptArgs a) {
             }
             // (the bounds hold for any batch, see PromptWs)
             int slot = -1;
+            const int units = part_units(a, n << a.lg);
             if (x.parts > 1) {
-                slot = atomicAdd(&s_slots, x.parts);
+                slot = atomicAdd(&s_slots, x.parts * units);
                 const int at = atomicAdd(&s_merges, 1);
                 if (at < a.max_merges) a.merges[at] = make_int4(slot, x.parts, q.ts + j0, n);
             }
             int at = atomicAdd(&s_hist[bucket], x.parts);
             for (int p = 0; p < x.parts; ++p, ++at) {
                 if (at >= a.max_pieces) break;
-                a.pieces[2 * at] = make_int4(r, slot < 0 ? -1 : slot + p, p * x.per, min((p + 1) * x.per, seen));
+                a.pieces[2 * at] = make_int4(r, slot < 0 ? -1 : slot + p * units, p * x.per, min((p + 1) * x.per, seen));
                 a.pieces[2 * at + 1] = make_int4(q.ts + j0, n, q.before + j0, 0);
             }
         };
@@ -309,18 +315,18 @@ __device__ inline typename std::conditional<MERGE, Merge, Piece>::type direct_pl
     const int seen = in ? max(q.before + q.n, 0) : 0;
     // (starts that decrease can ask for more than T tokens: none is served)
     const int all = __shfl(wave_sums(in ? q.n : 0, lane), 63, 64), cost = __shfl(wave_sums(seen, lane), 63, 64);
-    const Split x = split_of(seen, (in ? q.n : 0) << a.lg, share_of(cost, a.slots));
-    const int parts = in ? x.parts : 0, split = parts > 1 ? parts : 0;
+    const Split x = split_of(seen, (in ? q.n : 0) << a.lg, share_of(cost, a.slots), 1);
+    const int parts = in ? x.parts : 0, units = part_units(a, (in ? q.n : 0) << a.lg), split = parts > 1 ? parts * units : 0;
     const int slot_end = wave_sums(split, lane), end = MERGE ? wave_sums(split ? 1 : 0, lane) : wave_sums(parts, lane);
     const int begin = end - (MERGE ? (split ? 1 : 0) : parts);
     const uint64_t who = all > a.T ? 0 : __ballot(index >= begin && index < end);
-    const int r = who ? __builtin_ctzll(who) : 0, parts_r = __shfl(parts, r, 64), slot0 = __shfl(slot_end, r, 64) - parts_r;
+    const int r = who ? __builtin_ctzll(who) : 0, parts_r = __shfl(parts, r, 64), units_r = __shfl(units, r, 64), slot0 = __shfl(slot_end, r, 64) - parts_r * units_r;
     const int ts = __shfl(q.ts, r, 64), n = __shfl(q.n, r, 64), before = __shfl(q.before, r, 64);
     if constexpr (MERGE) {
         return {slot0, who ? parts_r : 0, ts, n};
     } else {
         const int part = index - __shfl(begin, r, 64), per = __shfl(x.per, r, 64);
-        return {who ? r : -1, parts_r > 1 ? slot0 + part : -1, part * per, min(part * per + per, __shfl(seen, r, 64)), ts, n, before};
+        return {who ? r : -1, parts_r > 1 ? slot0 + part * units_r : -1, part * per, min(part * per + per, __shfl(seen, r, 64)), ts, n, before};
     }
 }
 
@@ -882,7 +888,8 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
                     *reinterpret_cast<u32x2_e2_t *>(to + 32 * d + 8 * i) = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
             }
     } else {
-        float *to = a.partial + ((size_t)slot * a.Hkv + h) * a.part_rows * (D + 2);
+        const int units = part_units(a, rows), part_rows = 32 * units;
+        float *to = a.partial + ((size_t)slot * a.Hkv + (size_t)h * units) * 32 * (D + 2);
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -892,9 +899,9 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
                     f32x4_t{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
             }
         if (half == 0 && (!narrow || wave == 0)) {
-            float *ml = to + (size_t)a.part_rows * D;
+            float *ml = to + (size_t)part_rows * D;
             ml[row] = m * unit;
-            ml[a.part_rows + row] = l;
+            ml[part_rows + row] = l;
         }
     }
 }
@@ -920,9 +927,10 @@ __global__ __launch_bounds__(256) void merge_kernel(PromptArgs a) {
     const int rows = x.n << a.lg;
     const int u = threadIdx.x % LANES, parts = uni(x.parts);
     for (int row = blockIdx.y * RPW + threadIdx.x / LANES; row < min(rows, (int)(blockIdx.y + 1) * RPW); row += ROWS) {
-        const size_t stride = (size_t)a.Hkv * a.part_rows * (D + 2);
-        const float *p = a.partial + ((size_t)x.slot * a.Hkv + h) * a.part_rows * (D + 2);
-        const float *ml = p + (size_t)a.part_rows * D + row;
+        const int units = part_units(a, rows), part_rows = 32 * units;
+        const size_t stride = (size_t)a.Hkv * part_rows * (D + 2);
+        const float *p = a.partial + ((size_t)x.slot * a.Hkv + (size_t)h * units) * 32 * (D + 2);
+        const float *ml = p + (size_t)part_rows * D + row;
         float m = kNegInf, l = 0.0f;
         f32x4_t o = {};
         for (int k0 = 0; k0 < parts; k0 += BATCH) {
@@ -936,7 +944,7 @@ __global__ __launch_bounds__(256) void merge_kernel(PromptArgs a) {
                 if (k0 + k >= parts) continue;            // (the same for all threads)
                 const size_t part = (k0 + k) * stride;
                 mk[k] = ml[part];
-                lk[k] = ml[part + a.part_rows];
+                lk[k] = ml[part + part_rows];
                 ok[k] = *reinterpret_cast<const f32x4_t *>(p + part + (size_t)row * D + 4 * u);
             }
             float up = m;
