@@ -511,15 +511,13 @@ gp_status_t prompt_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, cons
     if (st != GP_OK) return st;
     if ((st = check_state(ps, kv)) != GP_OK) return st;
     if (!dims_ok(num_q_heads, kv->num_kv_heads, kv->head_dim)) return GP_ERR_UNSUPPORTED;
-    if (!(scale > 0.0f) || !isfinite(scale) || (kv8 && scale >= 0x1p111f) || num_tokens < 0) return GP_ERR_INVALID;
+    if (!(scale > 0.0f) || !(scale < (kv8 ? 0x1p111f : 0x1p127f)) || num_tokens < 0) return GP_ERR_INVALID;
     if (!tok_start && num_tokens != ps->num_reqs) return GP_ERR_INVALID;
     const int64_t row = (int64_t)num_q_heads * kv->head_dim;
     if (q_stride < row || q_stride > int64_t(1) << 30 || !aligned16(kv->k, kv->v)) return GP_ERR_INVALID;
     if (ps->num_reqs == 0 || num_tokens == 0) return GP_OK;
     if (!q || !out || !ws) return GP_ERR_INVALID;
     if (ps->num_reqs > 65535 || ps->max_pages > kMaxDecodePages || kv->num_kv_heads > kMaxListedHeads) return GP_ERR_UNSUPPORTED;
-    const int e = elem_bytes(kv->dtype);
-    if (overlap(out, num_tokens * row, q, (num_tokens - 1) * q_stride + row, e)) return GP_ERR_INVALID;
     PromptArgs a = {};
     a.G = num_q_heads / kv->num_kv_heads;
     while (1 << a.lg < a.G) ++a.lg;
@@ -527,6 +525,8 @@ gp_status_t prompt_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, cons
     a.direct = ps->num_reqs <= 64 && (!tok_start || num_tokens <= a.tokens);
     const PromptWs w = prompt_ws(ps->num_reqs, num_tokens, num_q_heads, kv->num_kv_heads, kv->head_dim, a.direct);
     if (w.items * kv->num_kv_heads >= int64_t(1) << 23) return GP_ERR_UNSUPPORTED;     // (a grid below 2^32 threads)
+    const int e = elem_bytes(kv->dtype);
+    if (overlap(out, num_tokens * row, q, (num_tokens - 1) * q_stride + row, e)) return GP_ERR_INVALID;
     if (ws_bytes < w.total) return GP_ERR_WORKSPACE;
     unsigned char *base = static_cast<unsigned char *>(ws);
     a.slots = w.slots;

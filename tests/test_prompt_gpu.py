@@ -336,3 +336,92 @@ def test_prompt_captured_and_on_streams(kind):
         other.call(stream=two)
         torch.cuda.synchronize()
         assert torch.equal(c.out, e.out) and torch.equal(other.out, want)
+
+
+def test_prompt_more_requests_than_the_planner_has_threads():
+    """Long prompts before and behind the first thousand of requests, single tokens, and starts that are not given."""
+    _say("1500 requests")
+    reqs = [((5 * r) % 90, 26, 300 if r in (3, 1023, 1024, 1499) else r % 3) for r in range(1500)]
+    c = Case("bf16", reqs, 4, 2, 64, 7)
+    c.call()
+    torch.cuda.synchronize()
+    c.check("1500")
+    c = Case("q8", [((11 * r) % 700, 45, 1) for r in range(300)], 4, 2, 64, 7, single=True)
+    c.call()
+    torch.cuda.synchronize()
+    c.check("300 singles")
+
+
+@pytest.mark.parametrize("kind,hq,hkv,d,reqs", [("bf16", 8, 1, 128, [(100000, 6260, 70)]), ("f32", 1, 1, 64, [(70000, 4380, 2), (30, 4, 9)]),
+                                                ("q8", 4, 1, 64, [(60000, 3800, 1)] * 3), ("bf16", 64, 64, 64, [(900, 70, 130), (5, 2, 20)]),
+                                                ("f32", 80, 40, 64, [(300, 30, 33)]), ("q8", 40, 40, 128, [(40, 9, 90), (2000, 130, 3)])])
+def test_prompt_few_and_many_heads(kind, hq, hkv, d, reqs):
+    """One KV head: an item in as many pieces as there are places for them; many heads: hardly any."""
+    _say(f"heads {kind} {hq}/{hkv}")
+    c = Case(kind, reqs, hq, hkv, d, 12)
+    c.call()
+    torch.cuda.synchronize()
+    c.check("heads")
+
+
+def test_prompt_one_workspace_for_calls_of_all_sizes():
+    """The workspace of the largest call serves smaller ones, whatever was left in it."""
+    _say("one workspace")
+    big = Case("bf16", [(500, 120, 900), (7, 40, 300), (3000, 200, 9)], 8, 2, 64, 1)
+    big.ws.random_(0, 256)
+    for reqs in ([(500, 120, 900), (7, 40, 300), (3000, 200, 9)], [(3000, 200, 1), (5, 1, 1), (100, 20, 6)], [(0, 9, 100), (0, 9, 0), (4, 1, 2)]):
+        c = Case("bf16", reqs, 8, 2, 64, 1)
+        assert c.ws.numel() <= big.ws.numel()
+        c.ws = big.ws
+        for _ in range(2):
+            c.out.fill_(7.0)
+            c.call()
+            torch.cuda.synchronize()
+            c.check("workspace")
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "q8"])
+def test_prompt_pools_past_32_bits(kind):
+    """Pages whose bytes lie past 2^32 of the pool's start."""
+    _say(f"large pool {kind}")
+    hkv, d = 16, 128
+    c = Case(kind, [(200, 20, 90), (70, 6, 1)], 2 * hkv, hkv, d, 3)
+    page = hkv * 16 * d * c.kv.k.element_size()
+    pool, small = 2 ** 32 // page + 300, c.kv.k.shape[0]
+    ids = torch.randperm(pool - 2 ** 31 // page, generator=torch.Generator().manual_seed(0))[:small] + 2 ** 31 // page
+    ids[::2] = pool - 1 - torch.arange(len(ids[::2]))
+    made = []
+    for x in vars(c.kv).values():
+        y = torch.zeros((pool, *x.shape[1:]), dtype=torch.uint8 if kind == "q8" and x.dim() == 4 else x.dtype, device=DEV)
+        y[ids.to(DEV)] = x.view(torch.uint8) if y.dtype == torch.uint8 else x
+        made.append(y.view(x.dtype))
+    want = c.tokens(0, 0, 290).clone()
+    c.kv = type(c.kv)(*made)
+    c.table = torch.where(c.table >= 0, ids[c.table.clamp(min=0).long()].int(), -1)
+    c.ps = _state(c.table, [P for _, P, _ in c.reqs], [m for m, _, _ in c.reqs], pool)
+    assert torch.equal(c.tokens(0, 0, 290), want) and int(c.table.max()) * page > 2 ** 32
+    c.call()
+    torch.cuda.synchronize()
+    c.check("large pool")
+
+
+def test_prompt_scales_at_the_ends_of_their_range():
+    """Scales whose product with log2(e) is as small or as large as float32 holds: the mean, and the first of the largest scores."""
+    _say("scales")
+    c = Case("f32", [(40, 4, 9)], 2, 1, 64, 3)
+    V = c.tokens(1, 0, 49)[0]
+    c.scale = 1e-38
+    c.call()
+    torch.cuda.synchronize()
+    for j in range(9):
+        mean = V[:41 + j].mean(0)
+        assert bool(((c.out[j].double() - mean).abs() <= V.abs().mean() * 49 * 2.0 ** -20).all())
+    c.scale = 1.6e38                                            # below 2^127
+    c.q.zero_()
+    c.q[:, :, 0] = 2.0 ** -126
+    c.kv.k.masked_fill_(c.kv.k == c.kv.k, 0.0)                  # (the NaN of nobody's slots stay)
+    _put(c, 0, 7, 0, 0, 1000.0, 0)
+    c.call()
+    torch.cuda.synchronize()
+    # token 7 is ahead by 1000 * 1.6e38 * 2^-126 = 1880
+    assert torch.equal(c.out.double(), V[7].expand(9, 2, 64))

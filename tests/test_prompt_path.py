@@ -87,6 +87,58 @@ def test_rope_frequencies(lib):  # noqa: F811
         gp.Rope(0, [])
 
 
+PROMPT = dict(start=FAKE, tokens=40, advanced=0, q=0x100000, q_stride=4096, hq=32, scale=0.088, out=0x900000, ws=FAKE, ws_bytes=1 << 40)
+
+
+@pytest.mark.parametrize("q8", [False, True])
+def test_prompt_attention_refusals(lib, q8):  # noqa: F811
+    fn, kv = (lib.gp_prompt_attention_q8, _kv8) if q8 else (lib.gp_prompt_attention, _kv)
+
+    def call(kv_=None, ps=None, **kw):
+        a = dict(PROMPT, **kw)
+        return fn(kv_ or kv(), ps or _ps(), a["start"], a["tokens"], a["advanced"], a["q"], a["q_stride"], a["hq"], a["scale"], a["out"],
+                  a["ws"], a["ws_bytes"], None)
+    nan, inf = float("nan"), float("inf")
+    assert fn(None, _ps(), FAKE, 40, 0, FAKE, 4096, 32, 0.1, FAKE, FAKE, 1 << 40, None) == INVALID
+    assert fn(kv(), None, FAKE, 40, 0, FAKE, 4096, 32, 0.1, FAKE, FAKE, 1 << 40, None) == INVALID
+    for bad in (dict(scale=0.0), dict(scale=-0.1), dict(scale=nan), dict(scale=inf), dict(scale=2.0 ** 127), dict(tokens=-1), dict(start=None),
+                dict(q_stride=4095), dict(q_stride=(1 << 30) + 1), dict(q=None), dict(out=None), dict(ws=None), dict(out=0x100000),
+                dict(out=0x100000 + 8), dict(out=0x100000 + 39 * 8192 + 8190), dict(out=0x100000 - 40 * 8192 + 2)):
+        assert call(**bad) == INVALID, bad
+    if q8:
+        assert call(scale=2.0 ** 111) == INVALID
+    for bad in (kv(k=FAKE + 8), kv(v=FAKE + 4), kv(pool=99)):
+        assert call(bad) == INVALID
+    for bad in (kv(d=96), kv(page=32)):
+        assert call(bad) == UNSUPPORTED
+    for hq in (24, 4, 0, 128):
+        assert call(hq=hq) == UNSUPPORTED
+    assert call(ps=_ps(R=65536)) == call(ps=_ps(width=8193)) == UNSUPPORTED
+    assert call(tokens=1 << 25) == UNSUPPORTED                         # 2^25 * 4 / 128 pieces of 8 heads
+    assert call(tokens=2 ** 31 - 1, q_stride=1 << 30) == UNSUPPORTED
+    size = gp.gp_workspace_bytes(gp.GP_OP_PROMPT, 4, 40, 32, 8, 128, 10, torch.bfloat16)
+    assert call(ws_bytes=size - 1) == call(ws_bytes=256) == call(ws_bytes=0) == WORKSPACE
+    assert call(tokens=0, q=None, out=None, ws=None) == call(ps=_ps(R=0), q=None) == 0
+
+
+def test_prompt_workspace(lib):  # noqa: F811
+    """A workspace of more tokens, or more requests, is no smaller; none of what is no shape."""
+    size = lambda R=4, T=40, hq=32, hkv=8, d=128, dt=torch.bfloat16: gp.gp_workspace_bytes(gp.GP_OP_PROMPT, R, T, hq, hkv, d, 10, dt)  # noqa: E731
+    for hq, hkv, d in ((32, 8, 128), (64, 8, 64), (5, 5, 64), (8, 1, 128), (64, 64, 64)):
+        for dt in (torch.bfloat16, torch.float32):
+            steps = [1, 2, 3, 4, 5, 8, 9, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 500, 1000, 30000]
+            sizes = [size(R=R, T=T, hq=hq, hkv=hkv, d=d, dt=dt) for R in (1, 3, 64, 65, 700) for T in steps]
+            for i, x in enumerate(sizes):
+                assert 0 < x < 1 << 31
+                if i % len(steps):
+                    assert x >= sizes[i - 1]
+                if i >= len(steps):
+                    assert x >= sizes[i - len(steps)]
+    for bad in (dict(hq=24), dict(d=96), dict(R=-1), dict(T=-1)):
+        with pytest.raises(gp.GrowPageError):
+            size(**bad)
+
+
 def _state(R=4, width=10, pool=100, **none):
     a = dict(table=FAKE, pages=FAKE, lens=FAKE, refs=FAKE, stack=FAKE, height=FAKE)
     a.update(none)
