@@ -8,7 +8,7 @@ import torch
 
 import paper_2609_03494_amd as gp
 from paper_2609_03494_amd import _lib
-from test_cache_ops import FAKE, INVALID, ROPE, UNSUPPORTED, WORKSPACE, _kv, _kv8, _ps, lib  # noqa: F401
+from test_cache_ops import _NoLaunch, FAKE, INVALID, ROPE, UNSUPPORTED, WORKSPACE, _kv, _kv8, _ps, lib  # noqa: F401
 
 
 def _rope(layout=0, n=128, mag=1.0, freq=None):
@@ -211,3 +211,65 @@ def test_binding_refusals():
     with pytest.raises(ValueError):
         gp.Layers([layer, gp.KV8Layer(k.view(torch.uint8)[..., :64].contiguous(), k.view(torch.uint8)[..., :64].contiguous(),
                                       torch.zeros(100, 2), torch.zeros(100, 2))])
+
+
+def _device_calls():
+    """Each call of the binding on a prompt's way, with every tensor that its kernels reach, by name."""
+    pool, hkv, d, R = 6, 2, 64, 3
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8)  # noqa: E731
+    state = lambda: gp.PageState(i32(R, 4), i32(R), i32(R), i32(pool), i32(pool), i32(1))  # noqa: E731
+    layers = {"": lambda: gp.KVLayer(bf(pool, hkv, 16, d), bf(pool, hkv, 16, d)),
+              "_q8": lambda: gp.KV8Layer(u8(pool, hkv, 16, d), u8(pool, hkv, 16, d), torch.ones(pool, hkv), torch.ones(pool, hkv))}
+    of_state = lambda ps: dict(page_table=ps.page_table, num_pages=ps.num_pages, seq_lens=ps.seq_lens)  # noqa: E731
+    rope = gp.Rope(gp.GP_ROPE_HALF, [1.0] * 16)
+    for q8, layer in layers.items():
+        kv, ps, t = layer(), state(), dict(positions=i32(R), k_new=bf(R, hkv, d), v_new=bf(R, hkv, d), q=bf(R, hkv, d),
+                                           q_out=bf(R, hkv, d), tok_start=i32(R + 1))
+        yield f"gp_append_rotary{q8}", {**vars(kv), **of_state(ps), **t}, lambda fn, kv=kv, ps=ps, t=t: fn(
+            kv, ps, t["positions"], t["k_new"], t["v_new"], rope, q=t["q"], q_out=t["q_out"], tok_start=t["tok_start"])
+        kv, ps, t = layer(), state(), dict(q=bf(R, hkv, d), out=bf(R, hkv, d), ws=u8(64), tok_start=i32(R + 1))
+        yield f"gp_prompt_attention{q8}", {**vars(kv), **of_state(ps), **t}, lambda fn, kv=kv, ps=ps, t=t: fn(
+            kv, ps, t["q"], 0.1, t["out"], t["ws"], tok_start=t["tok_start"])
+        kv, ps, t = layer(), state(), dict(parents=i32(2), children=i32(2), forked=i32(2), lengths=i32(2), positions=i32(R))
+        yield f"gp_pages_fork{q8}", {**vars(kv), **vars(ps), **t}, lambda fn, kv=kv, ps=ps, t=t: fn(
+            [kv], ps, t["parents"], t["children"], t["forked"], lengths=t["lengths"], positions=t["positions"])
+    kv, ps, t = layers[""](), state(), dict(q_pre=bf(R, hkv, d), qstate=torch.zeros(R, 2, hkv, d), slot_ids=i32(R), positions=i32(R),
+                                            bnd=i32(1), k_counts=i32(1, hkv, 2), scores=torch.zeros(1, hkv, 48), ws=u8(64))
+    yield "gp_boundary_score_rotary", {**vars(kv), **of_state(ps), **t}, lambda fn: fn(
+        kv, ps, t["q_pre"], t["qstate"], t["slot_ids"], t["positions"], t["bnd"], gp.Params(), rope, t["k_counts"], t["scores"], t["ws"])
+    ps1, t1 = state(), dict(tokens=i32(R), granted=i32(R))
+    yield "gp_pages_reserve", {**vars(ps1), **t1}, lambda fn: fn(ps1, t1["tokens"], t1["granted"])
+    ps2, t2 = state(), dict(reqs=i32(2))
+    yield "gp_pages_release", {**vars(ps2), **t2}, lambda fn: fn(ps2, t2["reqs"])
+
+
+def test_every_tensor_lies_on_the_current_device(monkeypatch):
+    """Host tensors that say they lie on device 0: the call goes through.  One of them at a time on the host or on
+    another device, whichever it is: the call is refused and the library not reached."""
+    fake = _NoLaunch()
+    monkeypatch.setattr(_lib, "load", lambda: fake)
+    monkeypatch.setattr(_lib, "_stream", lambda stream: 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    names = set()
+    for name, tensors, call in _device_calls():
+        fn = getattr(gp, name)
+        for t in tensors.values():
+            t.get_device = lambda: 0
+        fake.calls = 0
+        call(fn)
+        assert fake.calls == 1, name
+        for what, t in tensors.items():
+            for dev in (-1, 1):
+                t.get_device = lambda dev=dev: dev
+                with pytest.raises(ValueError, match="device"):
+                    call(fn)
+                assert fake.calls == 1, (name, what)
+            t.get_device = lambda: 0
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)      # all on a device that is not the current one
+        with pytest.raises(ValueError, match="current device"):
+            call(fn)
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+        names.add(name)
+    assert len(names) == 9
