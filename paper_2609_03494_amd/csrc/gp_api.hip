@@ -522,7 +522,8 @@ gp_status_t prompt_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, cons
     a.G = num_q_heads / kv->num_kv_heads;
     while (1 << a.lg < a.G) ++a.lg;
     a.tokens = kPromptRows / a.G;
-    a.direct = ps->num_reqs <= 64 && (!tok_start || num_tokens <= a.tokens);
+    a.several = tok_start && num_tokens > a.tokens;
+    a.direct = ps->num_reqs <= 64 && (!a.several || num_tokens / a.tokens + ps->num_reqs <= 64);
     const PromptWs w = prompt_ws(ps->num_reqs, num_tokens, num_q_heads, kv->num_kv_heads, kv->head_dim, a.direct);
     if (w.items * kv->num_kv_heads >= int64_t(1) << 23) return GP_ERR_UNSUPPORTED;     // (a grid below 2^32 threads)
     const int e = elem_bytes(kv->dtype);

@@ -378,7 +378,7 @@ struct PromptArgs {
     int64_t q_stride;                 // elements from token to token
     int R, T, Hkv, G, lg, max_pages, pool_pages, advanced;   // lg: log2 G
     int tokens;                       // new tokens of an item
-    bool direct;                      // one item per request, no more than 64: without a list of pieces
+    bool direct, several;             // up to 64 items, without a list of pieces; a request may have several
     int slots;                        // pieces that the batch is divided into where items alone are fewer, about
     int fine;                         // pieces of up to 32 rows are so much smaller
     int max_pieces, max_merges, part_rows;   // pieces and split items of one KV head at most; rows of a partial of more than 32
