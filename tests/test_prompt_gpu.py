@@ -354,7 +354,8 @@ def test_prompt_more_requests_than_the_planner_has_threads():
 
 @pytest.mark.parametrize("kind,hq,hkv,d,reqs", [("bf16", 8, 1, 128, [(100000, 6260, 70)]), ("f32", 1, 1, 64, [(70000, 4380, 2), (30, 4, 9)]),
                                                 ("q8", 4, 1, 64, [(60000, 3800, 1)] * 3), ("bf16", 64, 64, 64, [(900, 70, 130), (5, 2, 20)]),
-                                                ("f32", 80, 40, 64, [(300, 30, 33)]), ("q8", 40, 40, 128, [(40, 9, 90), (2000, 130, 3)])])
+                                                ("f32", 80, 40, 64, [(300, 30, 33)]), ("q8", 40, 40, 128, [(40, 9, 90), (2000, 130, 3)]), ("bf16", 16, 4, 64, [(12000, 783, 512)]),
+                                                ("q8", 8, 2, 128, [(6000, 440, 1000), (9000, 628, 1030)])])
 def test_prompt_few_and_many_heads(kind, hq, hkv, d, reqs):
     """One KV head: an item in as many pieces as there are places for them; many heads: hardly any."""
     _say(f"heads {kind} {hq}/{hkv}")
