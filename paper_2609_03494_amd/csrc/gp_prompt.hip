@@ -1,19 +1,37 @@
 // Attention of new tokens over the paged cache (gp_prompt_attention; Sec. 3.1
 // attention-output equation with a causal limit): whole prompts, chunks behind a
-// context, drafted tokens.
+// context, drafted tokens, single tokens.
 //
-// Work item: one KV head and kRows rows of one request, a row being a (new token, query
+// Work item: one KV head and kPromptRows rows of one request, a row being a (new token, query
 // head of that KV head) pair: the G heads of a token read the same keys, so they lie
-// side by side and the causal border of an item is kRows / G tokens wide.  A wave has 32
-// rows.  Keys and values come in tiles of Tile::TOK tokens through two LDS stages, one
-// filled (from registers, so that the loads of a tile are in flight during the one
-// before) while the other is read.
+// side by side and the causal border of an item is kPromptRows / G tokens wide.  A wave has 32
+// rows; keys and values come in blocks of 32 tokens, two pages, through LDS.
 //
 // Products, both transposed: S^T = K Q^T, then O^T += V^T P^T, on 32 x 32 matrix
 // instructions.  A lane then holds scores of one row only (its column), so maxima and
 // sums are in-lane but for one exchange with lane ^ 32, the rescaling of O^T is in-lane
 // as well, and the scores become the second product's operand without moving: lane half
-// h has tokens 8 k + 4 h + 0..3 of every 16, and V^T is read in that order.
+// h has tokens 8 k + 4 h + 0..3 of every 16, and V^T is read in that order (16 bits: by
+// transposing LDS reads).  Softmax in one pass, weights in units of log2; the maximum may
+// lag behind by 2^8, so that O^T is rescaled in few blocks.  Scores, statistics and outputs are
+// float32; the weights of 16- and 8-bit caches are rounded to bfloat16 for the second product, the
+// only form in which the matrix instruction takes them (half a step is 2^-8 of a weight).
+//
+// Two paths, by an item's rows.  More than 32 (wide): the four waves share the blocks, and a wave works
+// on the scores of block b + 1 and the weights of block b at once, independent work for the
+// matrix unit and the others; up to four blocks are on their way straight into LDS.  Up to 32 (narrow:
+// drafted and single tokens, ends of requests): bound by reading the cache, so every wave has blocks of its own
+// and no barrier, and the waves' results meet in LDS at the end.
+//
+// Bound (8 chunks of 1024 tokens behind 8192, 32/8 heads): the matrix unit and with it the chip's power at
+// head_dim 128, 1085 TFLOP/s in 1077 us, where a library's product of two 8192 x 8192 matrices
+// reaches 1154; head_dim 64 has half of the products per weight and is bound by the vector instructions of
+// the softmax (16 exponentials of 16 cycles are half of them): 616 us, 948 TFLOP/s.  8-bit: each code is widened
+// once a workgroup, 1184 us and 987 TFLOP/s, 762 and 766.  float32: its matrix instructions' rate, 1063 us for a quarter
+// of it, 137 TFLOP/s of 153.  64 single tokens behind 1024 to 8143: the read of the cache, 5.1 TB/s.
+// Tried and slower: the sum of weights by the matrix unit as well (bf16, head_dim 64: 5 %), keys widened by two waves
+// and values by the others (8 bits, head_dim 64: 1 %), the merge by whoever ends an item last (5 tokens behind 6001:
+// 24 us against 15).
 #include <float.h>
 
 #include <limits.h>

@@ -1,8 +1,9 @@
 // New tokens into the paged cache with the position rotation on the way
-// (gp_append_rope; Sec. 3.1 paged cache): the decode step's tokens as well as
-// whole prompts, into bfloat16, float32 and 8-bit pools.
+// (gp_append_rope, gp_append_rotary; Sec. 3.1 paged cache): the decode step's tokens as
+// well as whole prompts, into bfloat16, float32 and 8-bit pools.
 //
-// Rotation.  Pair (x_i, x_{i + d/2}) turns by t theta^(-2 i / d).  The angle is
+// Rotation.  Pair (x_i, x_{i + d/2}) turns by t theta^(-2 i / d), or pairs side by side, of a
+// part of the head, by a caller's frequencies.  The angle is
 // kept as a number of turns in 64 bits, t * (theta^(-2 i / d) / 2 pi) less its
 // nearest integer, so that far positions lose nothing, and its cosine and sine are
 // taken in 64 bits and rounded once to float32; the products are rounded one at
