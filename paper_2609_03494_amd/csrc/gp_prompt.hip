@@ -166,14 +166,17 @@ struct Split { int parts, per; };
 __device__ inline Split split_of(int seen, int rows, int share, int fine) {
     // (fine: pieces of few rows per share, of an item that is more than one; their parts cost little, and
     // finer ones even out the places: 64 requests of 1024-8143 tokens, one token each, 243 -> 234 us)
-    const int least = rows <= 32 ? kPromptLeastNarrow : kPromptLeastWide, limit = max(share, least);
-    const int piece = rows <= 32 ? max(share / fine, least) : limit;
-    Split x = {1, seen};
-    if (seen <= limit + limit / 4) return x;
     // Many rows: parts of up to an eighth more than a share, so that items a little longer than a whole number of
-    // shares do not start another round of pieces (512 tokens behind 16000: 16 items of 4.0 shares
-    // in 5 parts each 185 us, in 4 144).  In either case at most 1.8 seen / piece
-    const int parts = max((int)((float)seen / (float)piece * (rows <= 32 ? 1.0f : 8.0f / 9.0f)) + 1, 2);
+    // shares do not start another round of pieces (512 tokens behind 16000: 16 items of 4.0 shares in 5 parts
+    // each 185 us, in 4 144); and only items of more than 1.75 shares, since a workgroup that is left alone on its
+    // CU is faster and parts have to be joined (8-bit chunks behind 9000 and 15000: split from 1.25 on 525 us, now 435; a
+    // prompt of 2048 67.5 and 62).  In either case at most 1.8 seen / piece
+    const bool few = rows <= 32;
+    const int least = few ? kPromptLeastNarrow : kPromptLeastWide, limit = max(share, least);
+    const int piece = few ? max(share / fine, least) : limit;
+    Split x = {1, seen};
+    if (seen <= max(few ? limit + limit / 4 : share + share / 2 + share / 4, least + least / 4)) return x;
+    const int parts = max((int)((float)seen / (float)piece * (few ? 1.0f : 8.0f / 9.0f)) + 1, 2);
     x.per = ((int)((float)seen / (float)parts) + 64) & ~63;              // at least seen / parts
     x.parts = (int)((float)seen / (float)x.per);
     while (x.parts * x.per < seen) ++x.parts;
