@@ -155,8 +155,9 @@ __device__ inline Asked asked(const PromptArgs &a, int r) {
 // request, its cost the tokens that its last row sees (an item of up to 32 rows reads as many
 // bytes in the time that 128 rows take to multiply them); where items are fewer or longer than the
 // chip has places, an item's tokens are split into pieces of about the batch's share per place, each
-// with a partial result of its own.  Pieces go out longest first, sorted by cost in kBuckets
-// steps; their order within a step is whoever came first and has no bearing on any result.
+// with a partial result of its own.  Pieces go out longest first (of many items request by
+// request), sorted by cost in kBuckets steps; their order within a step is whoever came first and
+// has no bearing on any result.
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kBuckets = 256;
 
 // An item's pieces: `per` tokens each (a multiple of 64), the last one less.  Quotients by
@@ -188,6 +189,15 @@ __device__ inline int part_units(const PromptArgs &a, int rows) { return rows <=
 __device__ inline int share_of(unsigned long long cost, int slots) {
     const unsigned long long x = (cost + slots - 1) / slots;
     return x < INT_MAX / 2 ? (int)x : INT_MAX / 2;
+}
+
+__device__ inline int wave_sums(int x, int lane) {
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int y = __shfl_up(x, o, 64);
+        if (lane >= o) x += y;
+    }
+    return x;
 }
 
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PromptArgs a) {
@@ -240,24 +250,37 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PromptArgs a) {
     const float scale = (float)(kBuckets - 1) / (float)max(s_most, 1);
     // pass 1: pieces per bucket; 2: pieces to their places.  Few items all start at once: any order
     const bool sorted = s_items > a.slots / 2;
+    // Of many items a request's go out one after the other, longest first, requests by their longest: workgroups that run
+    // at the same time then read the same keys and values, from the XCD's L2 (60 prompts of 150 to 2330 tokens 1245 us,
+    // 1125 so; 12 of 200 to 6000 1147 and 1119; 8 chunks of 1024 behind 8192 1092 and 1067).  Of few, each by its own
+    // length: the last ones should be short (six prompts of 300 to 1900 tokens in float32: 207 us, request by request 245)
+    const bool grouped = s_items >= 3 * a.slots;
     for (int pass = sorted ? 1 : 2; pass < 3; ++pass) {
-        auto take = [&](int r, const Asked &q, int i) {
-            const int j0 = i * a.tokens, n = min(a.tokens, q.n - j0), seen = max(q.before + j0 + n, 0);
-            const Split x = split_of(seen, n << a.lg, share, a.fine);
-            const int bucket = sorted ? max(kBuckets - 1 - (int)((float)min(x.per, seen) * scale), 0) : 0;
-            if (pass == 1) {
-                atomicAdd(&s_hist[bucket], x.parts);
-                return;
+        auto item = [&](const Asked &q, int i, int &n, int &seen) {
+            n = min(a.tokens, q.n - i * a.tokens);
+            seen = max(q.before + i * a.tokens + n, 0);
+            return split_of(seen, n << a.lg, share, a.fine);
+        };
+        auto bucket = [&](int longest) { return sorted ? max(kBuckets - 1 - (int)((float)longest * scale), 0) : 0; };
+        // a request's step: by its longest piece (one of its last two items')
+        auto bucket_of = [&](const Asked &q, int items) {
+            int longest = 0;
+            for (int i = items - 1; i >= max(items - 2, 0); --i) {
+                int n, seen;
+                const Split x = item(q, i, n, seen);
+                longest = max(longest, min(x.per, seen));
             }
-            // (the bounds hold for any batch, see PromptWs)
+            return bucket(longest);
+        };
+        // item i to places `at` and on (the bounds hold for any batch, see PromptWs)
+        auto put = [&](int r, const Asked &q, int i, int n, int seen, const Split &x, int at) {
             int slot = -1;
-            const int units = part_units(a, n << a.lg);
+            const int units = part_units(a, n << a.lg), j0 = i * a.tokens;
             if (x.parts > 1) {
                 slot = atomicAdd(&s_slots, x.parts * units);
-                const int at = atomicAdd(&s_merges, 1);
-                if (at < a.max_merges) a.merges[at] = make_int4(slot, x.parts, q.ts + j0, n);
+                const int to = atomicAdd(&s_merges, 1);
+                if (to < a.max_merges) a.merges[to] = make_int4(slot, x.parts, q.ts + j0, n);
             }
-            int at = atomicAdd(&s_hist[bucket], x.parts);
             for (int p = 0; p < x.parts; ++p, ++at) {
                 if (at >= a.max_pieces) break;
                 a.pieces[2 * at] = make_int4(r, slot < 0 ? -1 : slot + p * units, p * x.per, min((p + 1) * x.per, seen));
@@ -272,15 +295,39 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PromptArgs a) {
             if (items > kFew) {
                 const int at = atomicAdd(&s_nmany, 1);
                 s_many[at] = r;
-            } else {
-                for (int i = 0; i < items; ++i) take(r, q, i);
+            } else if (items) {
+                int at = 0, n, seen;
+                if (grouped) {
+                    int all = 0;
+                    for (int i = 0; i < items; ++i) all += item(q, i, n, seen).parts;
+                    at = atomicAdd(&s_hist[bucket_of(q, items)], all);
+                }
+                for (int i = items - 1; i >= 0; --i) {
+                    const Split x = item(q, i, n, seen);
+                    if (!grouped) at = atomicAdd(&s_hist[bucket(min(x.per, seen))], x.parts);
+                    if (pass == 2) put(r, q, i, n, seen, x, at);
+                    at += x.parts;
+                }
             }
             __syncthreads();
             for (int k = wave; k < s_nmany; k += kPlanWaves) {
                 const int rr = uni(s_many[k]);
                 const Asked big = r0 == 0 ? s_asked[rr] : asked(a, rr);
-                const int count = (big.n + a.tokens - 1) / a.tokens;
-                for (int i = lane; i < count; i += 64) take(rr, big, i);
+                const int count = (big.n + a.tokens - 1) / a.tokens, of_all = grouped ? bucket_of(big, count) : 0;
+                for (int i0 = count - 1; i0 >= 0; i0 -= 64) {
+                    const int i = i0 - lane;
+                    int n = 0, seen = 0, at = 0;
+                    Split x = {0, 0};
+                    if (i >= 0) x = item(big, i, n, seen);
+                    if (grouped) {
+                        const int upto = wave_sums(x.parts, lane);
+                        if (lane == 63) at = atomicAdd(&s_hist[of_all], upto);
+                        at = __shfl(at, 63, 64) + upto - x.parts;
+                    } else if (i >= 0) {
+                        at = atomicAdd(&s_hist[bucket(min(x.per, seen))], x.parts);
+                    }
+                    if (pass == 2 && i >= 0) put(rr, big, i, n, seen, x, at);
+                }
             }
             __syncthreads();
             if (tid == 0) s_nmany = 0;
@@ -324,14 +371,6 @@ struct Piece {
     int ts, n, before;            // the item's first row of q and out, its tokens, those that precede them
 };
 struct Merge { int slot, parts, ts, n; };
-__device__ inline int wave_sums(int x, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const int y = __shfl_up(x, o, 64);
-        if (lane >= o) x += y;
-    }
-    return x;
-}
 template <bool MERGE, bool SEVERAL>
 __device__ inline typename std::conditional<MERGE, Merge, Piece>::type direct_place(const PromptArgs &a, int index, int lane) {
     Asked q = {};
