@@ -24,10 +24,10 @@
 // and no barrier, and the waves' results meet in LDS at the end.
 //
 // Bound (8 chunks of 1024 tokens behind 8192, 32/8 heads): the matrix unit and with it the chip's power at
-// head_dim 128, 1085 TFLOP/s in 1077 us, where a library's product of two 8192 x 8192 matrices
+// head_dim 128, 1097 TFLOP/s in 1067 us, where a library's product of two 8192 x 8192 matrices
 // reaches 1154; head_dim 64 has half of the products per weight and is bound by the vector instructions of
-// the softmax (16 exponentials of 16 cycles are half of them): 616 us, 948 TFLOP/s.  8-bit: each code is widened
-// once a workgroup, 1184 us and 987 TFLOP/s, 762 and 766.  float32: its matrix instructions' rate, 1063 us for a quarter
+// the softmax (16 exponentials of 16 cycles are half of them): 620 us, 940 TFLOP/s.  8-bit: each code is widened
+// once a workgroup, 1184 us and 987 TFLOP/s, 750 and 778.  float32: its matrix instructions' rate, 1063 us for a quarter
 // of it, 137 TFLOP/s of 153.  64 single tokens behind 1024 to 8143: the read of the cache, 5.1 TB/s.
 // Tried and slower: the sum of weights by the matrix unit as well (bf16, head_dim 64: 5 %), keys widened by two waves
 // and values by the others (8 bits, head_dim 64: 1 %), the merge by whoever ends an item last (5 tokens behind 6001:
