@@ -528,7 +528,8 @@ gp_status_t prompt_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, cons
     if (w.items * kv->num_kv_heads >= int64_t(1) << 23) return GP_ERR_UNSUPPORTED;     // (a grid below 2^32 threads)
     const int e = elem_bytes(kv->dtype);
     if (overlap(out, num_tokens * row, q, (num_tokens - 1) * q_stride + row, e)) return GP_ERR_INVALID;
-    if (ws_bytes < w.total) return GP_ERR_WORKSPACE;
+    // (a call without a list takes less, but the size asked for depends on the shape alone)
+    if (ws_bytes < prompt_ws(ps->num_reqs, num_tokens, num_q_heads, kv->num_kv_heads, kv->head_dim, false).total) return GP_ERR_WORKSPACE;
     unsigned char *base = static_cast<unsigned char *>(ws);
     a.slots = w.slots;
     a.fine = w.fine;
