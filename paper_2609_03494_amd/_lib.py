@@ -192,15 +192,16 @@ def _ptr(t: torch.Tensor | None) -> int | None:
 def _stream(stream) -> int:
     # (the current stream's handle alone: torch.cuda.current_stream() makes an object
     # around it, 2.8 us of a call of 10-14)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
+
+
+_DTYPES = {torch.float32: GP_F32, torch.bfloat16: GP_BF16}
 
 
 def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
-        return GP_F32
-    if t.dtype == torch.bfloat16:
-        return GP_BF16
-    raise ValueError(f"unsupported dtype {t.dtype}")
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"unsupported dtype {t.dtype}")
+    return _DTYPES[t.dtype]
 
 
 @dataclass
@@ -210,8 +211,14 @@ class KVLayer:
     v: torch.Tensor
 
     def c(self) -> _KVLayer:
-        pool, hkv, b, d = self.k.shape
-        return _KVLayer(_ptr(self.k), _ptr(self.v), pool, hkv, b, d, _dtype_code(self.k))
+        k, v = self.k, self.v
+        shape, code = k.shape, _DTYPES.get(k.dtype)
+        if code is None:
+            raise ValueError(f"unsupported dtype {k.dtype}")
+        if v.shape != shape or v.dtype != k.dtype:
+            raise ValueError("pools: two tensors of one shape and type")
+        pool, hkv, b, d = shape
+        return _KVLayer(_ptr(k), _ptr(v), pool, hkv, b, d, code)
 
 
 _CODES = (torch.float8_e4m3fn, torch.uint8)

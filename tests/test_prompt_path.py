@@ -204,6 +204,11 @@ def test_binding_refusals():
         gp.gp_pages_release(ps, torch.zeros(3, dtype=torch.int64))
     with pytest.raises(ValueError):
         gp.gp_pages_reserve(ps, i32(4), torch.zeros(4))
+    for v in (k[:99], k.float(), k[:, :1]):                             # pools of two shapes or types
+        with pytest.raises(ValueError, match="one shape"):
+            gp.KVLayer(k, v).c()
+        with pytest.raises(ValueError, match="one shape"):
+            gp.Layers([layer, gp.KVLayer(k, v)])
     with pytest.raises(ValueError):                                     # not on a GPU
         gp.gp_pages_reserve(ps, i32(4), i32(4))
     with pytest.raises(ValueError):
