@@ -38,17 +38,12 @@ constexpr int kMaxPrefixSlotPages = 128;  // and at most (LDS id table)
 constexpr int kMaxDecodePages = 8192;     // table width the decode calls accept
 constexpr float kQ8KeyScale = 65536.0f;   // codes of 8-bit keys in units of their bfloat16 operands (see Page<E4m3>)
 constexpr int kPromptRows = 128;          // (token, query head) rows of a prompt attention item
-#ifndef GP_PROMPT_SLOTS
-#define GP_PROMPT_SLOTS 512
-#endif
-constexpr int kPromptSlots = GP_PROMPT_SLOTS;   // pieces of a small prompt attention call, all KV heads, about
-#ifndef GP_PROMPT_NARROW
-#define GP_PROMPT_NARROW 256
-#endif
-#ifndef GP_PROMPT_WIDE
-#define GP_PROMPT_WIDE 512
-#endif
-constexpr int kPromptLeastNarrow = GP_PROMPT_NARROW, kPromptLeastWide = GP_PROMPT_WIDE;   // tokens of a split item's piece at least
+// Pieces of a small prompt attention call over all KV heads, about: two workgroups a CU (512 tokens behind 16000 145 us,
+// with 384 or 256 of them 165; 768: a mixed step 304 -> 312, five tokens of 64 requests 291 -> 325).
+constexpr int kPromptSlots = 512;
+// Tokens of a split item's piece at least, of up to 32 rows and of more (128: 5 tokens behind 6001 14.5 -> 19.6 us, 384:
+// one token behind 1500 13.1 -> 14.1; 256: a prompt of 1000 32.4 -> 37.6, 768: 34.0, in float32 119 -> 137).
+constexpr int kPromptLeastNarrow = 256, kPromptLeastWide = 512;
 constexpr int kMaxRopeTokens = 1 << 27;   // tokens one gp_append_rope call takes, and
 constexpr int kMaxListedHeads = 8192;     // KV heads it, the page bounds and the selection take: grids below 2^32 threads
 constexpr size_t kScratchBytes = size_t(8) << 20;   // static scratch of gp_decode_attention_noalloc
@@ -188,9 +183,9 @@ __host__ __device__ inline size_t select_ws(int R, int Hkv, int max_pages) {
 }
 
 // Division of a prompt attention call (see plan_kernel).  An item has kPromptRows / G
-// new tokens; pieces of a split item cost no less than the batch's share per slot (of up to 32
-// rows: 1 / fine of it), and an item is split only where it is a quarter more than that: all
-// split items together have at most 1.8 slots pieces of many rows, or fine times as many of few.
+// new tokens; pieces of a split item cost no less than 8/9 of the batch's share per slot (of up to 32
+// rows: 1 / fine of it), and an item is split only where it is a quarter more than a share, or longer
+// (see split_of): all split items together have at most 1.8 slots pieces of many rows, or fine times as many of few.
 struct PromptWs {
     size_t counts, pieces, merges, partial, total;
     int64_t items;
