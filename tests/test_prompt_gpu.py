@@ -426,3 +426,15 @@ def test_prompt_scales_at_the_ends_of_their_range():
     torch.cuda.synchronize()
     # token 7 is ahead by 1000 * 1.6e38 * 2^-126 = 1880
     assert torch.equal(c.out.double(), V[7].expand(9, 2, 64))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "q8"])
+def test_prompt_requests_kept_together(kind):
+    """Items enough for pieces to go out request by request: prompts, a chunk, one long context that is split, short ones."""
+    _say(f"together {kind}")
+    reqs = [(3000, 270, 1300), (60000, 3760, 1), (0, 90, 1400), (9000, 600, 500), (100, 10, 3), (0, 1, 0), (-30, 4, 20), (7000, 440, 33), (40, 3, 60)]
+    for advanced in (False, True):
+        c = Case(kind, reqs, 64, 8, 64, 3, advanced)
+        c.call()
+        torch.cuda.synchronize()
+        c.check("together")
