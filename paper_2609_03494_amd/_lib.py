@@ -264,7 +264,8 @@ class Layers:
 
 @dataclass
 class PageState:
-    """Device page state (int32 tensors).  free_count is a one-element tensor."""
+    """Device page state (int32 tensors).  free_count is a one-element tensor.  free_list and
+    free_count may be None where a call does not look at the free stack."""
     page_table: torch.Tensor   # [R, max_pages]
     num_pages: torch.Tensor    # [R]
     seq_lens: torch.Tensor     # [R]
@@ -275,11 +276,13 @@ class PageState:
     def c(self) -> _PageState:
         table, pages, lens, refs, stack, height = (self.page_table, self.num_pages, self.seq_lens, self.refcount,
                                                    self.free_list, self.free_count)
+        R, maxp = table.shape
+        if pages is None or lens is None or stack is None or height is None:
+            return _PageState(*map(_ptr, (table, pages, lens, refs, stack, height)), R, maxp, refs.shape[0])
         # (one test and six pointers here: six calls of _ptr were 0.6 us of a call of 12)
         if not (table.is_contiguous() and pages.is_contiguous() and lens.is_contiguous() and refs.is_contiguous() and
                 stack.is_contiguous() and height.is_contiguous()):
             raise ValueError("tensors passed to the library must be contiguous")
-        R, maxp = table.shape
         return _PageState(table.data_ptr(), pages.data_ptr(), lens.data_ptr(), refs.data_ptr(), stack.data_ptr(),
                           height.data_ptr(), R, maxp, refs.shape[0])
 
@@ -691,6 +694,8 @@ def gp_decode_attention_pages_q8(kv: KV8Layer, ps: PageState, selected: torch.Te
 
 def _pages(name: str, ps: PageState, **tensors) -> _PageState:
     c_ps = ps.c()
+    if ps.free_list is None or ps.free_count is None:
+        raise ValueError(f"{name}: a state with free_list and free_count")
     for key, t in tensors.items():
         if t is not None and t.dtype != torch.int32:
             raise ValueError(f"{name}: {key} int32")
