@@ -246,7 +246,8 @@ class KV8Layer:
 
 class Layers:
     """The layers of one cache (KVLayer or KV8Layer, all of one kind) as the calls over several take
-    them, made once: a program keeps it beside the pools, whose tensors it holds."""
+    them, made once: a program keeps it beside the pools, whose tensors it holds.  A layer that gets
+    other tensors later wants a new Layers."""
 
     def __init__(self, layers):
         self.layers = list(layers)
@@ -255,7 +256,8 @@ class Layers:
             raise ValueError("Layers: one or more KVLayer, or KV8Layer")
         self.q8 = kinds == {KV8Layer}
         self._c = ((_KV8Layer if self.q8 else _KVLayer) * len(self.layers))(*[layer.c() for layer in self.layers])
-        devices = {t.get_device() for layer in self.layers for t in vars(layer).values()}
+        self._tensors = [t for layer in self.layers for t in vars(layer).values()]     # as they were when _c took their pointers
+        devices = {t.get_device() for t in self._tensors}
         self._device = devices.pop() if len(devices) == 1 else -1
 
     def __len__(self) -> int:

@@ -2,6 +2,8 @@
 import ctypes
 import gc
 import weakref
+import gc
+import weakref
 
 import pytest
 import torch
@@ -51,3 +53,18 @@ def test_state_without_lengths_is_the_library_s_to_refuse(lib):  # noqa: F811
         c = _state(**{key: None}).c()
         assert getattr(c, key) is None
         assert lib.gp_pages_release(ctypes.byref(c), 0x1000, 1, None) == 1
+
+
+def test_layers_hold_the_tensors_that_they_point_to():
+    """A layer whose pool is replaced later: the handle keeps the one that it was made of."""
+    pool = lambda dt=torch.float32: torch.zeros(6, 2, 16, 64).to(dt)  # noqa: E731
+    layer, layer8 = gp.KVLayer(pool(), pool()), gp.KV8Layer(pool(torch.uint8), pool(torch.uint8), torch.ones(6, 2), torch.ones(6, 2))
+    for x in (layer, layer8):
+        handle = gp.Layers([x])
+        old = {name: weakref.ref(t) for name, t in vars(x).items()}
+        at = {name: t.data_ptr() for name, t in vars(x).items()}
+        for name, t in list(vars(x).items()):
+            setattr(x, name, torch.ones_like(t))
+        gc.collect()
+        for name, t in old.items():
+            assert t() is not None and t().data_ptr() == getattr(handle._c[0], name) == at[name], name
