@@ -536,6 +536,7 @@ gp_status_t prompt_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, cons
     a.max_pieces = w.max_pieces;
     a.max_merges = w.max_merges;
     a.part_rows = w.part_rows;
+    a.units = w.units;
     a.counts = reinterpret_cast<int32_t *>(base + w.counts);
     a.pieces = reinterpret_cast<int4 *>(base + w.pieces);
     a.merges = reinterpret_cast<int4 *>(base + w.merges);

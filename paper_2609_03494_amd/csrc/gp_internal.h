@@ -4,8 +4,11 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <stdint.h>
 #include <stddef.h>
+
+#include <algorithm>
 
 #include "growpage.h"
 
@@ -182,14 +185,50 @@ __host__ __device__ inline size_t select_ws(int R, int Hkv, int max_pages) {
     return align_up((size_t)R * Hkv * max_pages * sizeof(float) + 64);
 }
 
-// Division of a prompt attention call (see plan_kernel).  An item has kPromptRows / G
-// new tokens; pieces of a split item cost no less than 8/9 of the batch's share per slot (of up to 32
-// rows: 1 / fine of it), and an item is split only where it is a quarter more than a share, or longer
-// (see split_of): all split items together have at most 1.8 slots pieces of many rows, or fine times as many of few.
+// An item's pieces: `per` tokens each (a multiple of 64), the last one less.  Quotients by
+// reciprocals, put right where they have to be exact: integer divisions were most of this
+// kernel's time.
+struct Split { int parts, per; };
+__host__ __device__ inline Split split_of(int seen, int rows, int share, int fine) {
+    // (fine: pieces of few rows per share, of an item that is more than one; their parts cost little, and
+    // finer ones even out the places: 64 requests of 1024-8143 tokens, one token each, 243 -> 234 us)
+    // Many rows: parts of up to an eighth more than a share, so that items a little longer than a whole number of
+    // shares do not start another round of pieces (512 tokens behind 16000: 16 items of 4.0 shares in 5 parts
+    // each 185 us, in 4 144); and only items of more than 1.75 shares, since a workgroup that is left alone on its
+    // CU is faster and parts have to be joined (8-bit chunks behind 9000 and 15000: split from 1.25 on 525 us, now 435; a
+    // prompt of 2048 67.5 and 62)
+    const bool few = rows <= 32;
+    const int least = few ? kPromptLeastNarrow : kPromptLeastWide, limit = std::max(share, least);
+    const int piece = few ? std::max(share / fine, least) : limit;
+    Split x = {1, seen};
+    if (seen <= std::max(few ? limit + limit / 4 : share + share / 2 + share / 4, least + least / 4)) return x;
+    const int parts = std::max((int)((float)seen / (float)piece * (few ? 1.0f : 8.0f / 9.0f)) + 1, 2);
+    x.per = ((int)((float)seen / (float)parts) + 64) & ~63;              // at least seen / parts
+    x.parts = (int)((float)seen / (float)x.per);
+    while (x.parts * x.per < seen) ++x.parts;
+    while (x.parts > 1 && (x.parts - 1) * x.per >= seen) --x.parts;
+    return x;
+}
+// The batch's cost over the places that it is divided into.
+__host__ __device__ inline int share_of(unsigned long long cost, int slots) {
+    const unsigned long long x = (cost + slots - 1) / slots;
+    return x < INT_MAX / 2 ? (int)x : INT_MAX / 2;
+}
+
+// Room for the pieces of a prompt attention call (see plan_kernel).  An item has kPromptRows / G new tokens, its
+// cost is the tokens that its last row sees, a share the batch's cost over `slots`.  Parts of split items, by
+// split_of:
+//  - few rows: only where seen > 1.25 max(share, least), into at most seen / piece + 1 parts, piece =
+//    max(share / fine, least); so at most 1.8 seen / piece of them, and 1.8 fine slots over the batch.
+//  - many rows: only where seen > max(1.75 share, 1.25 least), into at most 8/9 seen / max(share, least) + 1; so at most
+//    1.7 seen / share of them, and 1.7 slots over the batch.
+// Rounding a piece to 64 tokens makes fewer parts.  A split item has two parts or more: half as many of them.  `parts` has 2 slots
+// + 2 for 1.8 slots, which also covers share / fine cut to a whole number.  A part takes 1 unit of the workspace (few rows) or
+// part_rows / 32.
 struct PromptWs {
     size_t counts, pieces, merges, partial, total;
     int64_t items;
-    int slots, fine, max_pieces, max_merges, part_rows;
+    int slots, fine, max_pieces, max_merges, part_rows, units;
 };
 __host__ __device__ inline PromptWs prompt_ws(int R, int64_t T, int Hq, int Hkv, int D, bool direct) {
     PromptWs w;
@@ -201,7 +240,7 @@ __host__ __device__ inline PromptWs prompt_ws(int R, int64_t T, int Hq, int Hkv,
     w.max_pieces = (int)w.items + parts * w.fine;
     w.max_merges = (int)(w.items < parts * w.fine / 2 ? w.items : parts * w.fine / 2);
     w.part_rows = T * G < kPromptRows ? (int)(T * G + 31) / 32 * 32 : kPromptRows;
-    const int units = w.part_rows / 32 > w.fine ? w.part_rows / 32 : w.fine;
+    w.units = parts * (w.part_rows / 32 > w.fine ? w.part_rows / 32 : w.fine);
     size_t off = 0;
     w.counts = off;
     off += kAlign;
@@ -210,7 +249,7 @@ __host__ __device__ inline PromptWs prompt_ws(int R, int64_t T, int Hq, int Hkv,
     w.merges = off;
     off = align_up(off + (size_t)w.max_merges * 16);
     w.partial = off;    // float: [unit][Hkv][32][D + 2]
-    off = align_up(off + (size_t)parts * units * Hkv * 32 * (D + 2) * sizeof(float));
+    off = align_up(off + (size_t)w.units * Hkv * 32 * (D + 2) * sizeof(float));
     w.total = off;
     return w;
 }
@@ -377,6 +416,7 @@ struct PromptArgs {
     int slots;                        // pieces that the batch is divided into where items alone are fewer, about
     int fine;                         // pieces of up to 32 rows are so much smaller
     int max_pieces, max_merges, part_rows;   // pieces and split items of one KV head at most; rows of a partial of more than 32
+    int units;                        // units of 32 rows that the partials have room for
     float qscale;                     // scale * log2(e); 8-bit: times kQ8KeyScale
     float lag;                        // 8 / qscale
     // workspace regions (PromptWs)

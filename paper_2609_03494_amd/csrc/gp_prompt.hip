@@ -160,36 +160,8 @@ __device__ inline Asked asked(const PromptArgs &a, int r) {
 // has no bearing on any result.
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64, kBuckets = 256;
 
-// An item's pieces: `per` tokens each (a multiple of 64), the last one less.  Quotients by
-// reciprocals, put right where they have to be exact: integer divisions were most of this
-// kernel's time.
-struct Split { int parts, per; };
-__device__ inline Split split_of(int seen, int rows, int share, int fine) {
-    // (fine: pieces of few rows per share, of an item that is more than one; their parts cost little, and
-    // finer ones even out the places: 64 requests of 1024-8143 tokens, one token each, 243 -> 234 us)
-    // Many rows: parts of up to an eighth more than a share, so that items a little longer than a whole number of
-    // shares do not start another round of pieces (512 tokens behind 16000: 16 items of 4.0 shares in 5 parts
-    // each 185 us, in 4 144); and only items of more than 1.75 shares, since a workgroup that is left alone on its
-    // CU is faster and parts have to be joined (8-bit chunks behind 9000 and 15000: split from 1.25 on 525 us, now 435; a
-    // prompt of 2048 67.5 and 62).  In either case at most 1.8 seen / piece
-    const bool few = rows <= 32;
-    const int least = few ? kPromptLeastNarrow : kPromptLeastWide, limit = max(share, least);
-    const int piece = few ? max(share / fine, least) : limit;
-    Split x = {1, seen};
-    if (seen <= max(few ? limit + limit / 4 : share + share / 2 + share / 4, least + least / 4)) return x;
-    const int parts = max((int)((float)seen / (float)piece * (few ? 1.0f : 8.0f / 9.0f)) + 1, 2);
-    x.per = ((int)((float)seen / (float)parts) + 64) & ~63;              // at least seen / parts
-    x.parts = (int)((float)seen / (float)x.per);
-    while (x.parts * x.per < seen) ++x.parts;
-    while (x.parts > 1 && (x.parts - 1) * x.per >= seen) --x.parts;
-    return x;
-}
 // What a part takes of the workspace, in units of 32 rows.
 __device__ inline int part_units(const PromptArgs &a, int rows) { return rows <= 32 ? 1 : a.part_rows / 32; }
-__device__ inline int share_of(unsigned long long cost, int slots) {
-    const unsigned long long x = (cost + slots - 1) / slots;
-    return x < INT_MAX / 2 ? (int)x : INT_MAX / 2;
-}
 
 __device__ inline int wave_sums(int x, int lane) {
 #pragma unroll
@@ -971,6 +943,7 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
             }
     } else {
         const int units = part_units(a, rows), part_rows = 32 * units;
+        if (slot + units > a.units) return;                          // (no batch asks for more, see prompt_ws)
         float *to = a.partial + ((size_t)slot * a.Hkv + (size_t)h * units) * 32 * (D + 2);
 #pragma unroll
         for (int d = 0; d < DB; ++d)
@@ -1008,6 +981,7 @@ __global__ __launch_bounds__(256) void merge_kernel(PromptArgs a) {
     }
     const int rows = x.n << a.lg;
     const int u = threadIdx.x % LANES, parts = uni(x.parts);
+    if (x.slot + parts * part_units(a, rows) > a.units) return;
     for (int row = block * RPW + threadIdx.x / LANES; row < min(rows, (block + 1) * RPW); row += ROWS) {
         const int units = part_units(a, rows), part_rows = 32 * units;
         const size_t stride = (size_t)a.Hkv * part_rows * (D + 2);
