@@ -92,9 +92,9 @@ __device__ inline uint32_t pack_bf16(float a, float b) {             // to neare
 // 16 bytes a lane from base + off to LDS, `to` + 16 lane, past the registers.  Written as
 // assembly since the compiler makes every LDS read wait for all such loads in flight,
 // those into the other stage included; here the wave waits for them (wait_loads) before
-// the barrier that hands the stage over.  No register is written.
+// the barrier that hands the stage over.  No vector register is written; m0, the place in LDS, is.
 __device__ inline void load_lds(const void *base, uint32_t off, uint32_t to) {
-    __asm__ volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(to) : "memory");
+    __asm__ volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(to) : "m0", "memory");
 }
 __device__ inline uint32_t lds_addr(const void *p) {
     return (uint32_t)(size_t)(__attribute__((address_space(3))) const char *)p;
