@@ -660,7 +660,8 @@ gp_status_t gp_decode_attention_q8(const gp_kv8_layer_t *kv, const gp_page_state
  *  - A held request is left out: its rows of out are not written, nor are rows that
  *    belong to no request.  A row whose weights have no positive sum gets zeros, as in
  *    gp_decode_attention.  Tokens that a row does not see are never used, whatever
- *    they hold, infinities and NaN included.
+ *    they hold, infinities and NaN included.  Where a row with weights sees a value that is
+ *    infinite or NaN, its output in that dim is infinite or NaN, at any weight.
  *  - float32 sums and statistics; of a bfloat16 or 8-bit cache the weights are
  *    rounded to bfloat16 for their product with the values, and a weight below 2^-118
  *    of the row's largest may count as zero.  The scale is below 2^127 (GP_ERR_INVALID).

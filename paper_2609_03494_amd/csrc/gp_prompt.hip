@@ -573,7 +573,8 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
         }
         *reinterpret_cast<u32x4_t *>(to) = x;
     };
-    // ... and the rows that see such a token take them in from the pool: the result is infinite or NaN at any weight
+    // ... and the rows that see such a token take them in from the pool: the result is infinite or NaN at any weight, as
+    // where a weight of zero meets them in the product, and stays so wherever outputs are scaled by zero
     auto add_odd = [&](int blk, uint32_t odd) __attribute__((always_inline)) {
         for (; odd; odd &= odd - 1) {
             const int t = __builtin_ctz(odd);
@@ -914,7 +915,7 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
                 for (int w = 0; w < NW; ++w) {
                     const f32x4_t x = reinterpret_cast<const f32x4_t *>(s_o + w * 32 * D)[unit_of(col, 8 * d + 2 * i + half)];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) y[c] += f[w] == 0.0f ? 0.0f : x[c] * f[w];
+                    for (int c = 0; c < 4; ++c) y[c] += x[c] * f[w];
                 }
 #pragma unroll
                 for (int c = 0; c < 4; ++c) o[d][4 * i + c] = y[c];
@@ -1009,13 +1010,13 @@ __global__ __launch_bounds__(256) void merge_kernel(PromptArgs a) {
             const float f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - up);
             l *= f;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) o[c] = f == 0.0f ? 0.0f : o[c] * f;
+            for (int c = 0; c < 4; ++c) o[c] *= f;
 #pragma unroll
             for (int k = 0; k < BATCH; ++k) {
                 const float g = mk[k] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(mk[k] - up);
                 l += lk[k] * g;                           // (a sum that is NaN stays so)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) o[c] += g == 0.0f ? 0.0f : ok[k][c] * g;
+                for (int c = 0; c < 4; ++c) o[c] += ok[k][c] * g;
             }
             m = up;
         }
