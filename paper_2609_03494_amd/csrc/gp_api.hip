@@ -559,7 +559,7 @@ gp_status_t prompt_call(const gp_kv_layer_t *kv, const gp_kv8_layer_t *kv8, cons
     a.pool_pages = kv->pool_pages;
     a.advanced = advanced != 0;
     a.qscale = scale * 1.4426950408889634f * (kv8 ? kQ8KeyScale : 1.0f);
-    a.lag = 8.0f / a.qscale;
+    a.lag = std::min(8.0f / a.qscale, FLT_MAX);      // (infinite, it made NaN of a maximum of -inf)
     return from_hip(launch_prompt(kv8 ? 1 : e, kv->head_dim, a, stream));
 }
 

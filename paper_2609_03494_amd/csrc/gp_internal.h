@@ -418,7 +418,7 @@ struct PromptArgs {
     int max_pieces, max_merges, part_rows;   // pieces and split items of one KV head at most; rows of a partial of more than 32
     int units;                        // units of 32 rows that the partials have room for
     float qscale;                     // scale * log2(e); 8-bit: times kQ8KeyScale
-    float lag;                        // 8 / qscale
+    float lag;                        // 8 / qscale, finite
     // workspace regions (PromptWs)
     int32_t *counts;                  // pieces, split items
     int4 *pieces;                     // [max_pieces][2]: see Piece

@@ -63,3 +63,23 @@ def test_seen_values_that_are_not_finite(kind, hq, hkv, d):
                 assert not bool(got[first:, h * G:, dim].isfinite().any()), (others, dim)
                 assert torch.equal(got[:first, h * G:, dim], want[:first, h * G:, dim])
             assert torch.equal(got[:, h * G:, rest], want[:, h * G:, rest])
+@pytest.mark.parametrize("m,P,n", [(200, 13, 1), (700, 45, 1), (3, 14, 200)])
+def test_scales_of_which_the_lag_is_no_number(m, P, n):
+    """A scale so small that 2^8 of its units is past float32, and blocks in which one head's scores are all -inf, another's
+    not: the mean of the values that have weights."""
+    _say(f"lag {n} tokens behind {m}")
+    c = Case("f32", [(m, P, n)], 2, 1, 64, 3)
+    c.scale = 1e-39
+    total = m + n
+    V = c.tokens(1, 0, total)[0]
+    pages, slots = c.table[0, torch.arange(total) // 16].long(), torch.arange(total) % 16
+    c.kv.k[pages, 0, slots, 0] = torch.where(torch.arange(total) < 32, -1e30, 0.0).to(c.kv.k)
+    c.q[:, 0, 0], c.q[:, 1, 0] = 1e30, 0.0
+    c.call()
+    torch.cuda.synchronize()
+    for j in range(n):
+        sees = m + j + 1
+        for g, first in ((0, 32), (1, 0)):
+            want = V[first:sees].mean(0) if sees > first else torch.zeros_like(V[0])
+            # the sums of weights next to one: a step of 2^-24 for each token, twice, and the quotient's
+            assert bool(((c.out[j, g].double() - want).abs() <= V.abs().amax() * (2 * sees + 2) * 2.0 ** -24).all()), (j, g)
