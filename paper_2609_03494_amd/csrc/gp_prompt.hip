@@ -439,6 +439,10 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
     const float unit = CACHE == 1 ? 1.0f : a.qscale;                 // maxima to units of log2 (8-bit: in them already)
     const float lag = CACHE == 1 ? 8.0f : a.lag, offset = CACHE == 1 ? 8.0f : 0.0f;
     float m = kNegInf, l = 0.0f, above = kNegInf, from = 0.0f;       // above: the score that moves the maximum
+    // the factor from one maximum to another (halves: the difference of two scores may be past float32, and come back by the unit)
+    auto fall = [&](float of, float to) __attribute__((always_inline)) {
+        return of == kNegInf ? 0.0f : __builtin_amdgcn_exp2f((0.5f * of - 0.5f * to) * unit * 2.0f);
+    };
 
     // S^T of the 32 tokens whose keys lie at kb
     auto scores = [&](f32x16_t &st, const unsigned char *kb) __attribute__((always_inline)) {
@@ -478,7 +482,7 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
         }
         const float top = max_halves(fmaxf(t[0], t[1]));
         if (__any(top > above)) {
-            const float up = fmaxf(m, top), f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f((m - up) * unit);
+            const float up = fmaxf(m, top), f = fall(m, up);
             l *= f;
 #pragma unroll
             for (int d = 0; d < DB; ++d)
@@ -901,7 +905,7 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             const float mw = s_ml[0][w][col], lw = s_ml[1][w][col];
-            f[w] = mw == kNegInf ? 0.0f : __builtin_amdgcn_exp2f((mw - mx) * unit);
+            f[w] = fall(mw, mx);
             sum += lw * f[w];                                        // (no weight: lw is 0, or NaN, which stays)
         }
         // wave w finishes a share of the units

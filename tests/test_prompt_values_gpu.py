@@ -1,6 +1,8 @@
 """Prompt attention where one form of the division could give other results than another."""
 from __future__ import annotations
 
+import math
+
 import pytest
 import torch
 
@@ -83,3 +85,27 @@ def test_scales_of_which_the_lag_is_no_number(m, P, n):
             want = V[first:sees].mean(0) if sees > first else torch.zeros_like(V[0])
             # the sums of weights next to one: a step of 2^-24 for each token, twice, and the quotient's
             assert bool(((c.out[j, g].double() - want).abs() <= V.abs().amax() * (2 * sees + 2) * 2.0 ** -24).all()), (j, g)
+
+
+@pytest.mark.parametrize("m,P,n", [(200, 13, 1), (40, 3, 1), (3, 14, 200)])
+def test_scores_further_apart_than_float32_reaches(m, P, n):
+    """Scores of -3e38 and, from token 32 on, 3e38 under a scale that brings them next to each other."""
+    _say(f"far scores, {n} tokens behind {m}")
+    c = Case("f32", [(m, P, n)], 1, 1, 64, 3)
+    c.scale = 1e-38
+    total = m + n
+    V = c.tokens(1, 0, total)[0]
+    t = torch.arange(total)
+    c.kv.k[c.table[0, t // 16].long(), 0, t % 16] = 0.0
+    c.kv.k[c.table[0, t // 16].long(), 0, t % 16, 0] = torch.where(t < 32, -3e19, 3e19).to(c.kv.k)
+    c.q[:, :, 0] = 1e19
+    c.call()
+    torch.cuda.synchronize()
+    w = torch.where(t < 32, math.exp(-3.0), math.exp(3.0)).double().to(V)
+    for j in range(n):
+        sees = m + j + 1
+        want = (w[:sees, None] * V[:sees]).sum(0) / w[:sees].sum()
+        # the weights by the rounding of the scale (a denormal number of 23 bits and fewer: 2^-20), of scores of 4.4
+        # in log2 and of the exponential, twice, and the sums' steps
+        tol = V.abs().amax() * (2 * 3.0 * (2.0 ** -20 + 3 * 2.0 ** -23) + 2.0 ** -21 + (2 * sees + 2) * 2.0 ** -24)
+        assert bool(((c.out[j, 0].double() - want).abs() <= tol).all()), j
