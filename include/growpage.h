@@ -662,9 +662,12 @@ gp_status_t gp_decode_attention_q8(const gp_kv8_layer_t *kv, const gp_page_state
  *    gp_decode_attention.  Tokens that a row does not see are never used, whatever
  *    they hold, infinities and NaN included.  Where a row with weights sees a value that is
  *    infinite or NaN, its output in that dim is infinite or NaN, at any weight.
- *  - float32 sums and statistics; of a bfloat16 or 8-bit cache the weights are
- *    rounded to bfloat16 for their product with the values, and a weight below 2^-118
- *    of the row's largest may count as zero.  The scale is below 2^127 (GP_ERR_INVALID).
+ *  - float32 sums and statistics.  A request's tokens are taken 128 / G at a time (G query
+ *    heads per KV head).  Of a bfloat16 or 8-bit cache the weights (8-bit: times the values'
+ *    scales) of a run of more than 32 / G tokens are rounded to bfloat16 for their product
+ *    with the values; those of shorter runs, single and drafted tokens among them, are
+ *    split into two bfloat16 terms, as in gp_decode_attention.  A weight below 2^-118 of the
+ *    row's largest may count as zero.  The scale is below 2^127 (GP_ERR_INVALID).
  *    8-bit: q and out bfloat16, the scale as in gp_decode_attention_q8.
  * q: rows of q_stride elements, [num_q_heads][head_dim] contiguous; out [num_tokens]
  * [num_q_heads][head_dim], which may not overlap q (GP_ERR_INVALID).  Pools at multiples

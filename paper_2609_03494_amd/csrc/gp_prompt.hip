@@ -14,8 +14,13 @@
 // h has tokens 8 k + 4 h + 0..3 of every 16, and V^T is read in that order (16 bits: by
 // transposing LDS reads).  Softmax in one pass, weights in units of log2; the maximum may
 // lag behind by 2^8, so that O^T is rescaled in few blocks.  Scores, statistics and outputs are
-// float32; the weights of 16- and 8-bit caches are rounded to bfloat16 for the second product, the
-// only form in which the matrix instruction takes them (half a step is 2^-8 of a weight).
+// float32.  The weights (of 8 bits: times the values' scales) go to the second product of 16- and 8-bit caches as bfloat16, the
+// only form in which the matrix instruction takes them beside such values.  Items of up to 32 rows have them in two terms, as
+// the decode step does (2^-16 of a weight at most): they wait for the cache, and 64 single tokens take 235 us with one
+// term or two, five behind 6001 15.0 (60 single tokens of 8 heads per KV head at d 64, where little is read: 127.2 and 128.3).  Items of
+// more rows have one (half a step, 2^-8 of a weight): three products for two cost them a third and more (8 chunks of 1024 behind
+// 8192, below: 1072 and 1469 us, d 64 636 and 880, 8 bits 1197 and 1605), for a relative error (2-norm, random values) of
+// 0.00166 in place of 0.00183, where the output's own rounding is 0.00166.
 //
 // Two paths, by an item's rows.  More than 32 (wide): the four waves share the blocks, and a wave works
 // on the scores of block b + 1 and the weights of block b at once, independent work for the
@@ -506,8 +511,8 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
             for (int i = 0; i < 16; ++i) st[i] *= vs[i / 8];
         }
     };
-    // O^T += V^T P^T
-    auto values = [&](const f32x16_t &st, const unsigned char *vb) __attribute__((always_inline)) {
+    // O^T += V^T P^T; two: the weights in two bfloat16 terms
+    auto values = [&](const f32x16_t &st, const unsigned char *vb, auto two) __attribute__((always_inline)) {
         if constexpr (CACHE == 4) {
 #pragma unroll
             for (int d = 0; d < DB; ++d)
@@ -524,17 +529,22 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
             typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                u32x4_t p;
+                u32x4_t p, rest;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) p[c] = pack_bf16(st[8 * k + 2 * c], st[8 * k + 2 * c + 1]);
+                for (int c = 0; c < 4; ++c) {
+                    const float w0 = st[8 * k + 2 * c], w1 = st[8 * k + 2 * c + 1];
+                    p[c] = pack_bf16(w0, w1);
+                    if constexpr (two) rest[c] = pack_bf16(w0 - __uint_as_float(p[c] << 16), w1 - __uint_as_float(p[c] & 0xffff0000u));   // (exact before it is rounded)
+                }
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     // (units 4 d of a token: the swizzle flips units of 4, which 4 d xors with)
                     const unsigned char *x = vb + (v0 ^ (uint32_t)(d << 6)) + k * 16 * TL::ROWB;
                     const u32x2_t y0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)x));
                     const u32x2_t y1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(x + 8 * TL::ROWB)));
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, u32x4_t{y0[0], y0[1], y1[0], y1[1]}),
-                                                                   __builtin_bit_cast(bf16x8_t, p), o[d], 0, 0, 0);
+                    const bf16x8_t v = __builtin_bit_cast(bf16x8_t, u32x4_t{y0[0], y0[1], y1[0], y1[1]});
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8_t, p), o[d], 0, 0, 0);
+                    if constexpr (two) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8_t, rest), o[d], 0, 0, 0);
                 }
             }
         }
@@ -744,7 +754,7 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
             fetch(b, i);
             scores(nx, s_k + place(i + 1));
             weigh(st, ks, vs);
-            values(st, s_v + place(i));
+            values(st, s_v + place(i), std::false_type{});
             settle_scores(nx, (b + 1) * 32, kn, false);
             arrive(b, i);
             __syncthreads();
@@ -757,7 +767,7 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
             if (tid == 0) s_odd[(b + 2) & 3] = 0;
             if (mine) {
                 weigh(st, ks, vs);
-                values(st, s_v + place(i));
+                values(st, s_v + place(i), std::false_type{});
                 if ((b + 1) * 32 > border) {
                     const uint32_t odd = uni(s_odd[b & 3]);
                     if (odd) add_odd(b, odd);
@@ -872,7 +882,7 @@ __global__ __launch_bounds__(kThreads, CACHE != 4 && D == 64 ? 3 : 2) void promp
             }
             if (border)
                 for (int i = 0; i < NL; ++i) clean(s_v + i * 1024 + lane * 16, b, (i * 64 + lane) / TL::UPR, &s_odd[wave]);
-            values(st, s_v);
+            values(st, s_v, std::true_type{});
             if (border) {
                 const uint32_t odd = uni(s_odd[wave]);
                 if (odd) add_odd(b, odd);

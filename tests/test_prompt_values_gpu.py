@@ -6,7 +6,8 @@ import math
 import pytest
 import torch
 
-from test_prompt_gpu import INF, NAN, Case, _put
+from test_cache_ops_gpu import F32
+from test_prompt_gpu import INF, NAN, Case, _exact, _put
 
 pytestmark = pytest.mark.gpu
 
@@ -109,3 +110,30 @@ def test_scores_further_apart_than_float32_reaches(m, P, n):
         # in log2 and of the exponential, twice, and the sums' steps
         tol = V.abs().amax() * (2 * 3.0 * (2.0 ** -20 + 3 * 2.0 ** -23) + 2.0 ** -21 + (2 * sees + 2) * 2.0 ** -24)
         assert bool(((c.out[j, 0].double() - want).abs() <= tol).all()), j
+
+
+def _tol_few(out, size, dots, d, m):
+    """As _tol, with the weights in two terms: half a step of half a step, 2^-16."""
+    score = 2 * ((d + 4) * 2.0 ** -24 * dots + 2.0 ** -22)
+    return out.abs() * 2.0 ** -8 + size * (2.0 ** -16 + score + 2 * m * 2.0 ** -24) + 1e-37
+
+
+@pytest.mark.parametrize("kind,hq,hkv,d", [("bf16", 8, 2, 128), ("bf16", 2, 2, 64), ("bf16", 8, 1, 64), ("bf16", 4, 2, 128), ("q8", 8, 2, 128),
+                                           ("q8", 2, 2, 64), ("q8", 8, 1, 128)])
+def test_few_rows_are_as_exact_as_the_decode_step(kind, hq, hkv, d):
+    """Values that nearly cancel show the weights' rounding: single and drafted tokens have them in two terms, as
+    the decode calls do."""
+    reqs = [(3, 1, 1), (9, 1, 2), (40, 4, 3), (200, 13, 1), (1500, 96, 4), (7000, 440, 1), (0, 1, 1), (33, 5, 32 // (hq // hkv))]
+    for rs in (reqs, [reqs[5]], [reqs[4]], [(m, P, 1) for m, P, _ in reqs * 10]):
+        _say(f"exact {kind} {hq}/{hkv} d {d}, {len(rs)} requests")
+        c = Case(kind, rs, hq, hkv, d, 4, heavy=0.3)
+        v = c.kv.v.view(torch.uint8) if kind == "q8" else c.kv.v
+        v[:, :, 1::2] = torch.where(torch.isnan(c.kv.v[:, :, 1::2].float()), v[:, :, 1::2], v[:, :, ::2] ^ 0x80 if kind == "q8" else -v[:, :, ::2])
+        c.call()
+        torch.cuda.synchronize()
+        scale = float(torch.tensor(c.scale, dtype=F32))
+        for r, (m, P, n) in enumerate(rs):
+            got = c.out[c.starts[r]:c.starts[r + 1]].double()
+            want, size, dots = _exact(c.q[c.starts[r]:c.starts[r + 1]].double(), c.tokens(0, r, m + n), c.tokens(1, r, m + n), m, scale)
+            far = (got - want).abs() - _tol_few(want, size, dots, d, m + n)
+            assert bool((far <= 0).all()), (r, (m, P, n), float(far.max()), float((size * 2.0 ** -16).max()))
