@@ -656,7 +656,11 @@ gp_status_t gp_decode_attention_q8(const gp_kv8_layer_t *kv, const gp_page_state
  *    layer of a model but the last, between gp_append_rope with advance 0 and the
  *    next layer); a request without room for its n_r tokens (which the append
  *    then left out) gets zero outputs.  advanced != 0: they do, c_r = m_r - n_r (a
- *    token for which c_r + j + 1 <= 0 gets a zero output).
+ *    token for which c_r + j + 1 <= 0 gets a zero output).  A request that the append left
+ *    out cannot be told from one that it served then: its rows are not zero, they attend
+ *    over older tokens, each over n_r fewer than there are.  Where requests can be without room keep
+ *    advance and advanced 0 in all layers and let the lengths and positions of those that were
+ *    granted theirs grow behind the last (or leave the others out of tok_start).
  *  - A held request is left out: its rows of out are not written, nor are rows that
  *    belong to no request.  A row whose weights have no positive sum gets zeros, as in
  *    gp_decode_attention.  Tokens that a row does not see are never used, whatever

@@ -772,7 +772,7 @@ def gp_prompt_attention(kv: KVLayer, ps: PageState, q: torch.Tensor, scale: floa
                         tok_start: torch.Tensor | None = None, advanced: bool = False, stream=None) -> None:
     """New tokens attend over the cache that already holds them: q [T, Hq, d] with any stride from
     token to token, out [T, Hq, d]; tok_start [R + 1] int32, or None for one token per request;
-    advanced: seq_lens count the new tokens."""
+    advanced: seq_lens count the new tokens (all requests have had room for theirs)."""
     _prompt("gp_prompt_attention", kv, kv.k.dtype, ps, q, scale, out, ws, tok_start, advanced, stream)
 
 
