@@ -604,7 +604,8 @@ typedef struct {
  *  - otherwise by how often a pair turns over the first `context` tokens, u_i =
  *    context f_i / 2 pi: pairs of more than high_turns turns keep f_i, those of
  *    less than low_turns get f_i / factor, and in between f_i (w + (1 - w) /
- *    factor) with w = (u_i - low_turns) / (high_turns - low_turns).
+ *    factor) with w = (u_i - low_turns) / (high_turns - low_turns).  The ramp is linear in the
+ *    turns; a model whose ramp runs over the pair's index brings a list of its own.
  * factor >= 1, 0 <= low_turns < high_turns, theta, context > 0, all finite; rotary_dim
  * even, 2 to 128 (GP_ERR_INVALID). */
 gp_status_t gp_rope_frequencies(double *freq, int32_t rotary_dim, double theta, double factor,

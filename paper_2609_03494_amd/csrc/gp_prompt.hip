@@ -19,7 +19,7 @@
 // the decode step does (2^-16 of a weight at most): they wait for the cache, and 64 single tokens take 235 us with one
 // term or two, five behind 6001 15.0 (60 single tokens of 8 heads per KV head at d 64, where little is read: 127.2 and 128.3).  Items of
 // more rows have one (half a step, 2^-8 of a weight): three products for two cost them a third and more (8 chunks of 1024 behind
-// 8192, below: 1072 and 1469 us, d 64 636 and 880, 8 bits 1197 and 1605), for a relative error (2-norm, random values) of
+// 8192, see below, in turn on one card: 1072 and 1469 us, d 64 636 and 880, 8 bits 1197 and 1605), for a relative error (2-norm, random values) of
 // 0.00166 in place of 0.00183, where the output's own rounding is 0.00166.
 //
 // Two paths, by an item's rows.  More than 32 (wide): the four waves share the blocks, and a wave works
@@ -28,12 +28,12 @@
 // drafted and single tokens, ends of requests): bound by reading the cache, so every wave has blocks of its own
 // and no barrier, and the waves' results meet in LDS at the end.
 //
-// Bound (8 chunks of 1024 tokens behind 8192, 32/8 heads): the matrix unit and with it the chip's power at
-// head_dim 128, 1097 TFLOP/s in 1067 us, where a library's product of two 8192 x 8192 matrices
-// reaches 1154; head_dim 64 has half of the products per weight and is bound by the vector instructions of
-// the softmax (16 exponentials of 16 cycles are half of them): 620 us, 940 TFLOP/s.  8-bit: each code is widened
-// once a workgroup, 1184 us and 987 TFLOP/s, 750 and 778.  float32: its matrix instructions' rate, 1063 us for a quarter
-// of it, 137 TFLOP/s of 153.  64 single tokens behind 1024 to 8143: the read of the cache, 5.1 TB/s.
+// Bound (8 chunks of 1024 tokens behind 8192, 32/8 heads; cards differ by 10 %, a library's product of two 8192 x 8192
+// matrices with them; this one's reaches 1094 TFLOP/s): the matrix unit and with it the chip's power at head_dim 128, 1155 us, 1011 TFLOP/s; head_dim
+// 64 has half of the products per weight and is bound by the vector instructions of the softmax (16 exponentials of
+// 16 cycles are half of them): 681 us, 858 TFLOP/s.  8-bit: each code is widened once a workgroup, 1284 us and 910
+// TFLOP/s, 803 and 727.  float32: its matrix instructions' rate, 1062 us for 4 of 512 behind 4096,
+// 137 TFLOP/s of 154.  64 single tokens behind 1024 to 8143: the read of the cache, 5.1 TB/s.
 // Tried and slower: the sum of weights by the matrix unit as well (bf16, head_dim 64: 5 %), keys widened by two waves
 // and values by the others (8 bits, head_dim 64: 1 %), the merge by whoever ends an item last (5 tokens behind 6001:
 // 24 us against 15).
@@ -228,8 +228,8 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PromptArgs a) {
     // pass 1: pieces per bucket; 2: pieces to their places.  Few items all start at once: any order
     const bool sorted = s_items > a.slots / 2;
     // Of many items a request's go out one after the other, longest first, requests by their longest: workgroups that run
-    // at the same time then read the same keys and values, from the XCD's L2 (60 prompts of 150 to 2330 tokens 1245 us,
-    // 1125 so; 12 of 200 to 6000 1147 and 1119; 8 chunks of 1024 behind 8192 1092 and 1067).  Of few, each by its own
+    // at the same time then read the same keys and values, from the XCD's L2 (60 prompts of 150 to 2330 tokens 1242 us,
+    // 1117 so; two batches of 12 of 200 to 6000 1145 and 1124, 1096 and 1084; 8 chunks of 1024 behind 8192 1096 and 1058, at head_dim 64 620 and 625).  Of few, each by its own
     // length: the last ones should be short (six prompts of 300 to 1900 tokens in float32: 207 us, request by request 245)
     const bool grouped = s_items >= 3 * a.slots;
     for (int pass = sorted ? 1 : 2; pass < 3; ++pass) {
